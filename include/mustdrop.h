@@ -6,6 +6,7 @@
  *   mustdrop_encode_merge    Sec. 3.3  Local Spatial Merging (Eq. 5) + Key Retaining (Eq. 6-7)
  *   mustdrop_prefill_filter  Sec. 3.4  dual-attention filtering (Eq. 8-10) + token drop
  *   mustdrop_decode_evict    Sec. 3.5  output-aware cache policy, one decode step
+ * and, behind them, a paged cache held in 4 bits with the attention that reads it (mustdrop_cache4_*).
  *
  * Conventions common to all calls
  *   - Every data pointer is DEVICE memory owned by the caller (inputs, outputs and the workspace).
@@ -61,7 +62,7 @@ enum { MD_FILTER_BUDGET = 0, MD_FILTER_THRESHOLD = 1 };
 /* Thread-local text of the last error returned on this thread ("" if none). */
 const char* mustdrop_last_error(void);
 
-/* Library version, major*100 + minor (2: mustdrop_prefill_filter takes row_lse). */
+/* Library version, major*100 + minor (2: mustdrop_prefill_filter takes row_lse; 3: the cache held in 4 bits). */
 int mustdrop_version(void);
 
 /* ------------------------------------------------------------------------------------------
@@ -331,6 +332,85 @@ int mustdrop_decode_keep_strided(
     int n_layers, int B, int Lcap, int H, int d,
     int32_t* evicted_ids, int32_t* evicted_count,
     const md_kv_layout* cache_layout, int64_t layer_stride,
+    void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * A cache held in 4 bits, in pages (the cache of Eq. 3-4 in a smaller form).  What the stages above keep -- the rows of
+ * mustdrop_prefill_filter (k_out, v_out, with out_len rows per sample), then one entry per step -- goes into pages of a pool
+ * that all samples share, and attention reads the pages.
+ *
+ * Numbers.  32 consecutive channels of one token and head are 32 four-bit numbers (bit 3: sign, bits 0-2: index of the magnitude
+ * among 0, 0.5, 1, 1.5, 2, 3, 4, 6) times one scale 2^e.  With a the largest magnitude of the 32 and k = floor(log2 a): e = k - 2,
+ * or k - 1 where a >= 1.75 * 2^k (a is then rounded to 6 at most and not cut down to it), at least -100 and at most 125, and -100
+ * where a = 0.  x becomes the nearest value to x / 2^e, of two as near the one of the even index.  The scale is the byte e + 127;
+ * a group with an infinity or a NaN has 255 and all of it reads as NaN.  A value is off by at most a
+ * fifth of the group's largest magnitude, and by at most a fifth of itself where it is no smaller than a quarter of that.
+ *
+ * Pool.  [n_pages, H] pieces of page * (d + d/16) bytes (mustdrop_cache4_bytes in all), each one after the other
+ *   K codes [page, d/2] (channel 2i in the low half of byte i), K scales [page, d/32],
+ *   V codes [page/4, 16, 4, d/32] (four tokens side by side: their bytes of the d/16 channels of each sixteenth of the row),
+ *   V scales [page/4, d/32, 4].
+ * Nothing in the pool needs clearing: what lies behind a sample's length is not used, whatever it holds.
+ *
+ * Block table.  table [B, max_pages] i32: entry e of sample b names the page of its entries e*page .. e*page + page-1; entries
+ * behind ceil(len/page) are not read.  slot = page number * page + place in the page, i32; -1: none.  A page number outside the
+ * pool names no page: its entries take no part in attention, its rows are not read out; a slot outside the pool is not written.
+ *
+ * Limits of the cache4 calls: d in {64, 128}; page a power of two from 16 to 256; n_pages * page < 2^31,
+ * max_pages * page < 2^30; H <= 65535; rows in MD_BF16 or MD_F32; base pointers 16-byte aligned.  md_kv_layout as above
+ * (elements of the rows' type); NULL = dense token-major.
+ */
+size_t mustdrop_cache4_bytes(int n_pages, int page, int H, int d);      /* 0 for sizes that no call takes */
+
+/* Block tables and slots from lengths: every sample b is to hold new_len[b] entries, where it held len[b].  Both are taken as 0
+ * where negative and as max_pages*page where larger.  A sample holds ceil(length / page) pages.  Pages that are not needed any
+ * more go onto the stack of free pages, in the order of samples and entries, the first one uppermost; then the pages that are
+ * needed come off its top, in the order of samples and entries.  A call that takes back what another one did therefore leaves
+ * the stack as it was.
+ *   new_len  [B];  len [B] in/out;  table [B, max_pages] in/out (entries that are not taken in this call stay as they are,
+ *            released ones among them)
+ *   free_pages [n_pages] in/out: the stack, its bottom first;  n_free [1] in/out: its height
+ *   slots    [B, N]: slots of the new entries, slots[b][i] that of entry len[b] + i (len as it was), -1 from new_len[b] on; NULL if N = 0
+ *   missing  [1]: pages that the pool is short of.  If not 0, nothing else is changed, and the slots are all -1.
+ * One page per entry of the stack and the tables: a page named twice is handed out twice.  Errors: MD_EINVAL, MD_ESHAPE
+ * (limits, B > 65535), MD_EALIAS, MD_EALIGN, MD_EWORKSPACE, MD_EHIP. */
+size_t mustdrop_cache4_pages_workspace_bytes(int B);
+
+int mustdrop_cache4_pages(
+    const int32_t* new_len, int32_t* len, int32_t* table, int32_t* free_pages, int32_t* n_free, int32_t* slots, int32_t* missing,
+    int B, int max_pages, int n_pages, int page, int N, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rows into the cache: k_new, v_new [B, N, H, d] (dtype; rows_layout), row (b, i) to slots[b][i], rows without a slot not at all.
+ * No two rows of a call may have the same slot (the slot then holds parts of both).  Errors: MD_EINVAL, MD_ESHAPE, MD_EDTYPE,
+ * MD_EALIGN, MD_EALIAS (the rows or slots overlap the cache), MD_EHIP. */
+int mustdrop_cache4_write(
+    const void* k_new, const void* v_new, md_dtype dtype, const int32_t* slots, void* cache,
+    int B, int N, int H, int d, int n_pages, int page, const md_kv_layout* rows_layout, void* stream);
+
+/* Rows out of the cache, as the dense stages take them (mustdrop_decode_evict): k_out, v_out [B, N, H, d] (dtype; rows_layout),
+ * row (b, i) the entry first[b] + i; rows of entries outside 0 .. len[b]-1 are left untouched.  first [B] i32 or NULL (0).  The values
+ * are exact in bf16, but for magnitudes beyond its range (none that the write makes).  Errors as for mustdrop_cache4_write. */
+int mustdrop_cache4_read(
+    const void* cache, const int32_t* table, const int32_t* len, const int32_t* first, void* k_out, void* v_out, md_dtype dtype,
+    int B, int N, int H, int d, int n_pages, int page, int max_pages, const md_kv_layout* rows_layout, void* stream);
+
+/* Attention over the cache (Eq. 4), for the last q_len[b] entries of every sample: query row i stands at entry
+ * len[b] - q_len[b] + i and sees the entries up to its own, but for those that `keep` leaves out.  N = 1 is the decode step, a few
+ * rows a draft, many a piece of a prompt (whose entries are written before the call).  Query head h reads K/V head h / (Hq/H).
+ *   out = sum_j p_j v_j,  p = softmax_j(softmax_scale * q . k_j);  lse = the natural logarithm of the sum of exp(softmax_scale * q . k_j)
+ *   q        [B, N, Hq, d] (dtype; q_layout);  Hq a multiple of H
+ *   q_len    [B] i32 or NULL (= N); taken as 0 where negative, as N where larger;  len [B] i32, likewise within 0 .. max_pages*page
+ *   keep     [B, max_pages*page] u8 or NULL (all): entries with keep 0 are seen by no row (they may hold anything)
+ *   out      [B, N, Hq, d] (dtype; out_layout), rows >= q_len[b] untouched;  lse [B, Hq, N] f32 or NULL, likewise
+ * A row that sees no entry gets out = 0 and lse = -infinity.  Scores, sums and the running maximum are fp32; a probability
+ * enters the product with V as a sum of bf16 parts that carries 16 bits (24 for MD_F32).  Two calls on the same inputs give the
+ * same bits.  Errors: MD_EINVAL, MD_ESHAPE, MD_EDTYPE, MD_EALIGN (keep 4-byte aligned), MD_EALIAS, MD_EWORKSPACE, MD_EHIP. */
+size_t mustdrop_cache4_attend_workspace_bytes(int B, int N, int Hq, int H, int d, int max_pages, int page);
+
+int mustdrop_cache4_attend(
+    const void* q, md_dtype dtype, const void* cache, const int32_t* table, const int32_t* len, const int32_t* q_len, const uint8_t* keep,
+    int B, int N, int Hq, int H, int d, int n_pages, int page, int max_pages, float softmax_scale,
+    void* out, float* lse, const md_kv_layout* q_layout, const md_kv_layout* out_layout,
     void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus

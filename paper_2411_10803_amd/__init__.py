@@ -11,6 +11,8 @@ from .binding import (  # noqa: F401
     mustdrop_encode_merge_noalloc, mustdrop_prefill_filter,
     KvLayout, mustdrop_decode_append_strided, mustdrop_decode_evict_strided, mustdrop_decode_keep_strided,
     mustdrop_prefill_filter_strided,
+    cache4_buffer, cache4_pages_workspace, cache4_workspace, mustdrop_cache4_attend, mustdrop_cache4_pages, mustdrop_cache4_read,
+    mustdrop_cache4_write,
 )
 
 __all__ = [
@@ -20,4 +22,6 @@ __all__ = [
     "mustdrop_decode_keep", "mustdrop_encode_merge_adaptive", "mustdrop_encode_merge_noalloc",
     "KvLayout", "mustdrop_prefill_filter_strided", "mustdrop_decode_evict_strided", "mustdrop_decode_append_strided",
     "mustdrop_decode_keep_strided",
+    "cache4_buffer", "cache4_pages_workspace", "cache4_workspace", "mustdrop_cache4_pages", "mustdrop_cache4_write",
+    "mustdrop_cache4_read", "mustdrop_cache4_attend",
 ]

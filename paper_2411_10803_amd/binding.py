@@ -21,6 +21,8 @@ EXPORTS = [
     "mustdrop_decode_evict_workspace_bytes", "mustdrop_decode_evict", "mustdrop_decode_append", "mustdrop_decode_keep",
     "mustdrop_prefill_filter_strided", "mustdrop_decode_evict_strided", "mustdrop_decode_append_strided",
     "mustdrop_decode_keep_strided",
+    "mustdrop_cache4_bytes", "mustdrop_cache4_pages_workspace_bytes", "mustdrop_cache4_pages", "mustdrop_cache4_write",
+    "mustdrop_cache4_read", "mustdrop_cache4_attend_workspace_bytes", "mustdrop_cache4_attend",
     "mustdrop_profile_start", "mustdrop_profile_stop",
 ]
 
@@ -51,11 +53,13 @@ def library() -> C.CDLL:
         lib.mustdrop_last_error.restype = C.c_char_p
         lib.mustdrop_version.restype = C.c_int
         for n in ("mustdrop_encode_merge_workspace_bytes", "mustdrop_prefill_filter_workspace_bytes",
-                  "mustdrop_decode_evict_workspace_bytes"):
+                  "mustdrop_decode_evict_workspace_bytes", "mustdrop_cache4_bytes", "mustdrop_cache4_pages_workspace_bytes",
+                  "mustdrop_cache4_attend_workspace_bytes"):
             getattr(lib, n).restype = C.c_size_t
         for n in ("mustdrop_encode_merge", "mustdrop_encode_merge_adaptive", "mustdrop_encode_merge_noalloc", "mustdrop_prefill_filter", "mustdrop_decode_evict", "mustdrop_decode_append",
                   "mustdrop_decode_keep", "mustdrop_prefill_filter_strided", "mustdrop_decode_evict_strided",
-                  "mustdrop_decode_append_strided", "mustdrop_decode_keep_strided"):
+                  "mustdrop_decode_append_strided", "mustdrop_decode_keep_strided", "mustdrop_cache4_pages",
+                  "mustdrop_cache4_write", "mustdrop_cache4_read", "mustdrop_cache4_attend"):
             getattr(lib, n).restype = C.c_int
         _lib = lib
     return _lib
@@ -81,6 +85,10 @@ _SIGNATURES = {
     "mustdrop_decode_append_strided": _APPEND + "p" + "p",
     "mustdrop_decode_keep": _KEEP + "pzp",
     "mustdrop_decode_keep_strided": _KEEP + "pl" + "pzp",
+    "mustdrop_cache4_pages": "p" * 7 + "i" * 5 + "pzp",
+    "mustdrop_cache4_write": "ppipp" + "i" * 6 + "pp",
+    "mustdrop_cache4_read": "p" * 6 + "i" * 8 + "pp",
+    "mustdrop_cache4_attend": "pi" + "p" * 5 + "i" * 8 + "f" + "p" * 4 + "pzp",
 }
 _functions: Dict[str, object] = {}
 
@@ -408,6 +416,169 @@ def mustdrop_decode_keep_strided(k_caches, v_caches, keep, acc, ids, protect, le
         _ptr(evicted_ids), _ptr(evicted_count), C.byref(lay), k_caches.stride(0),
         _ptr(workspace), workspace.numel(), _stream(stream))
     return workspace
+
+
+def _same_device(*tensors):
+    """The launch goes to the current device: every tensor has to be there."""
+    import torch
+    here = None
+    for t in tensors:
+        if t is None:
+            continue
+        if t.device.type != "cuda":
+            raise ValueError(f"tensors must be on the GPU, not on {t.device}")
+        if here is None:
+            here = torch.cuda.current_device()
+        if t.device.index != here:
+            raise ValueError(f"a tensor on {t.device} in a call on device {here}: make its device the current one")
+
+
+def _typed(dtype, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+
+
+def _shaped(name, t, shape):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+
+
+def _pool(cache, d):
+    """(pages, heads, tokens of a page) of a cache held in 4 bits, uint8 [n_pages, H, page * (d + d / 16)]."""
+    import torch
+    _typed(torch.uint8, cache=cache)
+    if cache.dim() != 3 or d % 16 or cache.shape[2] % (d + d // 16):
+        raise ValueError(f"cache must be [n_pages, H, page * (d + d / 16)] with d = {d}, not {tuple(cache.shape)}")
+    return cache.shape[0], cache.shape[1], cache.shape[2] // (d + d // 16)
+
+
+def _same_layout(a, b):
+    return (a.batch, a.token, a.head) == (b.batch, b.token, b.head)
+
+
+def _rows_layout(t, what):
+    """md_kv_layout of a [B, N, H, d] view, with strides that the library takes also where an axis has one element."""
+    if t.dim() != 4 or t.stride(3) != 1:
+        raise ValueError(f"{what} must be [B, N, H, d] with contiguous d")
+    n, st = t.shape, list(t.stride())
+    for a in range(3):                                     # (torch leaves any number there)
+        if n[a] == 1:
+            st[a] = max([n[3]] + [st[c] * n[c] for c in range(3) if c != a and n[c] > 1])
+    return KvLayout(st[0], st[1], st[2])
+
+
+def cache4_buffer(n_pages, page, H, d, device="cuda"):
+    """The pool of a cache held in 4 bits: uint8 [n_pages, H, page * (d + d / 16)]."""
+    import torch
+    nbytes = library().mustdrop_cache4_bytes(int(n_pages), int(page), int(H), int(d))
+    if nbytes == 0:
+        raise ValueError(library().mustdrop_last_error().decode())
+    return torch.zeros(nbytes, dtype=torch.uint8, device=device).view(n_pages, H, nbytes // (n_pages * H))
+
+
+def cache4_pages_workspace(B, device="cuda"):
+    return _workspace(library().mustdrop_cache4_pages_workspace_bytes(B), device)
+
+
+def cache4_workspace(q, cache, table):
+    """Workspace of mustdrop_cache4_attend for queries [B, N, Hq, d] on this pool with block tables [B, max_pages]."""
+    B, N, Hq, d = q.shape
+    _, H, page = _pool(cache, d)
+    n = library().mustdrop_cache4_attend_workspace_bytes(B, N, Hq, H, d, table.shape[1], page)
+    return _workspace(n, q.device)
+
+
+def mustdrop_cache4_pages(new_len, length, table, free_pages, n_free, missing, page, slots=None, workspace=None, stream=None):
+    """Block tables and slots: every sample is to hold new_len entries; length, table, free_pages and n_free are updated in
+    place, slots [B, N] (or None) receives the slots of the new entries, missing [1] what the pool is short of (then nothing
+    else changes).  All int32.  Returns the workspace used."""
+    import torch
+    B, max_pages = table.shape
+    _typed(torch.int32, new_len=new_len, length=length, table=table, free_pages=free_pages, n_free=n_free, missing=missing, slots=slots)
+    for name, t in (("new_len", new_len), ("length", length)):
+        _shaped(name, t, (B,))
+    for name, t in (("n_free", n_free), ("missing", missing)):
+        _shaped(name, t, (1,))
+    N = 0 if slots is None else slots.shape[1]
+    _shaped("slots", slots, (B, N))
+    _same_device(new_len, length, table, free_pages, n_free, missing, slots, workspace)
+    if workspace is None:
+        workspace = cache4_pages_workspace(B, table.device)
+    _call("mustdrop_cache4_pages",
+        _ptr(new_len), _ptr(length), _ptr(table), _ptr(free_pages), _ptr(n_free), _ptr(slots), _ptr(missing),
+        B, max_pages, free_pages.shape[0], int(page), N,
+        _ptr(workspace), workspace.numel(), _stream(stream))
+    return workspace
+
+
+def mustdrop_cache4_write(k_new, v_new, slots, cache, stream=None):
+    """Rows [B, N, H, d] (bf16 / f32 views of one layout) into the cache, at slots [B, N]."""
+    import torch
+    B, N, H, d = k_new.shape
+    n_pages, heads, page = _pool(cache, d)
+    _typed(torch.int32, slots=slots)
+    _typed(k_new.dtype, v_new=v_new)
+    _shaped("v_new", v_new, k_new.shape)
+    _shaped("slots", slots, (B, N))
+    lay = _rows_layout(k_new, "k_new")
+    if heads != H or not _same_layout(lay, _rows_layout(v_new, "v_new")):
+        raise ValueError("k_new and v_new must have the heads of the cache and one layout")
+    _same_device(k_new, v_new, slots, cache)
+    _call("mustdrop_cache4_write",
+        _view_ptr(k_new), _view_ptr(v_new), _dtype_code(k_new), _ptr(slots), _ptr(cache),
+        B, N, H, d, n_pages, page, C.byref(lay), _stream(stream))
+
+
+def mustdrop_cache4_read(cache, table, length, k_out, v_out, first=None, stream=None):
+    """Entries first .. of the cache into k_out, v_out [B, N, H, d] (bf16 / f32 views of one layout); rows of entries from length on
+    are left as they are."""
+    import torch
+    B, N, H, d = k_out.shape
+    n_pages, heads, page = _pool(cache, d)
+    _typed(torch.int32, table=table, length=length, first=first)
+    _typed(k_out.dtype, v_out=v_out)
+    _shaped("v_out", v_out, k_out.shape)
+    _shaped("table", table, (B, table.shape[-1]))
+    _shaped("length", length, (B,))
+    _shaped("first", first, (B,))
+    lay = _rows_layout(k_out, "k_out")
+    if heads != H or not _same_layout(lay, _rows_layout(v_out, "v_out")):
+        raise ValueError("k_out and v_out must have the heads of the cache and one layout")
+    _same_device(cache, table, length, k_out, v_out, first)
+    _call("mustdrop_cache4_read",
+        _ptr(cache), _ptr(table), _ptr(length), _ptr(first), _view_ptr(k_out), _view_ptr(v_out), _dtype_code(k_out),
+        B, N, H, d, n_pages, page, table.shape[1], C.byref(lay), _stream(stream))
+
+
+def mustdrop_cache4_attend(q, cache, table, length, softmax_scale, out=None, lse=None, q_len=None, keep=None, workspace=None, stream=None):
+    """Attention of q [B, N, Hq, d] (bf16 / f32, any layout) over the cache, each sample's rows at its last entries (causal).
+    Returns out (made as zeros if None); lse [B, Hq, N] f32, q_len [B] int32 and keep [B, max_pages * page] uint8 may be None."""
+    import torch
+    B, N, Hq, d = q.shape
+    n_pages, H, page = _pool(cache, d)
+    if out is None:
+        out = torch.zeros((B, N, Hq, d), dtype=q.dtype, device=q.device)
+    _typed(torch.int32, table=table, length=length, q_len=q_len)
+    _typed(torch.float32, lse=lse)
+    _typed(torch.uint8, keep=keep)
+    _typed(q.dtype, out=out)
+    _shaped("out", out, q.shape)
+    _shaped("table", table, (B, table.shape[-1]))
+    _shaped("length", length, (B,))
+    _shaped("q_len", q_len, (B,))
+    _shaped("lse", lse, (B, Hq, N))
+    _shaped("keep", keep, (B, table.shape[1] * page))
+    _same_device(q, cache, table, length, out, lse, q_len, keep, workspace)
+    if workspace is None:
+        workspace = cache4_workspace(q, cache, table)
+    lq, lo = _rows_layout(q, "q"), _rows_layout(out, "out")
+    _call("mustdrop_cache4_attend",
+        _view_ptr(q), _dtype_code(q), _ptr(cache), _ptr(table), _ptr(length), _ptr(q_len), _ptr(keep),
+        B, N, Hq, H, d, n_pages, page, table.shape[1], softmax_scale,
+        _view_ptr(out), _ptr(lse), C.byref(lq), C.byref(lo),
+        _ptr(workspace), workspace.numel(), _stream(stream))
+    return out
 
 
 def profile_start():
