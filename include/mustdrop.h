@@ -357,7 +357,7 @@ int mustdrop_decode_keep_strided(
  * pool names no page: its entries take no part in attention, its rows are not read out; a slot outside the pool is not written.
  *
  * Limits of the cache4 calls: d in {64, 128}; page a power of two from 16 to 256; n_pages * page < 2^31,
- * max_pages * page < 2^30; H <= 65535; rows in MD_BF16 or MD_F32; base pointers 16-byte aligned.  md_kv_layout as above
+ * max_pages * page < 2^30; a pool of at most 256 GiB; H <= 65535; rows in MD_BF16 or MD_F32; base pointers 16-byte aligned.  md_kv_layout as above
  * (elements of the rows' type); NULL = dense token-major.
  */
 size_t mustdrop_cache4_bytes(int n_pages, int page, int H, int d);      /* 0 for sizes that no call takes */
@@ -403,8 +403,9 @@ int mustdrop_cache4_read(
  *   keep     [B, max_pages*page] u8 or NULL (all): entries with keep 0 are seen by no row (they may hold anything)
  *   out      [B, N, Hq, d] (dtype; out_layout), rows >= q_len[b] untouched;  lse [B, Hq, N] f32 or NULL, likewise
  * A row that sees no entry gets out = 0 and lse = -infinity.  Scores, sums and the running maximum are fp32; a probability
- * enters the product with V as a sum of bf16 parts that carries 16 bits (24 for MD_F32).  Two calls on the same inputs give the
- * same bits.  Errors: MD_EINVAL, MD_ESHAPE, MD_EDTYPE, MD_EALIGN (keep 4-byte aligned), MD_EALIAS, MD_EWORKSPACE, MD_EHIP. */
+ * enters the product with V as a sum of bf16 parts that carries 24 bits for MD_F32 and 16 for MD_BF16, but 8 for MD_BF16 where more
+ * than 16 query rows share a K/V head and there are more than 512 tiles of 16 such rows in the call.  Two calls on the same
+ * inputs with tables of the same width give the same bits.  Errors: MD_EINVAL, MD_ESHAPE, MD_EDTYPE, MD_EALIGN (keep 4-byte aligned), MD_EALIAS, MD_EWORKSPACE, MD_EHIP. */
 size_t mustdrop_cache4_attend_workspace_bytes(int B, int N, int Hq, int H, int d, int max_pages, int page);
 
 int mustdrop_cache4_attend(

@@ -418,21 +418,6 @@ def mustdrop_decode_keep_strided(k_caches, v_caches, keep, acc, ids, protect, le
     return workspace
 
 
-def _same_device(*tensors):
-    """The launch goes to the current device: every tensor has to be there."""
-    import torch
-    here = None
-    for t in tensors:
-        if t is None:
-            continue
-        if t.device.type != "cuda":
-            raise ValueError(f"tensors must be on the GPU, not on {t.device}")
-        if here is None:
-            here = torch.cuda.current_device()
-        if t.device.index != here:
-            raise ValueError(f"a tensor on {t.device} in a call on device {here}: make its device the current one")
-
-
 def _typed(dtype, **tensors):
     for name, t in tensors.items():
         if t is not None and t.dtype != dtype:
@@ -440,32 +425,55 @@ def _typed(dtype, **tensors):
 
 
 def _shaped(name, t, shape):
-    if t is not None and tuple(t.shape) != tuple(shape):
+    if t is not None and t.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+
+
+def _here(stream, *tensors) -> int:
+    """The stream of a call, on the current device: a launch goes there, so every tensor has to be there."""
+    import torch
+    at = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and (t.get_device() != at or at < 0):
+            raise ValueError(f"tensors must be on one GPU: {t.device}, {tensors[0].device}")
+    if at != torch.cuda.current_device():
+        raise ValueError(f"tensors on device {at} in a call on device {torch.cuda.current_device()}: make theirs the current one")
+    return torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
 
 
 def _pool(cache, d):
     """(pages, heads, tokens of a page) of a cache held in 4 bits, uint8 [n_pages, H, page * (d + d / 16)]."""
     import torch
-    _typed(torch.uint8, cache=cache)
-    if cache.dim() != 3 or d % 16 or cache.shape[2] % (d + d // 16):
-        raise ValueError(f"cache must be [n_pages, H, page * (d + d / 16)] with d = {d}, not {tuple(cache.shape)}")
-    return cache.shape[0], cache.shape[1], cache.shape[2] // (d + d // 16)
+    if cache.dtype is not torch.uint8:
+        raise TypeError(f"cache must be torch.uint8, not {cache.dtype}")
+    shape, size = cache.shape, d + d // 16
+    if len(shape) != 3 or d % 16 or shape[2] % size:
+        raise ValueError(f"cache must be [n_pages, H, page * (d + d / 16)] with d = {d}, not {tuple(shape)}")
+    return shape[0], shape[1], shape[2] // size
 
 
-def _same_layout(a, b):
-    return (a.batch, a.token, a.head) == (b.batch, b.token, b.head)
-
-
-def _rows_layout(t, what):
-    """md_kv_layout of a [B, N, H, d] view, with strides that the library takes also where an axis has one element."""
+def _rows(t, what):
+    """(pointer, md_kv_layout or None) of a [B, N, H, d] view; None for dense token-major memory.  An axis of one element gets a
+    stride that the library takes (torch leaves any number there)."""
+    if t.is_contiguous():
+        return t.data_ptr(), None
     if t.dim() != 4 or t.stride(3) != 1:
         raise ValueError(f"{what} must be [B, N, H, d] with contiguous d")
     n, st = t.shape, list(t.stride())
-    for a in range(3):                                     # (torch leaves any number there)
+    for a in range(3):
         if n[a] == 1:
             st[a] = max([n[3]] + [st[c] * n[c] for c in range(3) if c != a and n[c] > 1])
-    return KvLayout(st[0], st[1], st[2])
+    return t.data_ptr(), KvLayout(st[0], st[1], st[2])
+
+
+def _row_pair(k, v, names):
+    """Pointers and the one layout of two [B, N, H, d] views of one type and shape."""
+    _typed(k.dtype, **{names[1]: v})
+    _shaped(names[1], v, k.shape)
+    (kp, lay), (vp, other) = _rows(k, names[0]), _rows(v, names[1])
+    if (lay is None) != (other is None) or (lay and (lay.batch, lay.token, lay.head) != (other.batch, other.token, other.head)):
+        raise ValueError(f"{names[0]} and {names[1]} must have one layout")
+    return kp, vp, lay and C.byref(lay)
 
 
 def cache4_buffer(n_pages, page, H, d, device="cuda"):
@@ -495,20 +503,20 @@ def mustdrop_cache4_pages(new_len, length, table, free_pages, n_free, missing, p
     else changes).  All int32.  Returns the workspace used."""
     import torch
     B, max_pages = table.shape
-    _typed(torch.int32, new_len=new_len, length=length, table=table, free_pages=free_pages, n_free=n_free, missing=missing, slots=slots)
-    for name, t in (("new_len", new_len), ("length", length)):
-        _shaped(name, t, (B,))
-    for name, t in (("n_free", n_free), ("missing", missing)):
-        _shaped(name, t, (1,))
     N = 0 if slots is None else slots.shape[1]
+    _typed(torch.int32, new_len=new_len, length=length, table=table, free_pages=free_pages, n_free=n_free, missing=missing, slots=slots)
+    _shaped("new_len", new_len, (B,))
+    _shaped("length", length, (B,))
+    _shaped("n_free", n_free, (1,))
+    _shaped("missing", missing, (1,))
     _shaped("slots", slots, (B, N))
-    _same_device(new_len, length, table, free_pages, n_free, missing, slots, workspace)
+    raw = _here(stream, new_len, length, table, free_pages, n_free, missing, slots, workspace)
     if workspace is None:
         workspace = cache4_pages_workspace(B, table.device)
     _call("mustdrop_cache4_pages",
         _ptr(new_len), _ptr(length), _ptr(table), _ptr(free_pages), _ptr(n_free), _ptr(slots), _ptr(missing),
         B, max_pages, free_pages.shape[0], int(page), N,
-        _ptr(workspace), workspace.numel(), _stream(stream))
+        _ptr(workspace), workspace.numel(), raw)
     return workspace
 
 
@@ -518,16 +526,14 @@ def mustdrop_cache4_write(k_new, v_new, slots, cache, stream=None):
     B, N, H, d = k_new.shape
     n_pages, heads, page = _pool(cache, d)
     _typed(torch.int32, slots=slots)
-    _typed(k_new.dtype, v_new=v_new)
-    _shaped("v_new", v_new, k_new.shape)
     _shaped("slots", slots, (B, N))
-    lay = _rows_layout(k_new, "k_new")
-    if heads != H or not _same_layout(lay, _rows_layout(v_new, "v_new")):
-        raise ValueError("k_new and v_new must have the heads of the cache and one layout")
-    _same_device(k_new, v_new, slots, cache)
+    kp, vp, lay = _row_pair(k_new, v_new, ("k_new", "v_new"))
+    if heads != H:
+        raise ValueError(f"rows of {H} heads for a cache of {heads} heads")
+    raw = _here(stream, k_new, v_new, slots, cache)
     _call("mustdrop_cache4_write",
-        _view_ptr(k_new), _view_ptr(v_new), _dtype_code(k_new), _ptr(slots), _ptr(cache),
-        B, N, H, d, n_pages, page, C.byref(lay), _stream(stream))
+        kp, vp, _dtype_code(k_new), _ptr(slots), _ptr(cache),
+        B, N, H, d, n_pages, page, lay, raw)
 
 
 def mustdrop_cache4_read(cache, table, length, k_out, v_out, first=None, stream=None):
@@ -536,19 +542,18 @@ def mustdrop_cache4_read(cache, table, length, k_out, v_out, first=None, stream=
     import torch
     B, N, H, d = k_out.shape
     n_pages, heads, page = _pool(cache, d)
+    max_pages = table.shape[-1]
     _typed(torch.int32, table=table, length=length, first=first)
-    _typed(k_out.dtype, v_out=v_out)
-    _shaped("v_out", v_out, k_out.shape)
-    _shaped("table", table, (B, table.shape[-1]))
+    _shaped("table", table, (B, max_pages))
     _shaped("length", length, (B,))
     _shaped("first", first, (B,))
-    lay = _rows_layout(k_out, "k_out")
-    if heads != H or not _same_layout(lay, _rows_layout(v_out, "v_out")):
-        raise ValueError("k_out and v_out must have the heads of the cache and one layout")
-    _same_device(cache, table, length, k_out, v_out, first)
+    kp, vp, lay = _row_pair(k_out, v_out, ("k_out", "v_out"))
+    if heads != H:
+        raise ValueError(f"rows of {H} heads for a cache of {heads} heads")
+    raw = _here(stream, cache, table, length, k_out, v_out, first)
     _call("mustdrop_cache4_read",
-        _ptr(cache), _ptr(table), _ptr(length), _ptr(first), _view_ptr(k_out), _view_ptr(v_out), _dtype_code(k_out),
-        B, N, H, d, n_pages, page, table.shape[1], C.byref(lay), _stream(stream))
+        _ptr(cache), _ptr(table), _ptr(length), _ptr(first), kp, vp, _dtype_code(k_out),
+        B, N, H, d, n_pages, page, max_pages, lay, raw)
 
 
 def mustdrop_cache4_attend(q, cache, table, length, softmax_scale, out=None, lse=None, q_len=None, keep=None, workspace=None, stream=None):
@@ -557,27 +562,31 @@ def mustdrop_cache4_attend(q, cache, table, length, softmax_scale, out=None, lse
     import torch
     B, N, Hq, d = q.shape
     n_pages, H, page = _pool(cache, d)
+    max_pages = table.shape[-1]
     if out is None:
         out = torch.zeros((B, N, Hq, d), dtype=q.dtype, device=q.device)
     _typed(torch.int32, table=table, length=length, q_len=q_len)
-    _typed(torch.float32, lse=lse)
-    _typed(torch.uint8, keep=keep)
+    if lse is not None:
+        _typed(torch.float32, lse=lse)
+        _shaped("lse", lse, (B, Hq, N))
+    if keep is not None:
+        _typed(torch.uint8, keep=keep)
+        _shaped("keep", keep, (B, max_pages * page))
     _typed(q.dtype, out=out)
     _shaped("out", out, q.shape)
-    _shaped("table", table, (B, table.shape[-1]))
+    _shaped("table", table, (B, max_pages))
     _shaped("length", length, (B,))
     _shaped("q_len", q_len, (B,))
-    _shaped("lse", lse, (B, Hq, N))
-    _shaped("keep", keep, (B, table.shape[1] * page))
-    _same_device(q, cache, table, length, out, lse, q_len, keep, workspace)
+    raw = _here(stream, q, cache, table, length, out, lse, q_len, keep, workspace)
     if workspace is None:
         workspace = cache4_workspace(q, cache, table)
-    lq, lo = _rows_layout(q, "q"), _rows_layout(out, "out")
+    qp, lq = _rows(q, "q")
+    op, lo = _rows(out, "out")
     _call("mustdrop_cache4_attend",
-        _view_ptr(q), _dtype_code(q), _ptr(cache), _ptr(table), _ptr(length), _ptr(q_len), _ptr(keep),
-        B, N, Hq, H, d, n_pages, page, table.shape[1], softmax_scale,
-        _view_ptr(out), _ptr(lse), C.byref(lq), C.byref(lo),
-        _ptr(workspace), workspace.numel(), _stream(stream))
+        qp, _dtype_code(q), _ptr(cache), _ptr(table), _ptr(length), _ptr(q_len), _ptr(keep),
+        B, N, Hq, H, d, n_pages, page, max_pages, softmax_scale,
+        op, _ptr(lse), lq and C.byref(lq), lo and C.byref(lo),
+        _ptr(workspace), workspace.numel(), raw)
     return out
 
 

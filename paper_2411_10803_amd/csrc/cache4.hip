@@ -22,6 +22,8 @@ constexpr float kLog2eC = 1.4426950408889634f, kLn2C = 0.6931471805599453f;
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 struct Pool {
@@ -242,263 +244,788 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(
 
 // ------------------------------------------------------------------------------------------------ attention
 
-struct AttendDims { int B, N, G, tiles; };           // G: query heads of a K/V head; tiles: of 16 query rows
+constexpr int kRing = 2;                         // steps that a wave of the attention has on their way
+struct AttendDims { int B, N, G, tiles; };           // G: query heads of a K/V head; tiles: of query rows, in the longest case
 
-constexpr float kNoKey = -3.0e38f;                   // running maximum before the first key (below every finite score that matters)
+struct AttendArgs {
+    const void* q;
+    const uint8_t* cache;
+    const int32_t *table, *len, *q_len;
+    const uint8_t* keep;
+    void* out;
+    float* lse;
+    Pool p;
+    AttendDims dim;
+    float scale;
+    KvLayout ql, ol;
+};
 
-// fp32 as a sum of bf16 parts: two carry 16 bits, three carry all 24.
-template <int TERMS>
-__device__ __forceinline__ void split_bf16(float x, uint32_t (&part)[TERMS]) {
-#pragma unroll
-    for (int i = 0; i < TERMS; ++i) {
-        part[i] = f32_to_bf16(x);
-        x -= __uint_as_float(part[i] << 16);
+// Sums over a part of a unit's keys: tile rows of d channels, and the (maximum, sum) pairs.
+struct Parts {
+    float* o;                                        // [2 * blocks][tile rows][d]
+    float2* ml;                                      // [2 * blocks][tile rows]
+    int blocks, least;
+};
+
+#define MD_VM_WAIT(n) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory")
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+typedef const __attribute__((address_space(1))) void* global_ptr_t;
+
+constexpr float kNoKey = -3.0e38f;                   // running maximum before the first key (below every score that matters)
+// A running maximum may lag behind by this much (base 2) before the sums are scaled anew: probabilities up to 2^8 cost no accuracy.
+constexpr float kLag = 8.f;
+
+__device__ __forceinline__ uint32_t fp4_pair(uint32_t w, float s, int byte) {       // byte: a constant
+    switch (byte) {
+        case 0: return as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
+        case 1: return as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+        case 2: return as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
+        default: return as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
     }
 }
 
-// Sixteen query rows of one (sample, K/V head) per block, row r = i * G + g (token i, g-th query head of the K/V head); the
-// waves of the block take the 32-key steps in turn and join their sums at the end.
-//
-// A wave holds S^T = K Q^T in the 16x16 accumulators (lane: query n = lane % 16, keys 4 b + 0..3 with b = lane / 16), so the
-// probabilities are at once the right-hand operand of O^T = V^T P^T: with two 16-key tiles the eight contraction places of lane
-// group b are keys 4 b + 0..3 of either tile.  The pages hold V so that a lane loads those keys' codes of its channels, and of K so
-// that a lane loads d/4 channels of one token; nothing goes through LDS until the end.
-template <int D, bool F32>
-__global__ __launch_bounds__(256) void cache4_attend_kernel(
-    const void* __restrict__ q, const uint8_t* __restrict__ cache, const int32_t* __restrict__ table, const int32_t* __restrict__ len,
-    const int32_t* __restrict__ q_len, const uint8_t* __restrict__ keep, Pool p, AttendDims dim, float scale,
-    void* __restrict__ out, float* __restrict__ lse, KvLayout q_lay, KvLayout o_lay)
-{
-    constexpr int QT = F32 ? 3 : 1;                  // bf16 parts of a query: fp32 has 24 bits
-    constexpr int PT = F32 ? 3 : 2;                  // of a probability: in one part its rounding would be as large as the output's
-    constexpr int KS = D / 32;                       // contraction steps of S
-    constexpr int J = D / 16;                        // 16-channel tiles of O
-    constexpr int KB = D / 8;                        // bytes of codes a lane loads of a token's K, and of four tokens' V
-    __shared__ float s_o[4][16][D + 4];
-    __shared__ float s_m[4][16], s_l[4][16];
-    const int lane = lane_id(), wv = wave_id(), n = lane & 15, lb = lane >> 4;
-    const int tile = blockIdx.x % dim.tiles, bh = blockIdx.x / dim.tiles, h = bh % p.H, b = bh / p.H;
-    const int cap = p.max_pages << p.page_shift;
-    const int length = c4_clamp(len[b], 0, cap), nq = q_len ? c4_clamp(q_len[b], 0, dim.N) : dim.N;
-    const int live = nq * dim.G;                     // query rows of this sample and head
-    const int r0 = tile * 16;
-    if (r0 >= live) return;
-    const int r = r0 + n, i = r / dim.G, hq = h * dim.G + (r - i * dim.G);
-    // keys that a row sees: up to its own position
-    const int limit = r < live ? min(max(length - nq + i + 1, 0), length) : 0;
-    const int last = min(r0 + 15, live - 1);
-    const int end = min(max(length - nq + last / dim.G + 1, 0), length), full = max(length - nq + r0 / dim.G + 1, 0);
-
-    bf16x8 qf[KS][QT];
+// Two fp32 numbers as sums of bf16 parts, packed: two parts carry 16 bits, three carry all 24.
+template <int TERMS>
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t (&part)[TERMS]) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        float x[8] = {};
-        if (r < live) {
-            const long at = (long)b * q_lay.batch + (long)i * q_lay.token + (long)hq * q_lay.head + lb * (D / 4) + s * 8;
-            float y[8];
-            load_part<128, F32>(q, at, y);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = y[j];
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            uint32_t part[QT];
-            split_bf16<QT>(x[j], part);
-#pragma unroll
-            for (int t = 0; t < QT; ++t) qf[s][t][j] = __builtin_bit_cast(__bf16, (uint16_t)part[t]);
-        }
+    for (int i = 0; i < TERMS; ++i) {
+        part[i] = as_u32(__builtin_convertvector(f32x2{x, y}, bf16x2));
+        if (i + 1 < TERMS) { x -= bf16_lo(part[i]); y -= bf16_hi(part[i]); }
     }
+}
 
-    const float c = scale * kLog2eC;
-    float m = kNoKey, l = 0.f;
-    f32x4 o[J];
-#pragma unroll
-    for (int j = 0; j < J; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int32_t* row = table + (long)b * p.max_pages;
+// The larger of a value over the four lanes of one query (lane ^ 16, lane ^ 32), and the sum.
+__device__ __forceinline__ float max_over_groups(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16, kWave));
+    return fmaxf(v, __shfl_xor(v, 32, kWave));
+}
+__device__ __forceinline__ float sum_over_groups(float v) {
+    v += __shfl_xor(v, 16, kWave);
+    return v + __shfl_xor(v, 32, kWave);
+}
 
-    for (int t0 = wv * 32; t0 < end; t0 += 128) {
-        const uint8_t* base[2];
-        bool there[2];
-        int place[2];
+// A pointer to global memory.  (One that comes out of argument() below is any pointer to the compiler, whose accesses then wait for LDS too.)
+template <class T>
+__device__ __forceinline__ __attribute__((address_space(1))) T* global(T* p) { return reinterpret_cast<__attribute__((address_space(1))) T*>(reinterpret_cast<uintptr_t>(p)); }
+typedef const __attribute__((address_space(1))) uint8_t* bytes_t;
+template <class T>
+__device__ __forceinline__ T load_as(bytes_t p) { return *reinterpret_cast<const __attribute__((address_space(1))) T*>(p); }
+
+// Numbers that a whole wave wants and that no kernel here writes while one reads them: by the constant address space, which makes
+// the load a scalar one.  (As a vector load it would be waited for together with the keys on their way, which are younger.)
+typedef const __attribute__((address_space(4))) int32_t* uniform_ptr_t;
+__device__ __forceinline__ uniform_ptr_t uniform(const void* p) { return reinterpret_cast<uniform_ptr_t>(reinterpret_cast<uintptr_t>(p)); }
+
+// The kernel's arguments, read again: what only the beginning and the end of a unit want does not take scalar registers
+// while the keys go by (kept from the kernel's start on, 98 of them went through lanes of vector registers and back, step by step).
+template <class T>
+__device__ __forceinline__ T argument(int at) {
+    uintptr_t p = (uintptr_t)__builtin_amdgcn_kernarg_segment_ptr() + at;
+    asm volatile("" : "+s"(p));
+    int32_t w[sizeof(T) / 4];
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 4); ++i) w[i] = reinterpret_cast<uniform_ptr_t>(p)[i];
+    T r;
+    __builtin_memcpy(&r, w, sizeof(T));
+    return r;
+}
+constexpr int kPartsAt = (sizeof(AttendArgs) + 7) / 8 * 8;
+
+// What the entries of one sample look like to a call.
+struct Sample { int b, length, nq; };
+__device__ __forceinline__ Sample sample_of(const AttendArgs& A, int b) {
+    Sample s;
+    s.b = b;
+    s.length = c4_clamp(uniform(A.len)[b], 0, A.p.max_pages << A.p.page_shift);
+    s.nq = A.q_len ? c4_clamp(uniform(A.q_len)[b], 0, A.dim.N) : A.dim.N;
+    return s;
+}
+
+// What a walk over the keys of one (sample, K/V head) needs.
+struct Walk {
+    bytes_t base;                                    // of the head in page 0
+    uniform_ptr_t row, keep;                         // of the block table; of the mask, or null
+    uint32_t pitch;                                  // 64-byte units from page to page
+    int n_pages, page, page_shift, last_page;        // of the pool; tokens of a page; the table's last entry
+    int end, clear;                                  // keys that any row sees; that all rows see and no mask may leave out
+    float c;                                         // softmax scale, base 2
+};
+struct Pages { int id[2]; };                         // of a step's two 16-key tiles
+struct Kept { uint32_t w[2][4]; };                   // `keep` of a step's keys
+
+// rows: the first and the last one that count, of those that the sample and head have
+__device__ __forceinline__ Walk walk_of(const AttendArgs& A, const Sample& s, int h, int first_row, int last_row) {
+    Walk w;
+    w.base = global(A.cache) + h * A.p.stride;
+    w.row = uniform(A.table + (long)s.b * A.p.max_pages);
+    w.keep = A.keep ? uniform(A.keep + (long)s.b * (A.p.max_pages << A.p.page_shift)) : nullptr;
+    w.pitch = (uint32_t)(A.p.H * A.p.stride / 64);
+    w.n_pages = A.p.n_pages;
+    w.page = A.p.page;
+    w.page_shift = A.p.page_shift;
+    w.last_page = A.p.max_pages - 1;
+    w.end = min(max(s.length - s.nq + last_row / A.dim.G + 1, 0), s.length);
+    w.clear = A.keep ? 0 : min(max(s.length - s.nq + first_row / A.dim.G + 1, 0), w.end);
+    w.c = A.scale * kLog2eC;
+    return w;
+}
+// The entries as they stand in the table, which nobody looks at yet: a wave that asks for them a step ahead does not wait for them.
+__device__ __forceinline__ Pages pages_at(const Walk& w, int step) {
+    Pages r;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) r.id[u] = w.row[min((step * 32 + 16 * u) >> w.page_shift, w.last_page)];
+    return r;
+}
+// Whether they name pages that the step needs.
+__device__ __forceinline__ bool there(const Walk& w, int step, const Pages& p, int u) {
+    return step * 32 + 16 * u < w.end && c4_page_id(p.id[u], w.n_pages) >= 0;
+}
+__device__ __forceinline__ bool hole(const Walk& w, int step, const Pages& p) { return !(there(w, step, p, 0) && there(w, step, p, 1)); }
+// (page 0 is read in the place of one that is not there, and masked)
+__device__ __forceinline__ bytes_t page_base(const Walk& w, int id) {
+    return w.base + ((uint64_t)(((uint32_t)id < (uint32_t)w.n_pages ? (uint32_t)id : 0u) * w.pitch) << 6);
+}
+__device__ __forceinline__ Kept kept_at(const Walk& w, int step) {
+    Kept r;
+    if (w.keep) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int t = t0 + 16 * u;
-            const int id = t < end ? c4_page_id(__builtin_amdgcn_readfirstlane(row[t >> p.page_shift]), p.n_pages) : -1;
-            there[u] = id >= 0;                      // (page 0 is read in the place of one that is not there, and masked)
-            place[u] = t & (p.page - 1);
-            base[u] = cache + ((long)max(id, 0) * p.H + h) * p.stride;
+            const int at = min(step * 8 + 4 * u, ((w.last_page + 1) << w.page_shift) / 4 - 4);       // (of a tile within the mask; any will do behind the end)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) r.w[u][x] = w.keep[at + x];
         }
-        uint32_t kw[2][KB / 4], vw[2][KB / 4], ksc[2], vsc[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const uint8_t* kp = base[u] + c4_k_codes(place[u] + n, D) + lb * KB;
-            const uint8_t* vp = base[u] + c4_v_codes(p.page, place[u] + 4 * lb, n, D);
-            if (D == 128) {
-                const u32x4 a = *reinterpret_cast<const u32x4*>(kp), w = *reinterpret_cast<const u32x4*>(vp);
-#pragma unroll
-                for (int x = 0; x < KB / 4; ++x) { kw[u][x] = a[x]; vw[u][x] = w[x]; }
-            } else {
-                const u32x2 a = *reinterpret_cast<const u32x2*>(kp), w = *reinterpret_cast<const u32x2*>(vp);
-#pragma unroll
-                for (int x = 0; x < KB / 4; ++x) { kw[u][x] = a[x]; vw[u][x] = w[x]; }
-            }
-            ksc[u] = base[u][c4_k_scales(p.page, place[u] + n, D) + lb * D / 128];
-            vsc[u] = *reinterpret_cast<const uint32_t*>(base[u] + c4_v_scales(p.page, place[u] + 4 * lb, n * D / 512, D));
-        }
-        // which of this lane's keys its query row sees
-        uint32_t sees = 0xFF;
-        const bool masked = !there[0] || !there[1] || t0 + 32 > full || t0 + 32 > end || keep;
-        if (masked) {
-            sees = 0;
-            uint32_t drop = 0;                       // keys that no row sees: their V must not count, whatever it holds
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                uint32_t kept = 0x01010101u;
-                const int t = t0 + 16 * u + 4 * lb;
-                if (keep && t < cap) kept = *reinterpret_cast<const uint32_t*>(keep + (long)b * cap + t);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const bool on = there[u] && t + x < end && ((kept >> (8 * x)) & 0xFF) != 0;
-                    if (on && t + x < limit) sees |= 1u << (4 * u + x);
-                    if (!on) drop |= 1u << (4 * u + x);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    if (drop & (1u << (4 * u + x))) vsc[u] &= ~(0xFFu << (8 * x));
-            // A NaN in V of a key that some rows see and others do not: 0 * NaN would reach those too.  Its scale goes, and the
-            // rows that do see it get the NaN in that group's channels by themselves.
-            bool nan = false;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    if (((vsc[u] >> (8 * x)) & 0xFF) == 255) { nan = true; vsc[u] &= ~(0xFFu << (8 * x)); }
-            if (__any(nan)) {
-                float poison = 0.f;
-                for (int x = 0; x < 32; ++x) {
-                    const int u = x >> 4, t = t0 + x;
-                    if (!there[u] || t >= limit || (keep && keep[(long)b * cap + t] == 0)) continue;
-                    if (base[u][c4_v_scales(p.page, place[u] + (x & 15), lb * D / 128, D)] == 255) poison = __builtin_nanf("");
-                }
-#pragma unroll
-                for (int j = 0; j < J; ++j) o[j] += poison;
-            }
-        }
-        f32x4 st[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const float s = scale_of(ksc[u]);
-            f32x4 acc{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int y = 0; y < KS; ++y) {
-                uint32_t f[4];
-                f[0] = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(kw[u][y], s, 0));
-                f[1] = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(kw[u][y], s, 1));
-                f[2] = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(kw[u][y], s, 2));
-                f[3] = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(kw[u][y], s, 3));
-                const bf16x8 a = __builtin_bit_cast(bf16x8, u32x4{f[0], f[1], f[2], f[3]});
-#pragma unroll
-                for (int t = QT - 1; t >= 0; --t) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[y][t], acc, 0, 0, 0);
-            }
-            st[u] = acc;
-        }
-        // running maximum (base 2), probabilities
-        float x8[8], most = kNoKey;
+    } else {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const float v = st[u][x] * c;
-                x8[4 * u + x] = (sees >> (4 * u + x)) & 1 ? v : -INFINITY;
-                most = fmaxf(most, x8[4 * u + x]);
-            }
-        most = fmaxf(most, __shfl_xor(most, 16, kWave));
-        most = fmaxf(most, __shfl_xor(most, 32, kWave));
-        const float m2 = fmaxf(m, most), a = fast_exp2(m - m2);
-        m = m2;
-        l *= a;
+            for (int x = 0; x < 4; ++x) r.w[u][x] = 0x01010101u;
+    }
+    return r;
+}
+
+// 16 NT query rows of one (sample, K/V head) in a wave: queries, running maxima and sums.  Row r = i * G + g is the g-th query head
+// of the K/V head at token i.
+//
+// S^T = K Q^T stands in the 16x16 accumulators (lane: query n = lane % 16, keys 4 b + 0..3 with b = lane / 16), so the
+// probabilities are at once the right-hand operand of O^T = V^T P^T: with two 16-key tiles the eight contraction places of lane
+// group b are keys 4 b + 0..3 of either tile.  The pages hold V so that a lane loads those keys' codes of its channels, and of K so
+// that a lane loads d/4 channels of one token: from the loads to the matrix products no lane needs another's data.
+// PT: bf16 parts of a probability in the product with V; two carry 16 bits, one is as coarse as a bf16 output.
+template <int D, bool F32, int NT, int PT>
+struct Rows {
+    static constexpr int QT = F32 ? 3 : 1;           // bf16 parts of a query: fp32 has 24 bits
+    static constexpr int KS = D / 32;                // contraction steps of S
+    static constexpr int J = D / 16;                 // 16-channel tiles of O
+
+    bf16x8 q[NT][KS][QT];
+    float m[NT], l[NT];
+    f32x4 o[NT][J];
+    int limit[NT];                                   // keys that the lane's row sees: up to its own position
+    int n, lb;
+
+    __device__ __forceinline__ void begin(const AttendArgs& A, const Sample& s, int h, int r0) {
+        n = lane_id() & 15;
+        lb = lane_id() >> 4;
+        const int G = A.dim.G, live = s.nq * G;
 #pragma unroll
-        for (int j = 0; j < J; ++j) o[j] *= a;
-        uint32_t pw[PT][4];
+        for (int t = 0; t < NT; ++t) {
+            const int r = r0 + 16 * t + n, i = r / G, hq = h * G + (r - i * G);
+            limit[t] = r < live ? min(max(s.length - s.nq + i + 1, 0), s.length) : 0;
+            m[t] = kNoKey;
+            l[t] = 0.f;
+#pragma unroll
+            for (int j = 0; j < J; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int y = 0; y < KS; ++y) {
+                uint32_t w[QT][4] = {};
+                if (r < live) {
+                    const long at = (long)s.b * A.ql.batch + (long)i * A.ql.token + (long)hq * A.ql.head + lb * (D / 4) + y * 8;
+                    if (F32) {
+                        const bytes_t from = reinterpret_cast<bytes_t>(global(static_cast<const float*>(A.q)) + at);
+                        const f32x4 x[2] = {load_as<f32x4>(from), load_as<f32x4>(from + 16)};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            uint32_t part[QT];
+                            split_pair<QT>(x[j >> 1][2 * (j & 1)], x[j >> 1][2 * (j & 1) + 1], part);
+#pragma unroll
+                            for (int z = 0; z < QT; ++z) w[z][j] = part[z];
+                        }
+                    } else {
+                        const u32x4 v = load_as<u32x4>(reinterpret_cast<bytes_t>(global(static_cast<const uint16_t*>(A.q)) + at));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[0][j] = v[j];
+                    }
+                }
+#pragma unroll
+                for (int z = 0; z < QT; ++z) q[t][y][z] = __builtin_bit_cast(bf16x8, u32x4{w[z][0], w[z][1], w[z][2], w[z][3]});
+            }
+        }
+    }
+
+    // Keys of the step that the call leaves out for all rows get a V scale of 1 (0 * NaN would count); `sees` gets a bit for each
+    // of the lane's eight keys that its row sees.
+    __device__ __forceinline__ void mask(const Walk& w, int step, const Kept& kp, uint32_t (&vs)[2], uint32_t (&sees)[NT]) {
+        const Pages pg = pages_at(w, step);
+        const bool ok[2] = {there(w, step, pg, 0), there(w, step, pg, 1)};
+        bool nan = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sees[t] = 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int t = step * 32 + 16 * u + 4 * lb;
+            const uint32_t w0 = kp.w[u][0], w1 = kp.w[u][1], w2 = kp.w[u][2], w3 = kp.w[u][3];
+            const uint32_t even = lb & 2 ? w2 : w0, odd = lb & 2 ? w3 : w1, kept = lb & 1 ? odd : even;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const bool on = ok[u] && t + x < w.end && ((kept >> (8 * x)) & 0xFF) != 0;
+#pragma unroll
+                for (int z = 0; z < NT; ++z)
+                    if (on && t + x < limit[z]) sees[z] |= 1u << (4 * u + x);
+                const uint32_t code = (vs[u] >> (8 * x)) & 0xFF;
+                nan |= on && code == 255;
+                if (!on || code == 255) vs[u] = (vs[u] & ~(0xFFu << (8 * x))) | (127u << (8 * x));
+            }
+        }
+        // A NaN in V of a key that some rows see and others do not: the rows that see it get it in that group's channels here.
+        if (__any(nan)) {
+#pragma unroll
+            for (int z = 0; z < NT; ++z) {
+                float poison = 0.f;
+#pragma unroll 1
+                for (int x = 0; x < 32; ++x) {
+                    const int t = step * 32 + x, id = x < 16 ? pg.id[0] : pg.id[1];
+                    if (!(x < 16 ? ok[0] : ok[1]) || t >= w.end || (w.keep && ((w.keep[t >> 2] >> (8 * (t & 3))) & 0xFF) == 0)) continue;
+                    if (t < limit[z] && page_base(w, id)[c4_v_scales(w.page, t & (w.page - 1), lb * D / 128, D)] == 255) poison = __builtin_nanf("");
+                }
+#pragma unroll
+                for (int j = 0; j < J; ++j) o[z][j] += poison;
+            }
+        }
+    }
+
+    // Scores of keys that the lane's row does not see.
+    __device__ __forceinline__ static void hide(f32x4 (&st)[NT][2], uint32_t (&sees)[NT]) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            asm volatile("" : "+v"(sees[t]));        // (its bits are looked at here, and not in the steps that need no mask)
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+                if (!((sees[t] >> x) & 1)) st[t][x >> 2][x & 3] = -INFINITY;
+        }
+    }
+
+    // Probabilities of tile t's scores, in PT parts; the running maximum follows where the scores have outgrown it.
+    __device__ __forceinline__ void softmax(int t, const f32x4 (&st)[2], float c, bf16x8 (&p)[PT]) {
+        float most = st[0][0];
+#pragma unroll
+        for (int x = 1; x < 8; ++x) most = fmaxf(most, st[x >> 2][x & 3]);
+        most *= c;
+        if (__any(most > m[t] + kLag)) {
+            const float m2 = fmaxf(m[t], max_over_groups(most)), a = fast_exp2(m[t] - m2);
+            m[t] = m2;
+            l[t] *= a;
+#pragma unroll
+            for (int j = 0; j < J; ++j) o[t][j] *= a;
+        }
+        uint32_t w[PT][4];
 #pragma unroll
         for (int x = 0; x < 8; x += 2) {
-            const float p0 = fast_exp2(x8[x] - m), p1 = fast_exp2(x8[x + 1] - m);
-            l += p0 + p1;
-            uint32_t a0[PT], a1[PT];
-            split_bf16<PT>(p0, a0);
-            split_bf16<PT>(p1, a1);
+            const float p0 = fast_exp2(fmaf(st[x >> 2][x & 3], c, -m[t])), p1 = fast_exp2(fmaf(st[x >> 2][(x & 3) + 1], c, -m[t]));
+            l[t] += p0 + p1;
+            uint32_t part[PT];
+            split_pair<PT>(p0, p1, part);
 #pragma unroll
-            for (int t = 0; t < PT; ++t) pw[t][x / 2] = a0[t] | (a1[t] << 16);
+            for (int z = 0; z < PT; ++z) w[z][x / 2] = part[z];
         }
-        bf16x8 pf[PT];
 #pragma unroll
-        for (int t = 0; t < PT; ++t) pf[t] = __builtin_bit_cast(bf16x8, u32x4{pw[t][0], pw[t][1], pw[t][2], pw[t][3]});
+        for (int z = 0; z < PT; ++z) p[z] = __builtin_bit_cast(bf16x8, u32x4{w[z][0], w[z][1], w[z][2], w[z][3]});
+    }
+};
+
+// A wave that brings its own keys: steps of 32, straight from the pages.
+template <int D, bool F32, int NT, bool STREAM, int PT>
+struct Sweep : Rows<D, F32, NT, PT> {
+    typedef Rows<D, F32, NT, PT> R;
+    using R::KS; using R::J; using R::QT; using R::n; using R::lb; using R::q; using R::o;
+    static constexpr int RING = kRing;               // steps on their way
+    static constexpr int LOADS = D == 128 ? 5 : 3;   // load instructions of a step
+    static constexpr int CODES = 32 * D, SLOT = CODES + 256;     // bytes of a step's codes; of its place in LDS
+    static constexpr int KB = D / 8;                 // bytes of codes that a lane works on of a token's K, and of four tokens' V
+
+    struct Keys { uint32_t k[2][KB / 4], v[2][KB / 4], ks[2], vs[2]; };      // of one step
+
+    uint32_t at_k, at_v, at_s;                       // the byte offsets that the lane loads from, from its tile's place in a page on
+    bool second;                                     // the lane loads scales of the second tile
+
+    __device__ __forceinline__ void begin(const AttendArgs& A, const Sample& s, int h, int r0) {
+        R::begin(A, s, h, r0);
+        const int lane = lane_id(), half = D == 128 ? lane : lane & 31;
+        at_k = D == 128 ? c4_k_codes(n, D) + lb * KB : half * 16;
+        at_v = D == 128 ? c4_v_codes(A.p.page, 4 * lb, n, D) : c4_v_codes(A.p.page, 0, 0, D) + half * 16;
+        constexpr int W = D / 8;                     // words of a tile's scales of K; as many of V (d = 64: lanes from 32 on repeat)
+        const int word = lane & (4 * W - 1);
+        second = (word / W) & 1;
+        at_s = (word < 2 * W ? c4_k_scales(A.p.page, 0, D) : c4_v_scales(A.p.page, 0, 0, D)) + (word % W) * 4;
+    }
+
+    // Asks for a step's keys: loads that write LDS directly, SLOT bytes at `slot` (the wave's own).  They are a queue and nothing else: what
+    // a lane works with lies where the loads put it, and a wave has RING steps on their way without a register for them.
+    //   d = 128: a lane's 16 bytes of K and of V, tile by tile;  d = 64: the tiles' 512 bytes of K as they are, and of V
+    //   then the scales: 16 keys' bytes of K of the first and the second tile, then V's
+    __device__ __forceinline__ void ask(const Walk& w, int step, const Pages& pg, char* slot) const {
+        const int at = (step * 32) & (w.page - 1);
+        bytes_t base[2];
+        int place[2] = {at, at + 16};
+        base[0] = base[1] = page_base(w, pg.id[0]);
+        if (w.page_shift == 4) {                     // (other pages hold both tiles)
+            place[1] = 0;
+            base[1] = page_base(w, pg.id[1]);
+        }
+        if (D == 128) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                to_lds<16>(base[u] + place[u] * (D / 2) + at_k, slot + u * 1024);
+                to_lds<16>(base[u] + place[u] * (D / 2) + at_v, slot + 2048 + u * 1024);
+            }
+        } else {
+            const bytes_t codes = lane_id() < 32 ? base[0] + place[0] * (D / 2) : base[1] + place[1] * (D / 2);
+            to_lds<16>(codes + at_k, slot);
+            to_lds<16>(codes + at_v, slot + 1024);
+        }
+        to_lds<4>((second ? base[1] + place[1] * (D / 32) : base[0] + place[0] * (D / 32)) + at_s, slot + CODES);
+    }
+    template <int BYTES>
+    __device__ static __forceinline__ void to_lds(bytes_t from, char* to) {
+        const global_ptr_t g = reinterpret_cast<global_ptr_t>(from);
+        if constexpr (BYTES == 16) __builtin_amdgcn_global_load_lds(g, (lds_ptr_t)to, 16, 0, STREAM ? 2 : 0);
+        else __builtin_amdgcn_global_load_lds(g, (lds_ptr_t)to, 4, 0, STREAM ? 2 : 0);
+    }
+    // The keys of a step out of its slot: returns once they are in registers, and the slot is free.
+    __device__ __forceinline__ Keys take(const char* slot) const {
+        Keys r;
+        const uint32_t at = (uint32_t)(uintptr_t)(lds_ptr_t)const_cast<char*>(slot);
+        if constexpr (D == 128) {
+            u32x4 k0, k1, v0, v1;
+            asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:1024\n\tds_read_b128 %2, %8 offset:2048\n\tds_read_b128 %3, %8 offset:3072\n\t"
+                         "ds_read_u8 %4, %9 offset:4096\n\tds_read_u8 %5, %9 offset:4160\n\tds_read_b32 %6, %10 offset:4224\n\tds_read_b32 %7, %10 offset:4288\n\t"
+                         "s_waitcnt lgkmcnt(0)"
+                         : "=&v"(k0), "=&v"(k1), "=&v"(v0), "=&v"(v1), "=&v"(r.ks[0]), "=&v"(r.ks[1]), "=&v"(r.vs[0]), "=&v"(r.vs[1])
+                         : "v"(at + lane_id() * 16), "v"(at + n * 4 + lb), "v"(at + (lb * 4 + (n >> 2)) * 4) : "memory");
+#pragma unroll
+            for (int x = 0; x < 4; ++x) { r.k[0][x] = k0[x]; r.k[1][x] = k1[x]; r.v[0][x] = v0[x]; r.v[1][x] = v1[x]; }
+        } else {
+            u32x2 k0, k1, v0, v1;
+            asm volatile("ds_read_b64 %0, %8\n\tds_read_b64 %1, %8 offset:512\n\tds_read_b64 %2, %9\n\tds_read_b64 %3, %9 offset:512\n\t"
+                         "ds_read_u8 %4, %10 offset:2048\n\tds_read_u8 %5, %10 offset:2080\n\tds_read_b32 %6, %11 offset:2112\n\tds_read_b32 %7, %11 offset:2144\n\t"
+                         "s_waitcnt lgkmcnt(0)"
+                         : "=&v"(k0), "=&v"(k1), "=&v"(v0), "=&v"(v1), "=&v"(r.ks[0]), "=&v"(r.ks[1]), "=&v"(r.vs[0]), "=&v"(r.vs[1])
+                         : "v"(at + n * 32 + lb * 8), "v"(at + 1024 + lane_id() * 8), "v"(at + n * 2 + (lb >> 1)), "v"(at + (lb * 2 + (n >> 3)) * 4)
+                         : "memory");
+#pragma unroll
+            for (int x = 0; x < 2; ++x) { r.k[0][x] = k0[x]; r.k[1][x] = k1[x]; r.v[0][x] = v0[x]; r.v[1][x] = v1[x]; }
+        }
+        return r;
+    }
+
+    __device__ __forceinline__ void step(const Walk& w, const Keys& K, bool masked, uint32_t (&sees)[NT]) {
+        f32x4 st[NT][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const float ks = scale_of(K.ks[u]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) st[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int y = 0; y < KS; ++y) {
+                const bf16x8 a = __builtin_bit_cast(bf16x8, u32x4{fp4_pair(K.k[u][y], ks, 0), fp4_pair(K.k[u][y], ks, 1),
+                                                                  fp4_pair(K.k[u][y], ks, 2), fp4_pair(K.k[u][y], ks, 3)});
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int z = QT - 1; z >= 0; --z) st[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[t][y][z], st[t][u], 0, 0, 0);
+            }
+        }
+        if (masked) R::hide(st, sees);
+        bf16x8 p[NT][PT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) R::softmax(t, st[t], w.c, p[t]);
         // V^T P^T: byte y of a token's share is channels 2 y and 2 y + 1 of this lane
 #pragma unroll
         for (int y = 0; y < J / 2; ++y) {
             uint32_t lo[4], hi[4];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                uint32_t w[4];
+                uint32_t f[4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int at = t * (D / 32) + y;  // byte of the lane's load
-                    const float s = scale_of((vsc[u] >> (8 * t)) & 0xFF);
-                    const uint32_t src = vw[u][at / 4] >> (8 * (at % 4));
-                    w[t] = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(src, s, 0));
+                for (int x = 0; x < 4; ++x) {
+                    const int at = x * (D / 32) + y; // byte of the lane's load
+                    f[x] = fp4_pair(K.v[u][at / 4], scale_of((K.vs[u] >> (8 * x)) & 0xFF), at % 4);
                 }
-                lo[2 * u] = __builtin_amdgcn_perm(w[1], w[0], 0x05040100u);
-                lo[2 * u + 1] = __builtin_amdgcn_perm(w[3], w[2], 0x05040100u);
-                hi[2 * u] = __builtin_amdgcn_perm(w[1], w[0], 0x07060302u);
-                hi[2 * u + 1] = __builtin_amdgcn_perm(w[3], w[2], 0x07060302u);
+                lo[2 * u] = __builtin_amdgcn_perm(f[1], f[0], 0x05040100u);
+                lo[2 * u + 1] = __builtin_amdgcn_perm(f[3], f[2], 0x05040100u);
+                hi[2 * u] = __builtin_amdgcn_perm(f[1], f[0], 0x07060302u);
+                hi[2 * u + 1] = __builtin_amdgcn_perm(f[3], f[2], 0x07060302u);
             }
             const bf16x8 vl = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], lo[2], lo[3]});
             const bf16x8 vh = __builtin_bit_cast(bf16x8, u32x4{hi[0], hi[1], hi[2], hi[3]});
 #pragma unroll
-            for (int t = PT - 1; t >= 0; --t) {
-                o[2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vl, pf[t], o[2 * y], 0, 0, 0);
-                o[2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vh, pf[t], o[2 * y + 1], 0, 0, 0);
-            }
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int z = PT - 1; z >= 0; --z) {
+                    o[t][2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vl, p[t][z], o[t][2 * y], 0, 0, 0);
+                    o[t][2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vh, p[t][z], o[t][2 * y + 1], 0, 0, 0);
+                }
         }
     }
 
-    // the waves' sums: rows of 16 queries, channel d/4 * b + d/16 * (register) + tile
-    l += __shfl_xor(l, 16, kWave);
-    l += __shfl_xor(l, 32, kWave);
-    if (lb == 0) { s_m[wv][n] = m; s_l[wv][n] = l; }
+    // Steps first, first + stride, .. below `stop` (of 32 keys).  `ring`: the wave's RING slots.
+    __device__ __forceinline__ void run(const Walk& w, int first, int stop, int stride, char* ring) {
+        stop = min(stop, (w.end + 31) >> 5);
+        if (first >= stop) return;
+        uint32_t holes = 0;                                      // bit x: a page of the step in slot x is not there
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
+        for (int x = 0; x < RING; ++x)
+            if (first + x * stride < stop) {
+                const Pages pg = pages_at(w, first + x * stride);
+                if (hole(w, first + x * stride, pg)) holes |= 1u << x;
+                ask(w, first + x * stride, pg, ring + x * SLOT);
+            }
+        // The queries are there from here on: a wait for them within the loop would be one for the keys on their way too, step by step.
 #pragma unroll
-        for (int j = 0; j < J; ++j) s_o[wv][n][lb * (D / 4) + x * J + j] = o[j][x];
-    __syncthreads();
-    const int rr = threadIdx.x >> 4, part = threadIdx.x & 15, r2 = r0 + rr;
-    if (r2 >= live) return;
-    float top = kNoKey, sum = 0.f, acc[J] = {};
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, s_m[w][rr]);
+            for (int y = 0; y < KS; ++y)
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const float a = fast_exp2(s_m[w][rr] - top);
-        sum = fmaf(s_l[w][rr], a, sum);
-#pragma unroll
-        for (int j = 0; j < J; ++j) acc[j] = fmaf(s_o[w][rr][part * J + j], a, acc[j]);
+                for (int z = 0; z < QT; ++z) asm volatile("" : "+v"(q[t][y][z]));
+        int x = 0;
+        Pages next = pages_at(w, first + RING * stride);         // (asked for a step before they are needed)
+        Kept later = kept_at(w, first);
+        for (int i = first; i < stop; i += stride) {
+            const int ahead = i + RING * stride;
+            const Pages pg = next;
+            const Kept kp = later;
+            if (ahead - stride < stop) { MD_VM_WAIT((RING - 1) * LOADS); } else { MD_VM_WAIT(0); }
+            Keys k = take(ring + x * SLOT);
+            __builtin_amdgcn_sched_barrier(0);                   // (what is asked for before the wait for LDS is waited for with it)
+            next = pages_at(w, ahead + stride);
+            later = kept_at(w, i + stride);
+            const bool masked = ((holes >> x) & 1) != 0 || i * 32 + 32 > w.clear;
+            holes &= ~(1u << x);
+            if (ahead < stop) {
+                if (hole(w, ahead, pg)) holes |= 1u << x;
+                ask(w, ahead, pg, ring + x * SLOT);
+            }
+            x = x + 1 == RING ? 0 : x + 1;
+            uint32_t sees[NT];
+            if (masked) R::mask(w, i, kp, k.vs, sees);
+            step(w, k, masked, sees);
+        }
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;  // a row that sees no key: zeros
-    const int i2 = r2 / dim.G, h2 = h * dim.G + (r2 - i2 * dim.G);
-    const long to = (long)b * o_lay.batch + (long)i2 * o_lay.token + (long)h2 * o_lay.head + part * J;
+};
+
+// Writes one lane's share of a finished row: d/16 channels from `part` on.
+template <int D, bool F32>
+__device__ __forceinline__ void store_out(const AttendArgs& A, int b, int h, int r, int part, const float (&x)[D / 16], float m, float l) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;      // a row that sees no key: zeros
+    const int G = A.dim.G, i = r / G, hq = h * G + (r - i * G);
+    const long to = (long)b * A.ol.batch + (long)i * A.ol.token + (long)hq * A.ol.head + part * (D / 16);
     if (F32) {
+        auto p = reinterpret_cast<__attribute__((address_space(1))) f32x4*>(global(static_cast<float*>(A.out)) + to);
 #pragma unroll
-        for (int j = 0; j < J; ++j) static_cast<float*>(out)[to + j] = acc[j] * inv;
+        for (int j = 0; j < D / 64; ++j) p[j] = f32x4{x[4 * j] * inv, x[4 * j + 1] * inv, x[4 * j + 2] * inv, x[4 * j + 3] * inv};
     } else {
+        auto p = reinterpret_cast<__attribute__((address_space(1))) uint32_t*>(global(static_cast<uint16_t*>(A.out)) + to);
 #pragma unroll
-        for (int j = 0; j < J; j += 2)
-            *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(out) + to + j) = f32_to_bf16(acc[j] * inv) | (f32_to_bf16(acc[j + 1] * inv) << 16);
+        for (int j = 0; j < D / 32; ++j) p[j] = as_u32(__builtin_convertvector(f32x2{x[2 * j] * inv, x[2 * j + 1] * inv}, bf16x2));
     }
-    if (lse && part == 0)
-        lse[((long)b * p.H * dim.G + h2) * dim.N + i2] = sum == 0.f ? -INFINITY : (top + fast_log2(sum)) * kLn2C;
+    if (A.lse && part == 0) global(A.lse)[((long)b * A.p.H * G + hq) * A.dim.N + i] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2C;
+}
+template <int D>
+__device__ __forceinline__ void store_part(const Parts& parts, int place, int tile_rows, int row, int part, const float (&x)[D / 16], float m, float l) {
+    auto p = reinterpret_cast<__attribute__((address_space(1))) f32x4*>(global(parts.o) + ((long)place * tile_rows + row) * D + part * (D / 16));
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) p[j] = f32x4{x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
+    if (part == 0) *reinterpret_cast<__attribute__((address_space(1))) f32x2*>(global(parts.ml) + (long)place * tile_rows + row) = f32x2{m, l};
+}
+
+// A block's waves join their sums of 16 rows at a time through LDS: [waves][rows][D + 4] and the (m, l) pairs behind.  Then
+// thread (row, part) calls done(row, part, x, m, l).
+template <int D, int NT, class S, class Done>
+__device__ __forceinline__ void join_waves(S& w, int rows, float* lds, Done done) {
+    const int wv = wave_id(), nw = blockDim.x >> 6, tid = threadIdx.x, few = min(rows, 16);
+    float* so = lds;
+    float* sm = lds + nw * few * (D + 4);
+    float* sl = sm + nw * 16;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        if (16 * t >= rows) return;
+        if (t) __syncthreads();
+        const float l = sum_over_groups(w.l[t]);
+        if (w.n < few) {
+            if (w.lb == 0) { sm[wv * 16 + w.n] = w.m[t]; sl[wv * 16 + w.n] = l; }
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int j = 0; j < D / 16; j += 4)
+                    *reinterpret_cast<f32x4*>(so + (wv * few + w.n) * (D + 4) + w.lb * (D / 4) + x * (D / 16) + j) =
+                        f32x4{w.o[t][j][x], w.o[t][j + 1][x], w.o[t][j + 2][x], w.o[t][j + 3][x]};
+        }
+        __syncthreads();
+        const int row = tid >> 4, part = tid & 15;
+        if (row >= few || 16 * t + row >= rows) continue;
+        float top = kNoKey, sum = 0.f, acc[D / 16] = {};
+        for (int x = 0; x < nw; ++x) top = fmaxf(top, sm[x * 16 + row]);
+        for (int x = 0; x < nw; ++x) {
+            const float a = fast_exp2(sm[x * 16 + row] - top);
+            sum = fmaf(sl[x * 16 + row], a, sum);
+            const f32x4* from = reinterpret_cast<const f32x4*>(so + (x * few + row) * (D + 4) + part * (D / 16));
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) {
+                const f32x4 v = from[j];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) acc[4 * j + y] = fmaf(v[y], a, acc[4 * j + y]);
+            }
+        }
+        done(16 * t + row, part, acc, top, sum);
+    }
+}
+
+// A block per tile of query rows of a (sample, K/V head); its waves take the steps in turn.
+template <int D, bool F32, int NT, bool STREAM, int PT>
+__global__ __launch_bounds__(NT == 2 || (F32 && D == 128) ? 256 : 512, NT == 2 || (F32 && D == 128) ? 3 : 4) void cache4_attend_kernel(AttendArgs A0)
+{
+    extern __shared__ f32x4 s_lds[];
+    constexpr int ROWS = 16 * NT;
+    Sweep<D, F32, NT, STREAM, PT> sw;
+    Walk w;
+    {
+        const AttendArgs A = argument<AttendArgs>(0);
+        const int tile = blockIdx.x % A.dim.tiles, bh = blockIdx.x / A.dim.tiles, h = bh % A.p.H, b = bh / A.p.H, r0 = tile * ROWS;
+        const Sample s = sample_of(A, b);
+        if (r0 >= s.nq * A.dim.G) return;
+        sw.begin(A, s, h, r0);
+        w = walk_of(A, s, h, r0, min(r0 + ROWS, s.nq * A.dim.G) - 1);
+    }
+    char* lds = reinterpret_cast<char*>(s_lds);
+    sw.run(w, wave_id(), 0x7FFFFFFF, blockDim.x >> 6, lds + wave_id() * (sw.RING * sw.SLOT));
+    __syncthreads();
+    const AttendArgs A = argument<AttendArgs>(0);
+    const int tile = blockIdx.x % A.dim.tiles, bh = blockIdx.x / A.dim.tiles, h = bh % A.p.H, b = bh / A.p.H, r0 = tile * ROWS;
+    const Sample s = sample_of(A, b);
+    join_waves<D, NT>(sw, min(ROWS, s.nq * A.dim.G - r0), reinterpret_cast<float*>(s_lds), [&](int row, int part, const float (&x)[D / 16], float m, float l) {
+        store_out<D, F32>(A, b, h, r0 + row, part, x, m, l);
+    });
+}
+
+// All samples' work, added up by a wave: the total, and where sample `b` begins or which sample holds the first step of a run.
+struct Place { int total, b, begin; };
+__device__ __forceinline__ Place find_place(const AttendArgs& A, int tile_rows, int b, bool by_run, int run, int blocks, int least) {
+    const int cap = A.p.max_pages << A.p.page_shift, lane = lane_id();
+    auto work_of = [&](int x) {
+        if (x >= A.dim.B) return 0;
+        const C4Work w = c4_work(c4_clamp(global(A.len)[x], 0, cap), (A.q_len ? c4_clamp(global(A.q_len)[x], 0, A.dim.N) : A.dim.N) * A.dim.G, tile_rows);
+        return A.p.H * w.tiles * w.steps;
+    };
+    Place r{0, 0, 0};
+    const int mine = work_of(lane), incl = wave_incl_scan_i(mine);       // of the first 64 samples, which are often all
+    r.total = __builtin_amdgcn_readlane(incl, kWave - 1);
+    for (int x = kWave; x < A.dim.B; x += kWave) r.total += wave_sum_i(work_of(x + lane));
+    int at = 0;
+    if (by_run) {
+        const int runs = c4_runs(r.total, blocks, least);
+        if (run >= runs || r.total == 0) { r.b = -1; return r; }
+        at = c4_run_begin(run, r.total, runs);
+    }
+    int base = 0;
+    for (int x = 0; x < A.dim.B; x += kWave) {
+        const int w = x ? work_of(x + lane) : mine, in = x ? wave_incl_scan_i(w) : incl, sum = __builtin_amdgcn_readlane(in, kWave - 1);
+        if (by_run ? at < base + sum : b < x + kWave) {
+            const int l = by_run ? (int)__builtin_ctzll(__ballot(base + in > at)) : b - x;
+            r.b = x + l;
+            r.begin = base + __builtin_amdgcn_readlane(in, l) - __builtin_amdgcn_readlane(w, l);
+            return r;
+        }
+        base += sum;
+    }
+    r.b = -1;
+    return r;
+}
+
+// A block's run of steps, unit by unit: each(sample, K/V head, first row, first and last step, place of the part or -1).
+template <class Each>
+__device__ __forceinline__ void each_unit(int tile_rows, int run, Each each) {
+    int at, stop, b, begin, total, runs;
+    {
+        const AttendArgs A = argument<AttendArgs>(0);
+        const Parts parts = argument<Parts>(kPartsAt);
+        const Place place = find_place(A, tile_rows, 0, true, run, parts.blocks, parts.least);
+        if (place.b < 0) return;
+        total = place.total;
+        runs = c4_runs(total, parts.blocks, parts.least);
+        at = c4_run_begin(run, total, runs);
+        stop = c4_run_begin(run + 1, total, runs);
+        b = place.b;
+        begin = place.begin;
+    }
+    while (at < stop) {
+        const AttendArgs A = argument<AttendArgs>(0);
+        const Sample s = sample_of(A, b);
+        const C4Work w = c4_work(s.length, s.nq * A.dim.G, tile_rows);
+        const int whole = A.p.H * w.tiles * w.steps;
+        if (at - begin >= whole) { begin += whole; ++b; continue; }
+        const int unit = (at - begin) / w.steps, first = at - begin - unit * w.steps, last = min(w.steps, first + stop - at);
+        const int h = unit / w.tiles, r0 = (unit - h * w.tiles) * tile_rows;
+        each(A, s, h, r0, first, last, first == 0 && last == w.steps ? -1 : c4_part_place(run, begin + unit * w.steps, total, runs));
+        at += last - first;
+    }
+}
+
+// Few units, or units of unequal length: every block takes a run of as many steps, over the borders of units and samples.  A unit that
+// lies within a run is finished there, the parts of the others are joined by the next kernel.
+template <int D, bool F32, int NT, bool STREAM, int PT>
+__global__ __launch_bounds__(256, NT == 2 || (F32 && D == 128) ? 3 : 4) void cache4_attend_runs_kernel(AttendArgs A0, Parts parts0)
+{
+    extern __shared__ f32x4 s_lds[];
+    constexpr int ROWS = 16 * NT;
+    char* lds = reinterpret_cast<char*>(s_lds);
+    each_unit(ROWS, blockIdx.x, [&](const AttendArgs& A, const Sample& s, int h, int r0, int first, int last, int place) {
+        Sweep<D, F32, NT, STREAM, PT> sw;
+        sw.begin(A, s, h, r0);
+        const int rows = min(ROWS, s.nq * A.dim.G - r0), b = s.b;
+        const Walk w = walk_of(A, s, h, r0, r0 + rows - 1);
+        sw.run(w, first + wave_id(), last, 4, lds + wave_id() * (sw.RING * sw.SLOT));
+        __syncthreads();
+        const AttendArgs again = argument<AttendArgs>(0);
+        const Parts parts = argument<Parts>(kPartsAt);
+        join_waves<D, NT>(sw, rows, reinterpret_cast<float*>(s_lds), [&](int row, int part, const float (&x)[D / 16], float m, float l) {
+            if (place < 0) store_out<D, F32>(again, b, h, r0 + row, part, x, m, l);
+            else store_part<D>(parts, place, ROWS, row, part, x, m, l);
+        });
+        __syncthreads();
+    });
+}
+
+// The parts of a unit that its runs left, and the runs that left them.
+struct Cut { int begin, p0, p1, total, runs; };
+__device__ __forceinline__ Cut cut_of(const AttendArgs& A, const Parts& parts, const Sample& s, int h, int tile, int tile_rows) {
+    const Place place = find_place(A, tile_rows, s.b, false, 0, 0, 1);
+    const C4Work w = c4_work(s.length, s.nq * A.dim.G, tile_rows);
+    Cut c;
+    c.total = place.total;
+    c.runs = c4_runs(place.total, parts.blocks, parts.least);
+    c.begin = place.begin + (h * w.tiles + tile) * w.steps;
+    c.p0 = c4_run_of(c.begin, c.total, c.runs);
+    c.p1 = c4_run_of(c.begin + w.steps - 1, c.total, c.runs);
+    return c;
+}
+// One wave adds up parts x0, x0 + stride, .. of a row, 64 of them at a time: their weights side by side, their rows one after the other.
+// A lane gets d/64 channels.
+template <int D>
+__device__ __forceinline__ void add_parts(const Parts& parts, const Cut& c, int x0, int stride, int row, int tile_rows, float& m, float& l, float (&acc)[D / 64]) {
+    constexpr int C = D / 64;
+    const int lane = lane_id();
+    m = kNoKey;
+    l = 0.f;
+#pragma unroll
+    for (int j = 0; j < C; ++j) acc[j] = 0.f;
+    for (; x0 <= c.p1; x0 += stride * kWave) {
+        const int p = x0 + lane * stride;
+        const bool on = p <= c.p1;
+        const float2 ml = on ? parts.ml[(long)c4_part_place(p, c.begin, c.total, c.runs) * tile_rows + row] : float2{kNoKey, 0.f};
+        const float top = fmaxf(m, wave_max(ml.x)), a = fast_exp2(m - top), e = on ? fast_exp2(ml.x - top) : 0.f;
+        l = l * a + wave_sum(ml.y * e);
+        m = top;
+#pragma unroll
+        for (int j = 0; j < C; ++j) acc[j] *= a;
+        const int n = min(kWave, (c.p1 - x0) / stride + 1);
+        for (int y0 = 0; y0 < n; y0 += 8) {
+            float v[8][C];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+                const int q = x0 + min(y0 + y, n - 1) * stride;
+                const float* from = parts.o + ((long)c4_part_place(q, c.begin, c.total, c.runs) * tile_rows + row) * D + lane * C;
+#pragma unroll
+                for (int j = 0; j < C; ++j) v[y][j] = from[j];
+            }
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+                const float f = y0 + y < n ? lane_bcast_f(e, y0 + y) : 0.f;
+                if (y0 + y < n)
+#pragma unroll
+                    for (int j = 0; j < C; ++j) acc[j] = fmaf(v[y][j], f, acc[j]);
+            }
+        }
+    }
+}
+
+// Few rows: a block per query row, its waves share the parts.
+template <int D, bool F32>
+__global__ __launch_bounds__(1024) void cache4_join_kernel(AttendArgs A, Parts parts, int tile_rows)
+{
+    __shared__ float s_o[16][D];
+    __shared__ float s_m[16], s_l[16];
+    const int rows = A.dim.N * A.dim.G, r = blockIdx.x % rows, bh = blockIdx.x / rows, h = bh % A.p.H, b = bh / A.p.H;
+    const Sample s = sample_of(A, b);
+    if (r >= s.nq * A.dim.G) return;
+    const Cut c = cut_of(A, parts, s, h, r / tile_rows, tile_rows);
+    if (c.p0 == c.p1) return;                        // finished in its run
+    const int lane = lane_id(), wv = wave_id(), nw = blockDim.x >> 6;
+    constexpr int C = D / 64;
+    float m, l, acc[C];
+    add_parts<D>(parts, c, c.p0 + wv, nw, r % tile_rows, tile_rows, m, l, acc);
+#pragma unroll
+    for (int j = 0; j < C; ++j) s_o[wv][lane * C + j] = acc[j];
+    if (lane == 0) { s_m[wv] = m; s_l[wv] = l; }
+    __syncthreads();
+    if (threadIdx.x >= 16) return;
+    const int part = threadIdx.x;
+    float top = kNoKey, sum = 0.f, x[D / 16] = {};
+    for (int y = 0; y < nw; ++y) top = fmaxf(top, s_m[y]);
+    for (int y = 0; y < nw; ++y) {
+        const float a = fast_exp2(s_m[y] - top);
+        sum = fmaf(s_l[y], a, sum);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) x[j] = fmaf(s_o[y][part * (D / 16) + j], a, x[j]);
+    }
+    store_out<D, F32>(A, b, h, r, part, x, top, sum);
+}
+
+// Many rows, and then few parts of each: a block per sixteen rows of a unit, sixteen lanes per row.
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void cache4_join_tiles_kernel(AttendArgs A, Parts parts, int tile_rows)
+{
+    const int groups = tile_rows / 16, group = blockIdx.x % groups, unit = blockIdx.x / groups;
+    const int tile = unit % A.dim.tiles, bh = unit / A.dim.tiles, h = bh % A.p.H, b = bh / A.p.H;
+    const Sample s = sample_of(A, b);
+    const int row = group * 16 + (threadIdx.x >> 4), r = tile * tile_rows + row, part = threadIdx.x & 15, live = s.nq * A.dim.G;
+    if (tile * tile_rows + group * 16 >= live) return;
+    const Cut c = cut_of(A, parts, s, h, tile, tile_rows);
+    if (c.p0 == c.p1 || r >= live) return;
+    float m = kNoKey, l = 0.f, acc[D / 16] = {};
+    for (int p0 = c.p0; p0 <= c.p1; p0 += 4) {
+        float2 ml[4];
+        f32x4 v[4][D / 64];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const long at = (long)c4_part_place(min(p0 + y, c.p1), c.begin, c.total, c.runs) * tile_rows + row;
+            ml[y] = p0 + y <= c.p1 ? parts.ml[at] : float2{kNoKey, 0.f};
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) v[y][j] = reinterpret_cast<const f32x4*>(parts.o + at * D + part * (D / 16))[j];
+        }
+        const float top = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m), a = fast_exp2(m - top);
+        m = top;
+        l *= a;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) acc[j] *= a;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            if (p0 + y > c.p1) break;
+            const float e = fast_exp2(ml[y].x - top);
+            l = fmaf(ml[y].y, e, l);
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) acc[j] = fmaf(v[y][j >> 2][j & 3], e, acc[j]);
+        }
+    }
+    store_out<D, F32>(A, b, h, r, part, acc, m, l);
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -511,6 +1038,7 @@ int check_pool(const char* who, int H, int d, int n_pages, int page, int max_pag
     if ((long)n_pages * page > 0x7FFFFFFFl) return fail(MD_ESHAPE, "%s: a pool of %d pages of %d tokens has more slots than 31 bits name", who, n_pages, page);
     if ((long)max_pages * page > 0x7FFFFFFFl / 2) return fail(MD_ESHAPE, "%s: %d pages of %d tokens are too many for one request", who, max_pages, page);
     if (H > 65535) return fail(MD_ESHAPE, "%s: H=%d out of range", who, H);
+    if ((long)n_pages * H * c4_page_bytes(page, d) > (256l << 30)) return fail(MD_ESHAPE, "%s: a pool of more than 256 GiB", who);
     *p = Pool{n_pages, page, __builtin_ctz((unsigned)page), max_pages, H, (long)c4_page_bytes(page, d)};
     return MD_OK;
 }
@@ -621,10 +1149,33 @@ int read_impl(const void* cache, const int32_t* table, const int32_t* len, const
     return check_launch("cache4_read");
 }
 
+struct AttendPlan {
+    C4Attend cut;
+    Parts parts;
+    size_t lds, bytes;
+};
+AttendPlan attend_plan(void* workspace, bool f32, int B, int N, int Hq, int d, const Pool& p) {
+    AttendPlan a;
+    const int G = Hq / p.H, few = N * G < 16 ? N * G : 16;
+    a.cut = c4_attend(f32, B, N, G, p.H, d, (int64_t)p.max_pages * p.page);
+    const size_t join = sizeof(float) * ((size_t)a.cut.waves * few * (d + 4) + 2 * a.cut.waves * 16), ring = (size_t)a.cut.waves * kRing * (32 * d + 256);
+    a.lds = join > ring ? join : ring;
+    Carver c(workspace);
+    const size_t places = a.cut.runs ? (size_t)2 * kC4Blocks * a.cut.tile_rows : 0;
+    a.parts.o = c.take<float>(places * d);
+    a.parts.ml = c.take<float2>(places);
+    a.parts.blocks = kC4Blocks;
+    a.parts.least = kC4Least;
+    a.bytes = c.off > 256 ? c.off : 256;
+    return a;
+}
+
 size_t attend_bytes(int B, int N, int Hq, int H, int d, int max_pages, int page) {
     Pool p;
     if (B <= 0 || N <= 0 || Hq <= 0 || H <= 0 || Hq % H || check_pool("cache4_attend", H, d, 1, page, max_pages, &p) != MD_OK) return 0;
-    return 256;
+    if ((long)N * (Hq / H) > 0x7FFFFFFFl - 128) return 0;
+    const size_t x = attend_plan(nullptr, false, B, N, Hq, d, p).bytes, y = attend_plan(nullptr, true, B, N, Hq, d, p).bytes;
+    return x > y ? x : y;
 }
 
 int attend_impl(const void* q, int dtype, const void* cache, const int32_t* table, const int32_t* len, const int32_t* q_len, const uint8_t* keep,
@@ -648,10 +1199,10 @@ int attend_impl(const void* q, int dtype, const void* cache, const int32_t* tabl
     if (!aligned16(q) || !aligned16(out) || !aligned16(cache) || (reinterpret_cast<uintptr_t>(keep) & 3u))
         return fail(MD_EALIGN, "cache4_attend: tensors must be 16-byte aligned, keep 4-byte aligned");
     const int G = Hq / H;
-    if ((long)N * G > 0x7FFFFFFFl - 64) return fail(MD_ESHAPE, "cache4_attend: too many query rows");
-    const int tiles = (N * G + 15) / 16;
-    const long blocks = (long)B * H * tiles;
-    if (blocks > kMaxGrid) return fail(MD_ESHAPE, "cache4_attend: too many query rows");
+    if ((long)N * G > 0x7FFFFFFFl - 128) return fail(MD_ESHAPE, "cache4_attend: too many query rows");
+    const AttendPlan plan = attend_plan(workspace, dtype == MD_F32, B, N, Hq, d, p);
+    const long units = (long)B * H * plan.cut.tiles, rows = (long)B * Hq * N;
+    if (units > kMaxGrid / 2 || rows > kMaxGrid) return fail(MD_ESHAPE, "cache4_attend: too many query rows");
     const size_t need = attend_bytes(B, N, Hq, H, d, max_pages, page);
     const Range r[] = {{out, rows_bytes(ol, B, N, Hq, d, dtype)}, {lse, lse ? (size_t)B * Hq * N * 4 : 0}, {workspace, workspace ? need : 0},
                        {q, rows_bytes(ql, B, N, Hq, d, dtype)}, {cache, pool_bytes(p)}, {table, (size_t)B * max_pages * 4}, {len, (size_t)B * 4},
@@ -661,12 +1212,30 @@ int attend_impl(const void* q, int dtype, const void* cache, const int32_t* tabl
     if (!workspace || workspace_bytes < need)
         return fail(MD_EWORKSPACE, "cache4_attend: workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(MD_EALIGN, "cache4_attend: workspace must be 256-byte aligned");
-    const AttendDims dim{B, N, G, tiles};
+    const AttendArgs A{q, static_cast<const uint8_t*>(cache), table, len, q_len, keep, out, lse, p, AttendDims{B, N, G, plan.cut.tiles}, softmax_scale, ql, ol};
+    // a pool beyond half of the 256 MB Infinity Cache is streamed (64 x up to 4096 keys, 32 heads: 128 us, 141 with plain loads)
+    const bool stream_once = pool_bytes(p) > (size_t)128 << 20;
     hipStream_t st = static_cast<hipStream_t>(stream);
-#define MD_C4_ATTEND(D_, F_) MD_LAUNCH("cache4_attend", st, (cache4_attend_kernel<D_, F_>), (int)blocks, 256, 0, \
-        q, static_cast<const uint8_t*>(cache), table, len, q_len, keep, p, dim, softmax_scale, out, lse, ql, ol)
-    if (d == 128) { if (dtype == MD_F32) MD_C4_ATTEND(128, true); else MD_C4_ATTEND(128, false); }
-    else { if (dtype == MD_F32) MD_C4_ATTEND(64, true); else MD_C4_ATTEND(64, false); }
+#define MD_C4_ATTEND(D_, F_, NT_, S_, PT_)                                                                                                  \
+    do {                                                                                                                                  \
+        if (plan.cut.runs) {                                                                                                              \
+            MD_LAUNCH("cache4_attend_runs", st, (cache4_attend_runs_kernel<D_, F_, NT_, S_, PT_>), kC4Blocks, 256, plan.lds, A, plan.parts); \
+            if (rows <= 2048) MD_LAUNCH("cache4_join", st, (cache4_join_kernel<D_, F_>), (int)rows, rows <= 512 ? 1024 : 256, 0, A, plan.parts, 16 * NT_); \
+            else MD_LAUNCH("cache4_join", st, (cache4_join_tiles_kernel<D_, F_>), (int)(units * NT_), 256, 0, A, plan.parts, 16 * NT_);      \
+        } else {                                                                                                                          \
+            MD_LAUNCH("cache4_attend", st, (cache4_attend_kernel<D_, F_, NT_, S_, PT_>), (int)units, plan.cut.waves * 64, plan.lds, A);      \
+        }                                                                                                                                 \
+    } while (0)
+#define MD_C4_ATTEND_S(D_, F_, NT_, PT_) do { if (stream_once) MD_C4_ATTEND(D_, F_, NT_, true, PT_); else MD_C4_ATTEND(D_, F_, NT_, false, PT_); } while (0)
+#define MD_C4_ATTEND_D(D_)                                                                                                                  \
+    do {                                                                                                                                  \
+        if (dtype == MD_F32) MD_C4_ATTEND_S(D_, true, 1, 3);                                                                              \
+        else if (plan.cut.tile_rows == 16) MD_C4_ATTEND_S(D_, false, 1, 2);                                                               \
+        else MD_C4_ATTEND_S(D_, false, 2, 1);                                                                                             \
+    } while (0)
+    if (d == 128) MD_C4_ATTEND_D(128); else MD_C4_ATTEND_D(64);
+#undef MD_C4_ATTEND_D
+#undef MD_C4_ATTEND_S
 #undef MD_C4_ATTEND
     return check_launch("cache4_attend");
 }

@@ -61,5 +61,51 @@ MD_PLAN_FN int c4_scale_code(uint32_t most) {
     return c4_clamp((int)((most + 0x200000u) >> 23) - 2, 27, 252);
 }
 
+// How the attention is cut over blocks of equal work.  A sample's work is H * tiles units (a K/V head and a tile of query rows) of
+// `steps` 32-key steps each, in this order, one sample after the other; a block takes a run of consecutive steps.
+struct C4Work { int tiles, steps; };
+MD_PLAN_FN C4Work c4_work(int length, int rows, int tile_rows) {
+    C4Work w;
+    w.tiles = (rows + tile_rows - 1) / tile_rows;
+    w.steps = length > 0 ? (length + 31) >> 5 : 1;                // (rows that see no key are written by somebody too)
+    return w;
+}
+// Blocks that get a run: `least` steps each at least, where there are that many.
+MD_PLAN_FN int c4_runs(int total, int blocks, int least) { return c4_clamp(total / least, 1, blocks); }
+MD_PLAN_FN int c4_run_begin(int p, int total, int runs) { return (int)((int64_t)total * p / runs); }
+// The run that holds step `at`.
+MD_PLAN_FN int c4_run_of(int at, int total, int runs) { return (int)((((int64_t)at + 1) * runs - 1) / total); }
+// Where run p leaves the sums of a unit that it holds only a part of, of its two places: the second one for the unit that its run ends
+// in and begins with or before, the first one for the unit that began in an earlier run.
+MD_PLAN_FN int c4_part_place(int p, int unit_begin, int total, int runs) { return 2 * p + (c4_run_begin(p, total, runs) > unit_begin ? 0 : 1); }
+
+// How a call of the attention is cut up: by what the host knows, which is the tables' capacity and not the samples' lengths.
+//   tile_rows  query rows of a unit.  Of the G query heads of a K/V head and the N tokens, sixteen fill a matrix tile.  Two tiles to a
+//              unit convert each key once for 32 rows instead of 16, but leave half as many units and three blocks to a CU instead of four:
+//              they pay from about two units per CU on.  us with 16 / 32 rows: 4 x 512 tokens of 32 heads on 8, up to 5888 keys
+//              317 / 222, 16 x 128 of 32 heads, 704 keys 77 / 57, 1 x 512 of 32 heads on 8, 6000 keys 119 / 89; 1 x 128 of 32 heads on 8,
+//              1000 keys (256 units) 13.2 / 16.2, 1 x 64 of 32 heads, 4000 keys (128) 41 / 50, 16 x 5 of 32 heads on 8, 2000 keys 26 / 29
+//   runs       blocks of equal work, joined by a second kernel, instead of a block per unit.  Where there are few units, a block of
+//              eight waves takes 4.5 us + 0.165 us per 32 keys, the runs take 13 us and have all CUs; where sequences may be very
+//              long, one of them among short ones must not be left to one block.  us, a block per unit / runs: 8 units of 4000 keys 24 /
+//              16, of 16000 86 / 17, 32 units of 640 7.5 / 11, of 2000 16 / 16, of 4000 26 / 20, 128 of 4000 29 / 25, 256 of 2000 20 / 25, 512 of
+//              4000 55 / 64; 16 units of up to 100000 keys 473 / 46
+//   waves      of a block per unit: eight (four: 64 sequences of up to 4096 keys and 32 heads 124 us instead of 119, 32 units of 2000 keys
+//              22 instead of 16); four where a wave takes more registers, and where a unit has no more than eight steps
+struct C4Attend { int tile_rows, tiles, waves; bool runs; };
+constexpr int kC4Blocks = 1024;                      // of the runs: four to a CU
+constexpr int kC4Least = 4;                          // steps of a run, one per wave of its block
+inline C4Attend c4_attend(bool f32, int B, int N, int G, int H, int d, int64_t capacity) {
+    const int64_t rows = (int64_t)N * G, steps = (capacity + 31) / 32;
+    C4Attend a;
+    a.tile_rows = !f32 && rows > 16 && (int64_t)B * H * ((rows + 15) / 16) > 512 ? 32 : 16;
+    a.tiles = (int)((rows + a.tile_rows - 1) / a.tile_rows);
+    const int64_t units = (int64_t)B * H * a.tiles;
+    // (a run's steps are counted in 31 bits)
+    a.runs = (steps * (200 - units) > 16000 || steps > 512) && units < 0x7FFFFFFFl / steps;
+    a.waves = a.runs || a.tile_rows == 32 || (f32 && d == 128) || steps <= 8 ? 4 : 8;
+    return a;
+}
+
 }  // namespace
 }  // namespace md

@@ -34,7 +34,7 @@ static void regions() {
                     CHECK(k % width == 0 && v % width == 0 && s % 4 == 0, "d=%d page=%d lane %d", d, page, lane);
                     CHECK(k + width <= (int)used.size() && v + width <= (int)used.size() && s + 4 <= (int)used.size(), "lane %d", lane);
                 }
-            CHECK(c4_page_bytes(page, d) % 16 == 0, "d=%d page=%d", d, page);
+            CHECK(c4_page_bytes(page, d) % 64 == 0, "d=%d page=%d", d, page);
         }
 }
 
@@ -126,7 +126,83 @@ static void scales() {
     }
 }
 
+// The attention's cut: what the tests of the GPU rely on, and limits.
+static void forms() {
+    auto is = [](const C4Attend& a, int tile_rows, int waves, bool runs) { return a.tile_rows == tile_rows && a.waves == waves && a.runs == runs; };
+    CHECK(is(c4_attend(false, 3, 1, 1, 2, 128, 3040), 16, 4, true), "few units");
+    CHECK(is(c4_attend(false, 16, 1, 1, 2, 128, 112), 16, 4, false), "short");
+    CHECK(is(c4_attend(false, 16, 1, 1, 2, 128, 512), 16, 8, false), "eight waves");
+    CHECK(is(c4_attend(true, 16, 1, 1, 2, 128, 512), 16, 4, false) && is(c4_attend(true, 16, 1, 1, 2, 64, 512), 16, 8, false), "fp32");
+    CHECK(is(c4_attend(false, 22, 20, 1, 13, 64, 512), 32, 4, false), "two tiles");
+    CHECK(is(c4_attend(true, 22, 20, 1, 13, 64, 512), 16, 8, false), "two tiles, fp32");
+    CHECK(is(c4_attend(false, 22, 20, 1, 13, 128, 16640), 32, 4, true), "two tiles in runs");
+    CHECK(is(c4_attend(false, 16, 1, 1, 16, 64, 16640), 16, 4, true), "very long");
+    std::mt19937 rng(3);
+    for (int n = 0; n < 200000; ++n) {
+        const int B = 1 << (rng() % 16), N = 1 + rng() % (1 << (rng() % 12)), G = 1 + rng() % 16, H = 1 << (rng() % 7), d = rng() % 2 ? 64 : 128;
+        const int64_t cap = 16 + rng() % (1 << (4 + rng() % 26));
+        const C4Attend a = c4_attend(rng() % 4 == 0, B, N, G, H, d, cap);
+        const int64_t units = (int64_t)B * H * a.tiles, steps = (cap + 31) / 32;
+        CHECK((int64_t)a.tiles * a.tile_rows >= (int64_t)N * G && ((int64_t)a.tiles - 1) * a.tile_rows < (int64_t)N * G, "tiles");
+        CHECK(!a.runs || units * steps < 0x7FFFFFFFl, "%d %d: steps", B, N);
+        CHECK(a.waves == 4 || a.waves == 8, "waves");
+    }
+}
+
+// Runs over samples of any length: every step of every unit is in one run, what a run leaves of a unit lies where the join looks for it, and
+// nowhere else.
+static void runs() {
+    std::mt19937 rng(4);
+    for (int round = 0; round < 3000; ++round) {
+        const int B = 1 + rng() % 7, H = 1 + rng() % 4, rows_of = rng() % 3, blocks = 1 + rng() % 40, least = 1 + rng() % 5;
+        std::vector<C4Work> work;
+        std::vector<int> begin;
+        int total = 0;
+        for (int b = 0; b < B; ++b) {
+            const int length = rng() % 4 ? (int)(rng() % (1 << (rng() % 11))) : 0, rows = rows_of == 0 ? 1 : (int)(rng() % 70);
+            work.push_back(c4_work(length, rows, 16));
+            begin.push_back(total);
+            total += H * work[b].tiles * work[b].steps;
+        }
+        if (total == 0) continue;
+        const int n = c4_runs(total, blocks, least);
+        CHECK(n >= 1 && n <= blocks && (n == 1 || total / n >= least), "%d runs of %d", n, total);
+        CHECK(c4_run_begin(0, total, n) == 0 && c4_run_begin(n, total, n) == total, "ends");
+        std::vector<int> place(2 * blocks, -1);      // first step of the unit whose part lies there
+        std::vector<char> done(total, 0);
+        for (int p = 0; p < n; ++p) {
+            int at = c4_run_begin(p, total, n), b = 0;
+            const int stop = c4_run_begin(p + 1, total, n);
+            while (at < stop) {
+                while (at - begin[b] >= H * work[b].tiles * work[b].steps) ++b;
+                const int unit = (at - begin[b]) / work[b].steps, first = at - begin[b] - unit * work[b].steps;
+                const int last = first + stop - at < work[b].steps ? first + stop - at : work[b].steps, unit_begin = begin[b] + unit * work[b].steps;
+                for (int i = first; i < last; ++i) { CHECK(!done[unit_begin + i], "step twice"); done[unit_begin + i] = 1; CHECK(c4_run_of(unit_begin + i, total, n) == p, "run of a step"); }
+                if (first || last < work[b].steps) {
+                    const int to = c4_part_place(p, unit_begin, total, n);
+                    CHECK(to >= 0 && to < 2 * blocks && place[to] < 0, "place %d", to);
+                    place[to] = unit_begin;
+                }
+                at += last - first;
+            }
+        }
+        for (int i = 0; i < total; ++i) CHECK(done[i], "step %d of %d left out", i, total);
+        int parts = 0, found = 0;
+        for (int x : place) parts += x >= 0;
+        for (int b = 0; b < B; ++b)
+            for (int u = 0; u < H * work[b].tiles; ++u) {
+                const int first = begin[b] + u * work[b].steps;
+                const int p0 = c4_run_of(first, total, n), p1 = c4_run_of(first + work[b].steps - 1, total, n);
+                if (p0 == p1) continue;
+                for (int p = p0; p <= p1; ++p) { CHECK(place[c4_part_place(p, first, total, n)] == first, "part of run %d", p); ++found; }
+            }
+        CHECK(found == parts, "%d parts, %d looked for", parts, found);
+    }
+}
+
 int main() {
+    forms();
+    runs();
     regions();
     names();
     changes();

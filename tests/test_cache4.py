@@ -191,7 +191,7 @@ def test_attend_refusals(lib):
 def test_pool_bytes(lib):
     assert lib.mustdrop_cache4_bytes(10, 32, 4, 128) == 10 * 4 * 32 * 136 == 10 * 4 * ref.page_bytes(32, 128)
     assert lib.mustdrop_cache4_bytes(100000, 128, 64, 128) == 100000 * 64 * 128 * 136          # beyond 2^32
-    for bad in ((0, 32, 4, 128), (10, 20, 4, 128), (10, 32, 4, 80), (1 << 27, 16, 1, 64)):
+    for bad in ((0, 32, 4, 128), (10, 20, 4, 128), (10, 32, 4, 80), (1 << 27, 16, 1, 64), (1 << 24, 32, 8, 128)):
         assert lib.mustdrop_cache4_bytes(*bad) == 0
 
 

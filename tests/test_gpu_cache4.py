@@ -216,7 +216,8 @@ class Case:
         self.table, n_pages = scattered(rng, lengths, page, entries, fill=2 ** 31 - 1)
         # what nobody wrote reads as NaN
         self.pool = np.full((n_pages, H, ref.page_bytes(page, d)), 255, np.uint8)
-        self.K, self.V = np.zeros((B, entries * page, H, d)), np.zeros((B, entries * page, H, d))
+        reach = min(entries, -(-max(max(lengths), 1) // page)) * page
+        self.K, self.V = np.zeros((B, reach, H, d)), np.zeros((B, reach, H, d))
         for b, n in enumerate(lengths):
             k, v = rng.standard_normal((n, H, d)) * size, rng.standard_normal((n, H, d))
             if heavy and n:
@@ -226,7 +227,7 @@ class Case:
                     ref.put(self.pool, self.table[b, t // page] * page + t % page, h, k[t, h], v[t, h], page)
                     self.K[b, t, h], self.V[b, t, h] = ref.values(*ref.quantise(k[t, h])), ref.values(*ref.quantise(v[t, h]))
         self.q, self.qh = rows_on_gpu(rng.standard_normal((B, N, Hq, d)) + 0.3, dtype, layout, pad=1)
-        self.there = np.ones((B, entries * page), bool)
+        self.there = np.ones((B, reach), bool)
         self.q_len = None if q_len is None else np.asarray(q_len, np.int32)
         self.keep = keep
         if keep is not None and not isinstance(keep, np.ndarray):
@@ -245,12 +246,16 @@ class Case:
         return host(out).astype(np.float64), host(lse).astype(np.float64)
 
     def check(self, out, lse, nan_rows=()):
-        step, part = (2.0 ** -8, 2.0 ** -16) if self.dtype == BF16 else (2.0 ** -24, 2.0 ** -23)
+        # bf16 rows: probabilities in two bf16 parts, 16 bits; where 32 rows go together, in one, whose rounding is off by half a
+        # step, 2^-8, at most; fp32 rows: in three bf16 parts, 24 bits
+        rows = self.N * self.Hq // self.H
+        many = self.dtype == BF16 and rows > 16 and self.B * self.H * -(-rows // 16) > 512
+        step, part = (2.0 ** -8, 2.0 ** -8 if many else 2.0 ** -16) if self.dtype == BF16 else (2.0 ** -24, 2.0 ** -23)
         for b in range(self.B):
             nq = self.N if self.q_len is None else int(np.clip(self.q_len[b], 0, self.N))
-            n = int(np.clip(self.lengths[b], 0, self.K.shape[1]))
+            n = int(np.clip(self.lengths[b], 0, self.table.shape[1] * self.page))
             want, wl_, size, score = ref.attend(self.qh[b], self.K[b], self.V[b], self.there[b], n, nq, self.scale,
-                                                None if self.keep is None else self.keep[b])
+                                                None if self.keep is None else self.keep[b, :self.K.shape[1]])
             assert (out[b, nq:] == 7).all() and (lse[b, :, nq:] == 7).all(), f"sample {b}: rows behind the last were written"
             bound, lbound = ref.attend_bounds(want, wl_, size, score, self.d, n, step, part)
             got = out[b, :nq]
@@ -292,6 +297,19 @@ CASES = [
     dict(lengths=[3001, 1500, 1], N=1, Hq=2, H=1, d=128, page=32, dtype=BF16),
     dict(lengths=[2500, 700], N=20, Hq=4, H=2, d=64, page=64, dtype=BF16),
     dict(lengths=[2000], N=40, Hq=4, H=1, d=128, page=16, dtype=F32),
+    # runs of equal work over the borders of samples, some of them empty; more than 64 samples; many rows
+    dict(lengths=[0, 700, 1, 33, 0, 1234, 64], N=3, Hq=4, H=2, d=128, page=16, dtype=BF16, entries=200, q_len=[3, 3, 1, 0, 2, 3, 3]),
+    dict(lengths=[0, 700, 1, 33, 0, 1234, 64], N=3, Hq=4, H=2, d=64, page=16, dtype=F32, entries=200, keep=0.6),
+    dict(lengths=[(37 * b) % 90 for b in range(150)], N=1, Hq=1, H=1, d=64, page=256, dtype=BF16, entries=65),
+    dict(lengths=[300, 40, 90], N=90, Hq=12, H=2, d=64, page=256, dtype=BF16, entries=65, q_len=[90, 41, 90]),
+    dict(lengths=[1], N=1, Hq=3, H=3, d=128, page=32, dtype=BF16, entries=400),
+    # eight waves to a block: short sequences in tables of 512 entries
+    dict(lengths=[500, 3, 130, 0], N=1, Hq=5, H=5, d=128, page=64, dtype=BF16, entries=8),
+    dict(lengths=[500, 3, 130, 0], N=2, Hq=6, H=3, d=64, page=64, dtype=F32, entries=8, keep=0.5),
+    # 32 rows together, in blocks per unit and in runs
+    dict(lengths=[(29 * b) % 80 for b in range(22)], N=20, Hq=13, H=13, d=64, page=32, dtype=BF16, entries=16, q_len=[(7 * b) % 24 for b in range(22)]),
+    dict(lengths=[(29 * b) % 80 for b in range(22)], N=20, Hq=13, H=13, d=128, page=256, dtype=BF16, entries=65),
+    dict(lengths=[50] * 40, N=9, Hq=28, H=7, d=128, page=16, dtype=BF16, entries=16, keep=0.7, layout="heads"),
 ]
 
 
