@@ -357,7 +357,8 @@ int mustdrop_decode_keep_strided(
  * pool names no page: its entries take no part in attention, its rows are not read out; a slot outside the pool is not written.
  *
  * Limits of the cache4 calls: d in {64, 128}; page a power of two from 16 to 256; n_pages * page < 2^31,
- * max_pages * page < 2^30; a pool of at most 256 GiB; H <= 65535; rows in MD_BF16 or MD_F32; base pointers 16-byte aligned.  md_kv_layout as above
+ * max_pages * page < 2^30; a pool of at most 256 GiB; H <= 65535; rows in MD_BF16 or MD_F32, fewer than 2^28 - 15 of them
+ * (B*N) in or out in a call; base pointers 16-byte aligned.  md_kv_layout as above
  * (elements of the rows' type); NULL = dense token-major.
  */
 size_t mustdrop_cache4_bytes(int n_pages, int page, int H, int d);      /* 0 for sizes that no call takes */

@@ -36,55 +36,114 @@ __device__ __forceinline__ float scale_of(uint32_t code) { return __uint_as_floa
 
 // ------------------------------------------------------------------------------------------------ pages and slots
 
-// One request's part of a call, handed from the first kernel to the second: lengths before and after, and the place on the
+// One sample's part of a call, handed on to whoever writes its entries and slots: lengths before and after, and the place on the
 // stack of the first page that it takes.
 struct PagePlan { int old_len, new_len, first; };
 
-// One block: counts the pages that leave and come, puts the released ones on the stack, and gives each request its place on it.
-// A chain of two scans over the requests; its time is that chain's (see cache4_pages_impl).
+// Of 1024 samples whose entries follow one another from before[b] on, the one that entry x belongs to.
+__device__ __forceinline__ int owner_of(const int* before, int x) {
+    int b = 0;
+#pragma unroll
+    for (int step = 512; step; step >>= 1)
+        if (before[b + step] <= x) b += step;
+    return b;
+}
+
+__device__ __forceinline__ void write_slot(const PagePlan& p, int i, const int32_t* row, const int32_t* free_pages, int n_pages, int page_shift, int32_t* slot) {
+    const int at = p.old_len + i;
+    int s = -1;
+    if (at < p.new_len) {
+        const int e = at >> page_shift, held = c4_pages_of(p.old_len, page_shift), j = p.first - (e - held);
+        const int id = c4_page_id(e < held ? row[e] : (j >= 0 && j < n_pages ? free_pages[j] : -1), n_pages);
+        if (id >= 0) s = (int)(((uint32_t)id << page_shift) + (at & ((1 << page_shift) - 1)));
+    }
+    *slot = s;
+}
+
+// One block: counts the pages that leave and come, gives each sample its place on the stack and puts the released pages there.  The
+// entries of 1024 samples are shared out evenly, four loads of a thread on their way together, whoever's they are.  ALL: the block takes the
+// new pages and writes the slots too.
+template <bool ALL>
 __global__ __launch_bounds__(1024) void cache4_pages_kernel(
-    const int32_t* __restrict__ new_len, int32_t* __restrict__ len, const int32_t* __restrict__ table,
-    int32_t* __restrict__ free_pages, int32_t* __restrict__ n_free, int32_t* __restrict__ missing,
-    int B, int max_pages, int n_pages, int page_shift, PagePlan* __restrict__ plan)
+    const int32_t* __restrict__ new_len, int32_t* __restrict__ len, int32_t* table,
+    int32_t* free_pages, int32_t* __restrict__ n_free, int32_t* __restrict__ slots, int32_t* __restrict__ missing,
+    int B, int max_pages, int n_pages, int page_shift, int N, PagePlan* __restrict__ plan)
 {
-    __shared__ int s_red[16];
+    __shared__ int s_red[16], s_before[1024];
+    __shared__ PagePlan s_plan[1024];
     const int tid = threadIdx.x, top = c4_clamp(n_free[0], 0, n_pages);
-    long leave = 0, come = 0;
+    int leave = 0, come = 0;                         // (the host checks that B * max_pages fits 31 bits)
     for (int b = tid; b < B; b += 1024) {
         const C4Change c = c4_change(len[b], new_len[b], max_pages, page_shift);
         if (c.held > c.need) leave += c.held - c.need;
         else come += c.need - c.held;
     }
-    // (the host checks that B * max_pages fits 31 bits)
-    const int R = block_sum_i((int)leave, s_red), T = block_sum_i((int)come, s_red);
+    const int R = block_sum_i(leave, s_red), T = block_sum_i(come, s_red);
     const int left = top + R - T;
-    if (tid == 0) missing[0] = left < 0 ? -left : 0;
-    if (left < 0) {
-        for (int b = tid; b < B; b += 1024) plan[b] = PagePlan{0, 0, 0};
-        return;
+    if (tid == 0) {
+        missing[0] = left < 0 ? -left : 0;
+        if (left >= 0) n_free[0] = min(left, n_pages);
     }
     int left_before = 0, come_before = 0;
     for (int b0 = 0; b0 < B; b0 += 1024) {
         const int b = b0 + tid;
         C4Change c{0, 0, 0, 0};
-        if (b < B) c = c4_change(len[b], new_len[b], max_pages, page_shift);
-        const int lv = max(c.held - c.need, 0), cm = max(c.need - c.held, 0);
+        if (b < B && left >= 0) c = c4_change(len[b], new_len[b], max_pages, page_shift);
         int lt, ct;
-        const int lp = left_before + block_exscan_i(lv, s_red, lt), cp = come_before + block_exscan_i(cm, s_red, ct);
+        const int lp = block_exscan_i(max(c.held - c.need, 0), s_red, lt), cp = block_exscan_i(max(c.need - c.held, 0), s_red, ct);
+        const PagePlan mine{c.old_len, c.new_len, c4_taken_at(top, R, come_before + cp)};
+        s_plan[tid] = mine;
+        s_before[tid] = lp;
+        if (b < B) {
+            if (left >= 0) len[b] = c.new_len;
+            if (!ALL) plan[b] = mine;
+        }
+        __syncthreads();
+        for (int x0 = tid; x0 < lt; x0 += 4096) {
+            int id[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int x = x0 + i * 1024;
+                if (x >= lt) continue;
+                const int from = owner_of(s_before, x);
+                id[i] = table[(long)(b0 + from) * max_pages + c4_pages_of(s_plan[from].new_len, page_shift) + x - s_before[from]];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int x = x0 + i * 1024, at = c4_released_at(top, R, left_before + x);
+                if (x < lt && at < n_pages) free_pages[at] = id[i];
+            }
+        }
         left_before += lt;
         come_before += ct;
-        if (b >= B) continue;
-        for (int e = 0; e < lv; ++e) {
-            const int at = c4_released_at(top, R, lp + e);
-            if (at < n_pages) free_pages[at] = table[(long)b * max_pages + c.need + e];
+        __syncthreads();
+        if (!ALL) continue;
+        s_before[tid] = cp;                          // (ALL has one round: every page that is taken is on the stack by now)
+        __syncthreads();
+        for (int x0 = tid; x0 < ct; x0 += 4096) {
+            int id[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = c4_taken_at(top, R, x0 + i * 1024);
+                id[i] = x0 + i * 1024 < ct && at < n_pages ? free_pages[at] : -1;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int x = x0 + i * 1024;
+                if (x >= ct || c4_taken_at(top, R, x) >= n_pages) continue;
+                const int to = owner_of(s_before, x);
+                table[(long)to * max_pages + c4_pages_of(s_plan[to].old_len, page_shift) + x - s_before[to]] = id[i];
+            }
         }
-        plan[b] = PagePlan{c.old_len, c.new_len, c4_taken_at(top, R, cp)};
-        len[b] = c.new_len;
     }
-    if (tid == 0) n_free[0] = min(left, n_pages);
+    if (ALL)
+        for (int x = tid; x < B * N; x += 1024) {
+            const int b = x / N;
+            write_slot(s_plan[b], x - b * N, table + (long)b * max_pages, free_pages, n_pages, page_shift, slots + x);
+        }
 }
 
-// Entries and slots of one request per blockIdx.y.
+// Entries and slots of one sample per blockIdx.y.
 __global__ __launch_bounds__(256) void cache4_slots_kernel(
     const PagePlan* __restrict__ plan, int32_t* __restrict__ table, const int32_t* __restrict__ free_pages,
     int32_t* __restrict__ slots, int max_pages, int n_pages, int page_shift, int N)
@@ -93,21 +152,20 @@ __global__ __launch_bounds__(256) void cache4_slots_kernel(
     const PagePlan p = plan[b];
     const int held = c4_pages_of(p.old_len, page_shift), need = c4_pages_of(p.new_len, page_shift);
     int32_t* row = table + (long)b * max_pages;
-    // place `first - j` of the stack holds the j-th page that the request takes
+    // place `first - j` of the stack holds the j-th page that the sample takes
     if (i < need - held && p.first - i >= 0 && p.first - i < n_pages) row[held + i] = free_pages[p.first - i];
-    if (slots && i < N) {
-        const int at = p.old_len + i;
-        int slot = -1;
-        if (at < p.new_len) {
-            const int e = at >> page_shift, j = p.first - (e - held);
-            const int id = c4_page_id(e < held ? row[e] : (j >= 0 && j < n_pages ? free_pages[j] : -1), n_pages);
-            if (id >= 0) slot = (int)(((uint32_t)id << page_shift) + (at & ((1 << page_shift) - 1)));
-        }
-        slots[(long)b * N + i] = slot;
-    }
+    if (slots && i < N) write_slot(p, i, row, free_pages, n_pages, page_shift, slots + (long)b * N + i);
 }
 
 // ------------------------------------------------------------------------------------------------ rows in and out
+
+// Heads that a wave of the copies takes: one, unless there are waves for all of the chip more than once; then two on the way in and
+// four on the way out.  us with one / two / four heads: 16 x up to 640 rows of 32 heads in 30.5 / 29.3 / 28.4, out 27.1 / 25.2 / 23.9; 4 x 777
+// fp32 rows of 40 heads of 64 in 13.2 / 13.1 / 13.9; 64 x 1025 rows out 369 / 313 / 295; 64 rows in 3.0 / 3.8 / 4.4, 4 x 160 rows of 40 heads out 4.4 /
+// 4.6 / 4.8.  Rows out by streaming stores: 64 x 1025 rows 318 us with plain ones, 4 x 160 rows 5.3, and what follows does not wait for their
+// lines to leave the caches (rows in behind rows out 28.4 us, 36.7 behind plain stores).
+constexpr long kManyWaves = 16384;
+inline bool many_rows(long rows, int H) { return (rows + 3) / 4 * H >= kManyWaves; }
 
 // A lane's share of a row: d/16 channels, fp32.
 template <int D, bool F32>
@@ -122,13 +180,20 @@ __device__ __forceinline__ void load_part(const void* base, long at, float (&x)[
             for (int j = 0; j < 4; ++j) x[4 * i + j] = w[j];
         }
     } else {
-        const u32x2* p = reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(base) + at);
+        uint32_t w[C / 2];
+        if (D == 128) {
+            const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + at);
+            const u32x4 v = *p;
 #pragma unroll
-        for (int i = 0; i < C / 4; ++i) {
-            const u32x2 w = p[i];
-            x[4 * i] = bf16_lo(w[0]); x[4 * i + 1] = bf16_hi(w[0]);
-            x[4 * i + 2] = bf16_lo(w[1]); x[4 * i + 3] = bf16_hi(w[1]);
+            for (int i = 0; i < C / 2; ++i) w[i] = v[i];
+        } else {
+            const u32x2* p = reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(base) + at);
+            const u32x2 v = *p;
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i) w[i] = v[i];
         }
+#pragma unroll
+        for (int i = 0; i < C / 2; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
     }
 }
 
@@ -159,34 +224,41 @@ __device__ __forceinline__ void store_codes(uint8_t* p, uint32_t w) {
     else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w;
 }
 
-// A wave writes four rows of one head: sixteen lanes per row, d/16 channels each.
-template <int D, bool F32>
+// A wave writes four rows, sixteen lanes per row with d/16 channels each, of HEADS heads: their loads are on their way together.
+template <int D, bool F32, int HEADS>
 __global__ __launch_bounds__(256) void cache4_write_kernel(
     const void* __restrict__ k_new, const void* __restrict__ v_new, const int32_t* __restrict__ slots, uint8_t* __restrict__ cache,
-    Pool p, KvLayout lay, long rows, int N)
+    Pool p, KvLayout lay, int rows, int N)
 {
-    const int lane = lane_id(), part = lane & 15;
-    const long unit = (long)blockIdx.x * 4 + wave_id();
-    const int h = (int)(unit % p.H);
-    const long r = unit / p.H * 4 + (lane >> 4);
+    const int lane = lane_id(), part = lane & 15, h0 = blockIdx.y * HEADS;
+    const int r = (int)blockIdx.x * 16 + wave_id() * 4 + (lane >> 4);        // (the host checks that this fits 31 bits)
     C4Slot at{-1, 0};
     if (r < rows) at = c4_slot(slots[r], p.n_pages, p.page_shift);
-    float k[D / 16] = {}, v[D / 16] = {};
+    float k[HEADS][D / 16] = {}, v[HEADS][D / 16] = {};
     if (at.page >= 0) {
-        const long b = r / N, from = b * lay.batch + (r - b * N) * lay.token + (long)h * lay.head + part * (D / 16);
-        load_part<D, F32>(k_new, from, k);
-        load_part<D, F32>(v_new, from, v);
+        const int b = r / N;
+        const long from = b * lay.batch + (long)(r - b * N) * lay.token + part * (D / 16);
+#pragma unroll
+        for (int x = 0; x < HEADS; ++x)
+            if (h0 + x < p.H) {
+                load_part<D, F32>(k_new, from + (long)(h0 + x) * lay.head, k[x]);
+                load_part<D, F32>(v_new, from + (long)(h0 + x) * lay.head, v[x]);
+            }
     }
-    int ks, vs;
-    const uint32_t kw = quantise_part<D>(k, ks), vw = quantise_part<D>(v, vs);
-    if (at.page < 0) return;
-    uint8_t* to = cache + ((long)at.page * p.H + h) * p.stride;
-    store_codes<D>(to + c4_k_codes(at.place, D) + part * (D / 32), kw);
-    store_codes<D>(to + c4_v_codes(p.page, at.place, part, D), vw);
     const int group = part / (512 / D);
-    if (part % (512 / D) == 0) {
-        to[c4_k_scales(p.page, at.place, D) + group] = (uint8_t)ks;
-        to[c4_v_scales(p.page, at.place, group, D)] = (uint8_t)vs;
+    uint8_t* to = cache + ((long)at.page * p.H + h0) * p.stride;
+#pragma unroll
+    for (int x = 0; x < HEADS; ++x) {
+        int ks, vs;
+        const uint32_t kw = quantise_part<D>(k[x], ks), vw = quantise_part<D>(v[x], vs);
+        if (at.page < 0 || h0 + x >= p.H) continue;
+        store_codes<D>(to + c4_k_codes(at.place, D) + part * (D / 32), kw);
+        store_codes<D>(to + c4_v_codes(p.page, at.place, part, D), vw);
+        if (part % (512 / D) == 0) {
+            to[c4_k_scales(p.page, at.place, D) + group] = (uint8_t)ks;
+            to[c4_v_scales(p.page, at.place, group, D)] = (uint8_t)vs;
+        }
+        to += p.stride;
     }
 }
 
@@ -199,47 +271,58 @@ template <int D, bool F32>
 __device__ __forceinline__ void store_values(void* base, long at, uint32_t w, uint32_t code) {
     const float s = scale_of(code);
     if (F32) {
-        f32x2* p = reinterpret_cast<f32x2*>(static_cast<float*>(base) + at);
-        p[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0);
-        p[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
+        f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(base) + at);
+        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
+        __builtin_nontemporal_store(f32x4{a.x, a.y, b.x, b.y}, p);
         if (D == 128) {
-            p[D / 64] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2);
-            p[D / 64 + 1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
+            const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
+            __builtin_nontemporal_store(f32x4{c.x, c.y, d.x, d.y}, p + 1);
         }
     } else {
-        uint32_t* p = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(base) + at);
-        p[0] = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
-        p[1] = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+        uint16_t* p = static_cast<uint16_t*>(base) + at;
+        const uint32_t a = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0)), b = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
         if (D == 128) {
-            p[D / 64] = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
-            p[D / 64 + 1] = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+            const u32x4 v{a, b, as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2)), as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3))};
+            __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+        } else {
+            __builtin_nontemporal_store(u32x2{a, b}, reinterpret_cast<u32x2*>(p));
         }
     }
 }
 
 // The way back, shared out as in the write.
-template <int D, bool F32>
+template <int D, bool F32, int HEADS>
 __global__ __launch_bounds__(256) void cache4_read_kernel(
     const uint8_t* __restrict__ cache, const int32_t* __restrict__ table, const int32_t* __restrict__ len, const int32_t* __restrict__ first,
-    void* __restrict__ k_out, void* __restrict__ v_out, Pool p, KvLayout lay, long rows, int N)
+    void* __restrict__ k_out, void* __restrict__ v_out, Pool p, KvLayout lay, int rows, int N)
 {
-    const int lane = lane_id(), part = lane & 15;
-    const long unit = (long)blockIdx.x * 4 + wave_id();
-    const int h = (int)(unit % p.H);
-    const long r = unit / p.H * 4 + (lane >> 4);
+    const int lane = lane_id(), part = lane & 15, h0 = blockIdx.y * HEADS;
+    const int r = (int)blockIdx.x * 16 + wave_id() * 4 + (lane >> 4);
     if (r >= rows) return;
-    const int b = (int)(r / N), i = (int)(r - (long)b * N);
+    const int b = r / N, i = r - b * N;
     const long at = (first ? (long)first[b] : 0l) + i;
     if (at < 0 || at >= c4_clamp(len[b], 0, p.max_pages << p.page_shift)) return;
     const int t = (int)at & (p.page - 1), id = c4_page_id(table[(long)b * p.max_pages + ((int)at >> p.page_shift)], p.n_pages);
     if (id < 0) return;
-    const uint8_t* from = cache + ((long)id * p.H + h) * p.stride;
-    const uint32_t kw = load_codes<D>(from + c4_k_codes(t, D) + part * (D / 32)), vw = load_codes<D>(from + c4_v_codes(p.page, t, part, D));
+    const uint8_t* from = cache + ((long)id * p.H + h0) * p.stride;
     const int group = part / (512 / D);
-    const uint32_t ks = from[c4_k_scales(p.page, t, D) + group], vs = from[c4_v_scales(p.page, t, group, D)];
-    const long to = b * lay.batch + i * lay.token + (long)h * lay.head + part * (D / 16);
-    store_values<D, F32>(k_out, to, kw, ks);
-    store_values<D, F32>(v_out, to, vw, vs);
+    uint32_t kw[HEADS], vw[HEADS], ks[HEADS], vs[HEADS];
+#pragma unroll
+    for (int x = 0; x < HEADS; ++x)
+        if (h0 + x < p.H) {
+            kw[x] = load_codes<D>(from + c4_k_codes(t, D) + part * (D / 32));
+            vw[x] = load_codes<D>(from + c4_v_codes(p.page, t, part, D));
+            ks[x] = from[c4_k_scales(p.page, t, D) + group];
+            vs[x] = from[c4_v_scales(p.page, t, group, D)];
+            from += p.stride;
+        }
+    const long to = b * lay.batch + i * lay.token + part * (D / 16);
+#pragma unroll
+    for (int x = 0; x < HEADS; ++x)
+        if (h0 + x < p.H) {
+            store_values<D, F32>(k_out, to + (long)(h0 + x) * lay.head, kw[x], ks[x]);
+            store_values<D, F32>(v_out, to + (long)(h0 + x) * lay.head, vw[x], vs[x]);
+        }
 }
 
 // ------------------------------------------------------------------------------------------------ attention
@@ -1049,6 +1132,7 @@ int check_dtype(const char* who, int dtype) {
 }
 
 constexpr long kMaxGrid = 0x7FFFFFFFl;
+constexpr long kMaxRows = (1l << 28) - 16;            // 16 threads per row, and a launch has fewer than 2^32 along x
 
 struct Range { const void* p; size_t n; };
 // None of the first `outs` ranges may share a byte with any other range.
@@ -1082,11 +1166,18 @@ int pages_impl(const int32_t* new_len, int32_t* len, int32_t* table, int32_t* fr
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(MD_EALIGN, "cache4_pages: workspace must be 256-byte aligned");
     PagePlan* plan = static_cast<PagePlan*>(workspace);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    MD_LAUNCH("cache4_pages", st, (cache4_pages_kernel), 1, 1024, 0,
-        new_len, len, table, free_pages, n_free, missing, B, max_pages, n_pages, p.page_shift, plan);
-    const int most = N > max_pages ? N : max_pages;
-    MD_LAUNCH("cache4_slots", st, (cache4_slots_kernel), dim3((most + 255) / 256, B), 256, 0,
-        plan, table, free_pages, slots, max_pages, n_pages, p.page_shift, N);
+    // One launch while a thread has up to 16 slots to write, else a second one with all of the chip.  us of a call that grows and one that
+    // shrinks, one launch / two: 1 x 1 to 64 x 256 slots 14.5 / 18.3 (the host's time), 64 x 512 19.6 / 18.2, 256 x 128 19.7 / 18.0.
+    if (B <= 1024 && (long)B * N <= 16384) {
+        MD_LAUNCH("cache4_pages", st, (cache4_pages_kernel<true>), 1, 1024, 0,
+            new_len, len, table, free_pages, n_free, slots, missing, B, max_pages, n_pages, p.page_shift, N, plan);
+    } else {
+        MD_LAUNCH("cache4_pages", st, (cache4_pages_kernel<false>), 1, 1024, 0,
+            new_len, len, table, free_pages, n_free, slots, missing, B, max_pages, n_pages, p.page_shift, N, plan);
+        const int most = N > max_pages ? N : max_pages;
+        MD_LAUNCH("cache4_slots", st, (cache4_slots_kernel), dim3((most + 255) / 256, B), 256, 0,
+            plan, table, free_pages, slots, max_pages, n_pages, p.page_shift, N);
+    }
     return check_launch("cache4_pages");
 }
 
@@ -1106,17 +1197,21 @@ int write_impl(const void* k_new, const void* v_new, int dtype, const int32_t* s
     rc = read_layout("cache4_write", "rows", rows_layout, B, N, H, d, &lay);
     if (rc != MD_OK) return rc;
     if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(cache)) return fail(MD_EALIGN, "cache4_write: tensors must be 16-byte aligned");
-    const long rows = (long)B * N, blocks = ((rows + 3) / 4 * H + 3) / 4;
-    if (blocks > kMaxGrid) return fail(MD_ESHAPE, "cache4_write: too many rows");
+    const long rows = (long)B * N;
+    if (rows > kMaxRows) return fail(MD_ESHAPE, "cache4_write: %ld rows are too many for one call", rows);
     const size_t in = rows_bytes(lay, B, N, H, d, dtype);
     const Range r[] = {{cache, pool_bytes(p)}, {k_new, in}, {v_new, in}, {slots, (size_t)rows * 4}};
     rc = check_apart("cache4_write", r, 1, 4);
     if (rc != MD_OK) return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
-#define MD_C4_WRITE(D_, F_) MD_LAUNCH("cache4_write", st, (cache4_write_kernel<D_, F_>), (int)blocks, 256, 0, k_new, v_new, slots, static_cast<uint8_t*>(cache), p, lay, rows, N)
+#define MD_C4_WRITE2(D_, F_, X_)                                                                                                          \
+    MD_LAUNCH("cache4_write", st, (cache4_write_kernel<D_, F_, X_>), dim3((int)((rows + 15) / 16), (H + X_ - 1) / X_), 256, 0,            \
+        k_new, v_new, slots, static_cast<uint8_t*>(cache), p, lay, (int)rows, N)
+#define MD_C4_WRITE(D_, F_) do { if (many_rows(rows, H)) MD_C4_WRITE2(D_, F_, 2); else MD_C4_WRITE2(D_, F_, 1); } while (0)
     if (d == 128) { if (dtype == MD_F32) MD_C4_WRITE(128, true); else MD_C4_WRITE(128, false); }
     else { if (dtype == MD_F32) MD_C4_WRITE(64, true); else MD_C4_WRITE(64, false); }
 #undef MD_C4_WRITE
+#undef MD_C4_WRITE2
     return check_launch("cache4_write");
 }
 
@@ -1134,18 +1229,22 @@ int read_impl(const void* cache, const int32_t* table, const int32_t* len, const
     rc = read_layout("cache4_read", "rows", rows_layout, B, N, H, d, &lay);
     if (rc != MD_OK) return rc;
     if (!aligned16(k_out) || !aligned16(v_out) || !aligned16(cache)) return fail(MD_EALIGN, "cache4_read: tensors must be 16-byte aligned");
-    const long rows = (long)B * N, blocks = ((rows + 3) / 4 * H + 3) / 4;
-    if (blocks > kMaxGrid) return fail(MD_ESHAPE, "cache4_read: too many rows");
+    const long rows = (long)B * N;
+    if (rows > kMaxRows) return fail(MD_ESHAPE, "cache4_read: %ld rows are too many for one call", rows);
     const size_t outb = rows_bytes(lay, B, N, H, d, dtype);
     const Range r[] = {{k_out, outb}, {v_out, outb}, {cache, pool_bytes(p)}, {table, (size_t)B * max_pages * 4}, {len, (size_t)B * 4},
                        {first, first ? (size_t)B * 4 : 0}};
     rc = check_apart("cache4_read", r, 2, 6);
     if (rc != MD_OK) return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
-#define MD_C4_READ(D_, F_) MD_LAUNCH("cache4_read", st, (cache4_read_kernel<D_, F_>), (int)blocks, 256, 0, static_cast<const uint8_t*>(cache), table, len, first, k_out, v_out, p, lay, rows, N)
+#define MD_C4_READ2(D_, F_, X_)                                                                                                           \
+    MD_LAUNCH("cache4_read", st, (cache4_read_kernel<D_, F_, X_>), dim3((int)((rows + 15) / 16), (H + X_ - 1) / X_), 256, 0,              \
+        static_cast<const uint8_t*>(cache), table, len, first, k_out, v_out, p, lay, (int)rows, N)
+#define MD_C4_READ(D_, F_) do { if (many_rows(rows, H)) MD_C4_READ2(D_, F_, 4); else MD_C4_READ2(D_, F_, 1); } while (0)
     if (d == 128) { if (dtype == MD_F32) MD_C4_READ(128, true); else MD_C4_READ(128, false); }
     else { if (dtype == MD_F32) MD_C4_READ(64, true); else MD_C4_READ(64, false); }
 #undef MD_C4_READ
+#undef MD_C4_READ2
     return check_launch("cache4_read");
 }
 

@@ -151,6 +151,7 @@ def test_rows_refusals(lib, call):
     assert call(lib, lay=layout(3 * 512, 512, 0)) == EINVAL
     assert call(lib, lay=layout(3 * 512, 512, 64)) == ESHAPE                     # heads overlap
     assert call(lib, B=1 << 20, N=1 << 20, H=1) == ESHAPE
+    assert call(lib, B=1 << 8, N=1 << 20, H=1) == ESHAPE and b"rows" in lib.mustdrop_last_error()   # 2^28
     if call is read:
         assert call(lib, v=P(1)) == EALIAS and call(lib, k=P(5)) == EALIAS and call(lib, max_pages=0) == EINVAL
 

@@ -184,6 +184,38 @@ def test_rows_in_and_out(B, N, H, d, page, dtype, layout):
                     assert np.array_equal(vo[b, i, h], gv.astype(np.float32), equal_nan=True), (b, i, h)
 
 
+@pytest.mark.parametrize("B, N, H, d, dtype, layout", [(3, 3001, 9, 128, BF16, "heads"), (2, 5003, 7, 64, F32, "tokens"), (1, 16400, 5, 128, F32, "heads"),
+                                                       (5, 1300, 13, 64, BF16, "tokens")])
+def test_many_rows_are_what_few_rows_are(B, N, H, d, dtype, layout):
+    """A call of many rows takes several heads per wave: the same bytes as its pieces of few rows, which the test above checks."""
+    import torch
+    import paper_2411_10803_amd as md
+    page = 64
+    rng = np.random.default_rng(N)
+    length = np.full(B, N, np.int32)
+    length[-1] -= 77
+    table, n_pages = scattered(rng, length, page, -(-N // page))
+    at = np.arange(N)
+    slots = dev(np.where(at < length[:, None], table[:, at // page] * page + at % page, -1).astype(np.int32))
+    k, _ = rows_on_gpu(rng.standard_normal((B, N, H, d)), dtype, layout, pad=1)
+    v, _ = rows_on_gpu(rng.standard_normal((B, N, H, d)), dtype, layout, pad=1)
+    whole, parts = (torch.full_like(md.cache4_buffer(n_pages, page, H, d), 0x5A) for _ in range(2))
+    md.mustdrop_cache4_write(k, v, slots, whole)
+    for i in range(0, N, 999):
+        md.mustdrop_cache4_write(k[:, i:i + 999], v[:, i:i + 999], slots[:, i:i + 999].contiguous(), parts)
+    torch.cuda.synchronize()
+    assert torch.equal(whole, parts)
+    table, length = dev(table), dev(length)
+    out = [rows_on_gpu(np.full((B, N, H, d), 7.0), dtype, layout, pad=1)[0] for _ in range(4)]
+    md.mustdrop_cache4_read(whole, table, length, out[0], out[1])
+    for i in range(0, N, 999):
+        first = torch.full((B,), i, dtype=torch.int32, device="cuda")
+        md.mustdrop_cache4_read(whole, table, length, out[2][:, i:i + 999], out[3][:, i:i + 999], first=first)
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3])
+    assert (out[0][-1, -77:] == 7).all() and not (out[0][-1, :-77] == 7).all()
+
+
 def test_rows_out_of_bad_pages_and_places_are_left_alone():
     import torch
     import paper_2411_10803_amd as md
