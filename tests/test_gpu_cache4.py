@@ -239,7 +239,7 @@ def test_rows_out_of_bad_pages_and_places_are_left_alone():
 class Case:
     """Inputs of one attention call, on both sides."""
 
-    def __init__(self, seed, lengths, N, Hq, H, d, page, dtype, q_len=None, keep=None, layout="tokens", entries=None, size=1.0, heavy=True):
+    def __init__(self, seed, lengths, N, Hq, H, d, page, dtype, q_len=None, keep=None, layout="tokens", entries=None, size=1.0, heavy=True, spread=0):
         import torch
         rng = np.random.default_rng(seed)
         B = len(lengths)
@@ -258,7 +258,11 @@ class Case:
                 for h in range(H):
                     ref.put(self.pool, self.table[b, t // page] * page + t % page, h, k[t, h], v[t, h], page)
                     self.K[b, t, h], self.V[b, t, h] = ref.values(*ref.quantise(k[t, h])), ref.values(*ref.quantise(v[t, h]))
-        self.q, self.qh = rows_on_gpu(rng.standard_normal((B, N, Hq, d)) + 0.3, dtype, layout, pad=1)
+        q = rng.standard_normal((B, N, Hq, d)) + 0.3
+        if spread:                                     # channels of all sizes
+            q *= np.exp2(rng.integers(-spread, 1, q.shape).astype(float))
+        self.q, self.qh = rows_on_gpu(q, dtype, layout, pad=1)
+        self.spread = spread
         self.there = np.ones((B, reach), bool)
         self.q_len = None if q_len is None else np.asarray(q_len, np.int32)
         self.keep = keep
@@ -289,6 +293,11 @@ class Case:
             want, wl_, size, score = ref.attend(self.qh[b], self.K[b], self.V[b], self.there[b], n, nq, self.scale,
                                                 None if self.keep is None else self.keep[b, :self.K.shape[1]])
             assert (out[b, nq:] == 7).all() and (lse[b, :, nq:] == 7).all(), f"sample {b}: rows behind the last were written"
+            if self.spread and self.dtype == BF16 and self.d == 128:
+                # a channel below 2^-14 of its row's largest is off by 2^-22 of that at most: so much times |k| more per score, where
+                # attend_bounds counts (d + 4) 2^-24 of sum |q||k|
+                most = np.abs(self.qh[b]).max(-1) * self.scale * np.abs(self.K[b]).sum(-1).max()
+                score = score + most * 2.0 ** -22 / ((self.d + 4) * 2.0 ** -24)
             bound, lbound = ref.attend_bounds(want, wl_, size, score, self.d, n, step, part)
             got = out[b, :nq]
             assert np.array_equal(np.isnan(got), np.isnan(want[:nq])), f"sample {b}: NaN"
@@ -342,6 +351,10 @@ CASES = [
     dict(lengths=[(29 * b) % 80 for b in range(22)], N=20, Hq=13, H=13, d=64, page=32, dtype=BF16, entries=16, q_len=[(7 * b) % 24 for b in range(22)]),
     dict(lengths=[(29 * b) % 80 for b in range(22)], N=20, Hq=13, H=13, d=128, page=256, dtype=BF16, entries=65),
     dict(lengths=[50] * 40, N=9, Hq=28, H=7, d=128, page=16, dtype=BF16, entries=16, keep=0.7, layout="heads"),
+    # queries whose channels are far apart
+    dict(lengths=[260, 31], N=2, Hq=4, H=2, d=128, page=32, dtype=BF16, spread=30, size=8.0),
+    dict(lengths=[260, 31], N=2, Hq=4, H=2, d=128, page=32, dtype=BF16, spread=13, size=8.0),
+    dict(lengths=[260, 31], N=2, Hq=4, H=2, d=64, page=32, dtype=BF16, spread=30, size=8.0),
 ]
 
 
