@@ -593,32 +593,33 @@ struct Rows {
         }
     }
 
-    // Keys of the step that the call leaves out for all rows get a V scale of 1 (0 * NaN would count); `sees` gets a bit for each
-    // of the lane's eight keys that its row sees.
-    __device__ __forceinline__ void mask(const Walk& w, int step, const Kept& kp, uint32_t (&vs)[2], uint32_t (&sees)[NT]) {
+    // Keys of the step that the call leaves out for all rows get a V scale of 1 (0 * NaN would count); `hides` gets a bit for each
+    // of the lane's eight keys that its row does not see: of key x of tile u bit 8 x + 7 - 4 u.  Four keys at a time, a byte each.
+    __device__ __forceinline__ void mask(const Walk& w, int step, const Kept& kp, uint32_t (&vs)[2], uint32_t (&hides)[NT]) {
+        constexpr uint32_t kTops = 0x80808080u;
+        const auto nonzero = [](uint32_t x) { return (((x & ~kTops) + ~kTops) | x) & kTops; };
+        const auto first = [](int n) { return n <= 0 ? 0u : kTops >> (32 - 8 * min(n, 4)); };
         const Pages pg = pages_at(w, step);
         const bool ok[2] = {there(w, step, pg, 0), there(w, step, pg, 1)};
-        bool nan = false;
+        uint32_t nan = 0;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sees[t] = 0;
+        for (int t = 0; t < NT; ++t) hides[t] = 0;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int t = step * 32 + 16 * u + 4 * lb;
             const uint32_t w0 = kp.w[u][0], w1 = kp.w[u][1], w2 = kp.w[u][2], w3 = kp.w[u][3];
             const uint32_t even = lb & 2 ? w2 : w0, odd = lb & 2 ? w3 : w1, kept = lb & 1 ? odd : even;
+            const uint32_t on = nonzero(kept) & first((ok[u] ? w.end : 0) - t), nans = kTops & ~nonzero(~vs[u]);
+            nan |= on & nans;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const bool on = ok[u] && t + x < w.end && ((kept >> (8 * x)) & 0xFF) != 0;
-#pragma unroll
-                for (int z = 0; z < NT; ++z)
-                    if (on && t + x < limit[z]) sees[z] |= 1u << (4 * u + x);
-                const uint32_t code = (vs[u] >> (8 * x)) & 0xFF;
-                nan |= on && code == 255;
-                if (!on || code == 255) vs[u] = (vs[u] & ~(0xFFu << (8 * x))) | (127u << (8 * x));
-            }
+            for (int z = 0; z < NT; ++z) hides[z] |= (on & first(limit[z] - t)) >> (4 * u);
+            const uint32_t out = (kTops & ~on) | nans, bytes = (out << 1) - (out >> 7);
+            vs[u] = (vs[u] & ~bytes) | (bytes & 0x7F7F7F7Fu);
         }
+#pragma unroll
+        for (int z = 0; z < NT; ++z) hides[z] = ~hides[z];
         // A NaN in V of a key that some rows see and others do not: the rows that see it get it in that group's channels here.
-        if (__any(nan)) {
+        if (__any(nan != 0)) {
 #pragma unroll
             for (int z = 0; z < NT; ++z) {
                 float poison = 0.f;
@@ -635,13 +636,15 @@ struct Rows {
     }
 
     // Scores of keys that the lane's row does not see.
-    __device__ __forceinline__ static void hide(f32x4 (&st)[NT][2], uint32_t (&sees)[NT]) {
+    __device__ __forceinline__ static void hide(f32x4 (&st)[NT][2], uint32_t (&hides)[NT]) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            asm volatile("" : "+v"(sees[t]));        // (its bits are looked at here, and not in the steps that need no mask)
+            asm volatile("" : "+v"(hides[t]));       // (its bits are looked at here, and not in the steps that need no mask)
 #pragma unroll
-            for (int x = 0; x < 8; ++x)
-                if (!((sees[t] >> x) & 1)) st[t][x >> 2][x & 3] = -INFINITY;
+            for (int x = 0; x < 8; ++x) {
+                const uint32_t h = (uint32_t)__builtin_amdgcn_sbfe((int)hides[t], 8 * (x & 3) + 7 - 4 * (x >> 2), 1);
+                st[t][x >> 2][x & 3] = __uint_as_float((h & 0xFF800000u) | (~h & __float_as_uint(st[t][x >> 2][x & 3])));
+            }
         }
     }
 
@@ -758,7 +761,7 @@ struct Sweep : Rows<D, F32, NT, PT> {
         return r;
     }
 
-    __device__ __forceinline__ void step(const Walk& w, const Keys& K, bool masked, uint32_t (&sees)[NT]) {
+    __device__ __forceinline__ void step(const Walk& w, const Keys& K, bool masked, uint32_t (&hides)[NT]) {
         f32x4 st[NT][2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -784,7 +787,7 @@ struct Sweep : Rows<D, F32, NT, PT> {
                     for (int z = QT - 1; z >= 0; --z) st[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[t][y][z], st[t][u], 0, 0, 0);
             }
         }
-        if (masked) R::hide(st, sees);
+        if (masked) R::hide(st, hides);
         bf16x8 p[NT][PT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) R::softmax(t, st[t], w.c, p[t]);
@@ -860,9 +863,9 @@ struct Sweep : Rows<D, F32, NT, PT> {
                 ask(w, ahead, pg, ring + x * SLOT);
             }
             x = x + 1 == RING ? 0 : x + 1;
-            uint32_t sees[NT];
-            if (masked) R::mask(w, i, kp, k.vs, sees);
-            step(w, k, masked, sees);
+            uint32_t hides[NT];
+            if (masked) R::mask(w, i, kp, k.vs, hides);
+            step(w, k, masked, hides);
         }
     }
 };
