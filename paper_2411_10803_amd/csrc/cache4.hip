@@ -436,21 +436,24 @@ struct Walk {
 struct Pages { int id[2]; };                         // of a step's two 16-key tiles
 struct Kept { uint32_t w[2][4]; };                   // `keep` of a step's keys
 
-// rows: the first and the last one that count, of those that the sample and head have
-__device__ __forceinline__ Walk walk_of(const AttendArgs& A, const Sample& s, int h, int first_row, int last_row) {
+// What the block table alone takes, so that its first entries can be asked for before the sample's length is there.
+__device__ __forceinline__ Walk table_of(const AttendArgs& A, int b) {
     Walk w;
+    w.row = uniform(A.table + (long)b * A.p.max_pages);
+    w.page_shift = A.p.page_shift;
+    w.last_page = A.p.max_pages - 1;
+    return w;
+}
+// rows: the first and the last one that count, of those that the sample and head have
+__device__ __forceinline__ void walk_of(Walk& w, const AttendArgs& A, const Sample& s, int h, int first_row, int last_row) {
     w.base = global(A.cache) + h * A.p.stride;
-    w.row = uniform(A.table + (long)s.b * A.p.max_pages);
     w.keep = A.keep ? uniform(A.keep + (long)s.b * (A.p.max_pages << A.p.page_shift)) : nullptr;
     w.pitch = (uint32_t)(A.p.H * A.p.stride / 64);
     w.n_pages = A.p.n_pages;
     w.page = A.p.page;
-    w.page_shift = A.p.page_shift;
-    w.last_page = A.p.max_pages - 1;
     w.end = min(max(s.length - s.nq + last_row / A.dim.G + 1, 0), s.length);
     w.clear = A.keep ? 0 : min(max(s.length - s.nq + first_row / A.dim.G + 1, 0), w.end);
     w.c = A.scale * kLog2eC;
-    return w;
 }
 // The entries as they stand in the table, which nobody looks at yet: a wave that asks for them a step ahead does not wait for them.
 __device__ __forceinline__ Pages pages_at(const Walk& w, int step) {
@@ -458,6 +461,18 @@ __device__ __forceinline__ Pages pages_at(const Walk& w, int step) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) r.id[u] = w.row[min((step * 32 + 16 * u) >> w.page_shift, w.last_page)];
     return r;
+}
+// Those of a wave's first steps, on their way together with the sample's length: 0.3 us of a short unit's 10.
+struct Early { Pages at[kRing + 1]; };
+__device__ __forceinline__ Early early_pages(const Walk& w, int first, int stride) {
+    Early r;
+#pragma unroll
+    for (int x = 0; x <= kRing; ++x) r.at[x] = pages_at(w, first + x * stride);
+    return r;
+}
+__device__ __forceinline__ void arrived(Early& r, int& a, int& b) {
+    static_assert(kRing == 2);
+    asm volatile("" : "+s"(r.at[0].id[0]), "+s"(r.at[0].id[1]), "+s"(r.at[1].id[0]), "+s"(r.at[1].id[1]), "+s"(r.at[2].id[0]), "+s"(r.at[2].id[1]), "+s"(a), "+s"(b));
 }
 // Whether they name pages that the step needs.
 __device__ __forceinline__ bool there(const Walk& w, int step, const Pages& p, int u) {
@@ -821,14 +836,14 @@ struct Sweep : Rows<D, F32, NT, PT> {
     }
 
     // Steps first, first + stride, .. below `stop` (of 32 keys).  `ring`: the wave's RING slots.
-    __device__ __forceinline__ void run(const Walk& w, int first, int stop, int stride, char* ring) {
+    __device__ __forceinline__ void run(const Walk& w, int first, int stop, int stride, char* ring, const Early& early) {
         stop = min(stop, (w.end + 31) >> 5);
         if (first >= stop) return;
         uint32_t holes = 0;                                      // bit x: a page of the step in slot x is not there
 #pragma unroll
         for (int x = 0; x < RING; ++x)
             if (first + x * stride < stop) {
-                const Pages pg = pages_at(w, first + x * stride);
+                const Pages pg = early.at[x];
                 if (hole(w, first + x * stride, pg)) holes |= 1u << x;
                 ask(w, first + x * stride, pg, ring + x * SLOT);
             }
@@ -845,7 +860,7 @@ struct Sweep : Rows<D, F32, NT, PT> {
                 for (int z = 0; z < QT; ++z) asm volatile("" : "+v"(q[t][y][z]));
         }
         int x = 0;
-        Pages next = pages_at(w, first + RING * stride);         // (asked for a step before they are needed)
+        Pages next = early.at[RING];                             // (asked for a step before they are needed)
         Kept later = kept_at(w, first);
         for (int i = first; i < stop; i += stride) {
             const int ahead = i + RING * stride;
@@ -945,16 +960,20 @@ __global__ __launch_bounds__(NT == 2 || (F32 && D == 128) ? 256 : 512, NT == 2 |
     constexpr int ROWS = 16 * NT;
     Sweep<D, F32, NT, STREAM, PT> sw;
     Walk w;
+    Early early;
     {
         const AttendArgs A = argument<AttendArgs>(0);
         const int tile = blockIdx.x % A.dim.tiles, bh = blockIdx.x / A.dim.tiles, h = bh % A.p.H, b = bh / A.p.H, r0 = tile * ROWS;
-        const Sample s = sample_of(A, b);
+        w = table_of(A, b);
+        early = early_pages(w, wave_id(), blockDim.x >> 6);
+        Sample s = sample_of(A, b);
+        if (NT == 1) arrived(early, s.length, s.nq);             // (32 rows together are many steps to a wave: a prompt's piece 169 us, 171 so)
         if (r0 >= s.nq * A.dim.G) return;
         sw.begin(A, s, h, r0);
-        w = walk_of(A, s, h, r0, min(r0 + ROWS, s.nq * A.dim.G) - 1);
+        walk_of(w, A, s, h, r0, min(r0 + ROWS, s.nq * A.dim.G) - 1);
     }
     char* lds = reinterpret_cast<char*>(s_lds);
-    sw.run(w, wave_id(), 0x7FFFFFFF, blockDim.x >> 6, lds + wave_id() * (sw.RING * sw.SLOT));
+    sw.run(w, wave_id(), 0x7FFFFFFF, blockDim.x >> 6, lds + wave_id() * (sw.RING * sw.SLOT), early);
     __syncthreads();
     const AttendArgs A = argument<AttendArgs>(0);
     const int tile = blockIdx.x % A.dim.tiles, bh = blockIdx.x / A.dim.tiles, h = bh % A.p.H, b = bh / A.p.H, r0 = tile * ROWS;
@@ -1037,10 +1056,12 @@ __global__ __launch_bounds__(256, NT == 2 || (F32 && D == 128) ? 3 : 4) void cac
     char* lds = reinterpret_cast<char*>(s_lds);
     each_unit(ROWS, blockIdx.x, [&](const AttendArgs& A, const Sample& s, int h, int r0, int first, int last, int place) {
         Sweep<D, F32, NT, STREAM, PT> sw;
+        Walk w = table_of(A, s.b);
+        const Early early = early_pages(w, first + wave_id(), 4);
         sw.begin(A, s, h, r0);
         const int rows = min(ROWS, s.nq * A.dim.G - r0), b = s.b;
-        const Walk w = walk_of(A, s, h, r0, r0 + rows - 1);
-        sw.run(w, first + wave_id(), last, 4, lds + wave_id() * (sw.RING * sw.SLOT));
+        walk_of(w, A, s, h, r0, r0 + rows - 1);
+        sw.run(w, first + wave_id(), last, 4, lds + wave_id() * (sw.RING * sw.SLOT), early);
         __syncthreads();
         const AttendArgs again = argument<AttendArgs>(0);
         const Parts parts = argument<Parts>(kPartsAt);

@@ -91,7 +91,10 @@ MD_PLAN_FN int c4_part_place(int p, int unit_begin, int total, int runs) { retur
 //              16, of 16000 86 / 17, 32 units of 640 7.5 / 11, of 2000 16 / 16, of 4000 26 / 20, 128 of 4000 29 / 25, 256 of 2000 20 / 25, 512 of
 //              4000 55 / 64; 16 units of up to 100000 keys 473 / 46
 //   waves      of a block per unit: eight (four: 64 sequences of up to 4096 keys and 32 heads 124 us instead of 119, 32 units of 2000 keys
-//              22 instead of 16); four where a wave takes more registers, and where a unit has no more than eight steps
+//              22 instead of 16); four where a wave takes more registers, where a unit has no more than eight steps, and where there
+//              are more units than the 512 blocks of eight waves that run at a time and no long ones.  us with four / eight: units of up
+//              to 1000 keys in tables of 2000, 640 of them 20.5 / 22.0, 1024 24 / 27.5, 2048 38 / 45.5, 512 16.6 / 16.9, 256 12.8 / 11.7; of up
+//              to 300 in 600, 2048 22 / 30; of d = 64, 1000 in 2000, 2048 29 / 36; 1024 of up to 2000 in 4000 41 / 38
 struct C4Attend { int tile_rows, tiles, waves; bool runs; };
 constexpr int kC4Blocks = 1024;                      // of the runs: four to a CU
 constexpr int kC4Least = 4;                          // steps of a run, one per wave of its block
@@ -103,7 +106,7 @@ inline C4Attend c4_attend(bool f32, int B, int N, int G, int H, int d, int64_t c
     const int64_t units = (int64_t)B * H * a.tiles;
     // (a run's steps are counted in 31 bits)
     a.runs = (steps * (200 - units) > 16000 || steps > 512) && units < 0x7FFFFFFFl / steps;
-    a.waves = a.runs || a.tile_rows == 32 || (f32 && d == 128) || steps <= 8 ? 4 : 8;
+    a.waves = a.runs || a.tile_rows == 32 || (f32 && d == 128) || steps <= 8 || (steps <= 64 && units > 512) ? 4 : 8;
     return a;
 }
 

@@ -134,7 +134,7 @@ static void forms() {
     CHECK(is(c4_attend(false, 16, 1, 1, 2, 128, 512), 16, 8, false), "eight waves");
     CHECK(is(c4_attend(true, 16, 1, 1, 2, 128, 512), 16, 4, false) && is(c4_attend(true, 16, 1, 1, 2, 64, 512), 16, 8, false), "fp32");
     CHECK(is(c4_attend(false, 22, 20, 1, 13, 64, 512), 32, 4, false), "two tiles");
-    CHECK(is(c4_attend(true, 22, 20, 1, 13, 64, 512), 16, 8, false), "two tiles, fp32");
+    CHECK(is(c4_attend(true, 22, 20, 1, 13, 64, 512), 16, 4, false), "two tiles, fp32");
     CHECK(is(c4_attend(false, 22, 20, 1, 13, 128, 16640), 32, 4, true), "two tiles in runs");
     CHECK(is(c4_attend(false, 16, 1, 1, 16, 64, 16640), 16, 4, true), "very long");
     std::mt19937 rng(3);
