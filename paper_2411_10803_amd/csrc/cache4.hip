@@ -656,10 +656,8 @@ struct Rows {
         for (int t = 0; t < NT; ++t) {
             asm volatile("" : "+v"(hides[t]));       // (its bits are looked at here, and not in the steps that need no mask)
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                const uint32_t h = (uint32_t)__builtin_amdgcn_sbfe((int)hides[t], 8 * (x & 3) + 7 - 4 * (x >> 2), 1);
-                st[t][x >> 2][x & 3] = __uint_as_float((h & 0xFF800000u) | (~h & __float_as_uint(st[t][x >> 2][x & 3])));
-            }
+            for (int x = 0; x < 8; ++x)
+                if ((hides[t] >> (8 * (x & 3) + 7 - 4 * (x >> 2))) & 1) st[t][x >> 2][x & 3] = -INFINITY;
         }
     }
 
@@ -952,6 +950,23 @@ __device__ __forceinline__ void join_waves(S& w, int rows, float* lds, Done done
     }
 }
 
+// The sample of the blocks that come `at`-th: of each 64, the longest first, so that the last blocks to run are short.  us as they come / so: a
+// prompt's piece of 4 x 512 tokens behind up to 5888 keys 169 / 152, of 8 x 512 behind 1500 keys each 157 / 154.  Not for single tokens, which
+// wait for memory: 64 x up to 4096 keys 114 / 122, 64 x up to 500 26 / 33.
+__device__ __forceinline__ int by_length(const AttendArgs& A, int at) {
+    const int base = at & -kWave, lane = lane_id(), n = min(A.dim.B - base, kWave);
+    int mine = -1, before = 0;
+    if (lane < n) {
+        mine = c4_clamp(global(A.len)[base + lane], 0, A.p.max_pages << A.p.page_shift);
+        if (A.q_len && global(A.q_len)[base + lane] <= 0) mine = 0;
+    }
+    for (int j = 0; j < n; ++j) {
+        const int other = __builtin_amdgcn_readlane(mine, j);
+        before += other > mine || (other == mine && j < lane) ? 1 : 0;
+    }
+    return base + (int)__builtin_ctzll(__ballot(lane < n && before == at - base));
+}
+
 // A block per tile of query rows of a (sample, K/V head); its waves take the steps in turn.
 template <int D, bool F32, int NT, bool STREAM, int PT>
 __global__ __launch_bounds__(NT == 2 || (F32 && D == 128) ? 256 : 512, NT == 2 || (F32 && D == 128) ? 3 : 4) void cache4_attend_kernel(AttendArgs A0)
@@ -961,9 +976,12 @@ __global__ __launch_bounds__(NT == 2 || (F32 && D == 128) ? 256 : 512, NT == 2 |
     Sweep<D, F32, NT, STREAM, PT> sw;
     Walk w;
     Early early;
+    int b;
     {
         const AttendArgs A = argument<AttendArgs>(0);
-        const int tile = blockIdx.x % A.dim.tiles, bh = blockIdx.x / A.dim.tiles, h = bh % A.p.H, b = bh / A.p.H, r0 = tile * ROWS;
+        const int tile = blockIdx.x % A.dim.tiles, bh = blockIdx.x / A.dim.tiles, h = bh % A.p.H, r0 = tile * ROWS;
+        b = bh / A.p.H;
+        if (NT == 2 && A.dim.B > 1) b = by_length(A, b);
         w = table_of(A, b);
         early = early_pages(w, wave_id(), blockDim.x >> 6);
         Sample s = sample_of(A, b);
@@ -976,7 +994,7 @@ __global__ __launch_bounds__(NT == 2 || (F32 && D == 128) ? 256 : 512, NT == 2 |
     sw.run(w, wave_id(), 0x7FFFFFFF, blockDim.x >> 6, lds + wave_id() * (sw.RING * sw.SLOT), early);
     __syncthreads();
     const AttendArgs A = argument<AttendArgs>(0);
-    const int tile = blockIdx.x % A.dim.tiles, bh = blockIdx.x / A.dim.tiles, h = bh % A.p.H, b = bh / A.p.H, r0 = tile * ROWS;
+    const int tile = blockIdx.x % A.dim.tiles, h = blockIdx.x / A.dim.tiles % A.p.H, r0 = tile * ROWS;
     const Sample s = sample_of(A, b);
     join_waves<D, NT>(sw, min(ROWS, s.nq * A.dim.G - r0), reinterpret_cast<float*>(s_lds), [&](int row, int part, const float (&x)[D / 16], float m, float l) {
         store_out<D, F32>(A, b, h, r0 + row, part, x, m, l);

@@ -355,6 +355,9 @@ CASES = [
     dict(lengths=[260, 31], N=2, Hq=4, H=2, d=128, page=32, dtype=BF16, spread=30, size=8.0),
     dict(lengths=[260, 31], N=2, Hq=4, H=2, d=128, page=32, dtype=BF16, spread=13, size=8.0),
     dict(lengths=[260, 31], N=2, Hq=4, H=2, d=64, page=32, dtype=BF16, spread=30, size=8.0),
+    # 32 rows together in more than 64 samples, which are taken by their length; many are as long as others, some have no rows
+    dict(lengths=[(23 * b) % 61 for b in range(70)], N=40, Hq=4, H=2, d=64, page=16, dtype=BF16, entries=8, q_len=[(7 * b) % 44 - 2 for b in range(70)]),
+    dict(lengths=[40 - b % 3 for b in range(66)], N=33, Hq=4, H=2, d=128, page=32, dtype=BF16, entries=2),
 ]
 
 
