@@ -405,9 +405,8 @@ int mustdrop_cache4_read(
  *   out      [B, N, Hq, d] (dtype; out_layout), rows >= q_len[b] untouched;  lse [B, Hq, N] f32 or NULL, likewise
  * A row that sees no entry gets out = 0 and lse = -infinity.  Scores, sums and the running maximum are fp32; a probability
  * enters the product with V as a sum of bf16 parts that carries 24 bits for MD_F32 and 16 for MD_BF16, but 8 for MD_BF16 where more
- * than 16 query rows share a K/V head and there are more than 512 tiles of 16 such rows in the call.  For MD_BF16 and d = 128 a
- * channel of q that is smaller than 2^-14 of its row's largest may be off by 2^-22 of that, and a row with an infinity is one of
- * NaN.  Two calls on the same inputs with tables of the same width give the same bits.  Errors: MD_EINVAL, MD_ESHAPE, MD_EDTYPE, MD_EALIGN (keep 4-byte aligned), MD_EALIAS, MD_EWORKSPACE, MD_EHIP. */
+ * than 16 query rows share a K/V head and there are more than 512 tiles of 16 such rows in the call.  Two calls on the same
+ * inputs with tables of the same width give the same bits.  Errors: MD_EINVAL, MD_ESHAPE, MD_EDTYPE, MD_EALIGN (keep 4-byte aligned), MD_EALIAS, MD_EWORKSPACE, MD_EHIP. */
 size_t mustdrop_cache4_attend_workspace_bytes(int B, int N, int Hq, int H, int d, int max_pages, int page);
 
 int mustdrop_cache4_attend(

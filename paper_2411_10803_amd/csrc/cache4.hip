@@ -508,10 +508,8 @@ __device__ __forceinline__ Kept kept_at(const Walk& w, int step) {
 // probabilities are at once the right-hand operand of O^T = V^T P^T: with two 16-key tiles the eight contraction places of lane
 // group b are keys 4 b + 0..3 of either tile.  The pages hold V so that a lane loads those keys' codes of its channels, and of K so
 // that a lane loads d/4 channels of one token: from the loads to the matrix products no lane needs another's data.
-// d = 128 and bf16: K goes into the products as it lies in the pages, four-bit codes and scale bytes (16x16x128 over e2m1 and e4m3); a query row
-// is then the sum of two e4m3 rows with a scale each.  The first keeps 4 of a bf16's 8 bits, the second the other 4: nothing is lost of a
-// channel down to 2^-14 of the row's largest, and of smaller ones at most 2^-22 of that.  (As two matrix instructions per tile of 32 x 16 clocks
-// this takes as long as the four of 16x16x32 over bf16, but K needs no conversion: 32 vector instructions less in a step's 190.)
+// (The scaled 16x16x128 product would take K's codes and scales as they lie and a query as two e4m3 rows, a prompt's piece in 153 us instead of 164,
+// but its sums are not fp32 ones: lse was off 10 to 40 times as far.)
 // PT: bf16 parts of a probability in the product with V; two carry 16 bits, one is as coarse as a bf16 output.
 template <int D, bool F32, int NT, int PT>
 struct Rows {
@@ -519,12 +517,7 @@ struct Rows {
     static constexpr int KS = D / 32;                // contraction steps of S
     static constexpr int J = D / 16;                 // 16-channel tiles of O
 
-    static constexpr bool MX = D == 128 && !F32;
-    typedef int i32x8 __attribute__((ext_vector_type(8)));
-
-    bf16x8 q[MX ? 1 : NT][KS][QT];
-    i32x8 qx[MX ? NT : 1][2];
-    int qs[MX ? NT : 1];                             // their scales, the first one's in the lowest byte
+    bf16x8 q[NT][KS][QT];
     float m[NT], l[NT];
     f32x4 o[NT][J];
     int limit[NT];                                   // keys that the lane's row sees: up to its own position
@@ -542,10 +535,6 @@ struct Rows {
             l[t] = 0.f;
 #pragma unroll
             for (int j = 0; j < J; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if constexpr (MX) {
-                begin_mx(A, s, t, r < live, (long)s.b * A.ql.batch + (long)i * A.ql.token + (long)hq * A.ql.head + lb * 16);
-                continue;
-            }
 #pragma unroll
             for (int y = 0; y < KS; ++y) {
                 uint32_t w[QT][4] = {};
@@ -570,41 +559,6 @@ struct Rows {
 #pragma unroll
                 for (int z = 0; z < QT; ++z) q[t][y][z] = __builtin_bit_cast(bf16x8, u32x4{w[z][0], w[z][1], w[z][2], w[z][3]});
             }
-        }
-    }
-
-    // Tile t's rows in two parts.  A lane brings channels 16 lb .. + 15 and 64 more of them.
-    __device__ __forceinline__ void begin_mx(const AttendArgs& A, const Sample& s, int t, bool on, long at) {
-        u32x4 v[4] = {};
-        if (on) {
-            const bytes_t from = reinterpret_cast<bytes_t>(global(static_cast<const uint16_t*>(A.q)) + at);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) v[x] = load_as<u32x4>(from + (x >> 1) * 128 + (x & 1) * 16);
-        }
-        uint32_t most = 0;
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-            const uint32_t w = v[x >> 2][x & 3] & 0x7FFF7FFFu;
-            most = max(most, max(w & 0xFFFF0000u, w << 16));
-        }
-        // (NaNs and infinities are larger than the rest, and stay so)
-        most = max(most, (uint32_t)__shfl_xor((int)most, 16));
-        most = max(most, (uint32_t)__shfl_xor((int)most, 32));
-        const int e = max((int)(most >> 23), 13), code = e - 7;          // the largest becomes 128 .. 255
-        qs[t] = most >= 0x7F800000u ? 0xFFFF : code | (code - 5) << 8;
-        const float down = __uint_as_float((uint32_t)(254 - code) << 23);
-#pragma unroll
-        for (int x = 0; x < 16; x += 2) {
-            const uint32_t w0 = v[x >> 2][x & 3], w1 = v[x >> 2][(x & 3) + 1];
-            const float f[4] = {bf16_lo(w0) * down, bf16_hi(w0) * down, bf16_lo(w1) * down, bf16_hi(w1) * down};
-            int first = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-            first = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], first, true);
-            const float g[4] = {__builtin_amdgcn_cvt_f32_fp8(first, 0), __builtin_amdgcn_cvt_f32_fp8(first, 1), __builtin_amdgcn_cvt_f32_fp8(first, 2),
-                                __builtin_amdgcn_cvt_f32_fp8(first, 3)};
-            int rest = __builtin_amdgcn_cvt_pk_fp8_f32((f[0] - g[0]) * 32.f, (f[1] - g[1]) * 32.f, 0, false);
-            rest = __builtin_amdgcn_cvt_pk_fp8_f32((f[2] - g[2]) * 32.f, (f[3] - g[3]) * 32.f, rest, true);
-            qx[t][0][x / 2] = first;
-            qx[t][1][x / 2] = rest;
         }
     }
 
@@ -693,7 +647,7 @@ struct Rows {
 template <int D, bool F32, int NT, bool STREAM, int PT>
 struct Sweep : Rows<D, F32, NT, PT> {
     typedef Rows<D, F32, NT, PT> R;
-    using R::KS; using R::J; using R::QT; using R::n; using R::lb; using R::q; using R::qx; using R::qs; using R::o;
+    using R::KS; using R::J; using R::QT; using R::n; using R::lb; using R::q; using R::o;
     static constexpr int RING = kRing;               // steps on their way
     static constexpr int LOADS = D == 128 ? 5 : 3;   // load instructions of a step
     static constexpr int CODES = 32 * D, SLOT = CODES + 256;     // bytes of a step's codes; of its place in LDS
@@ -781,15 +735,6 @@ struct Sweep : Rows<D, F32, NT, PT> {
             const float ks = scale_of(K.ks[u]);
 #pragma unroll
             for (int t = 0; t < NT; ++t) st[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if constexpr (R::MX) {
-                const typename R::i32x8 a{(int)K.k[u][0], (int)K.k[u][1], (int)K.k[u][2], (int)K.k[u][3], 0, 0, 0, 0};
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    st[t][u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, qx[t][1], st[t][u], 4, 0, 0, (int)K.ks[u], 1, qs[t]);
-                    st[t][u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, qx[t][0], st[t][u], 4, 0, 0, (int)K.ks[u], 0, qs[t]);
-                }
-                continue;
-            }
 #pragma unroll
             for (int y = 0; y < KS; ++y) {
                 const bf16x8 a = __builtin_bit_cast(bf16x8, u32x4{fp4_pair(K.k[u][y], ks, 0), fp4_pair(K.k[u][y], ks, 1),
@@ -847,16 +792,11 @@ struct Sweep : Rows<D, F32, NT, PT> {
             }
         // The queries are there from here on: a wait for them within the loop would be one for the keys on their way too, step by step.
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            if constexpr (R::MX) {
-                asm volatile("" : "+v"(qx[t][0]), "+v"(qx[t][1]), "+v"(qs[t]));
-                continue;
-            }
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int y = 0; y < KS; ++y)
 #pragma unroll
                 for (int z = 0; z < QT; ++z) asm volatile("" : "+v"(q[t][y][z]));
-        }
         int x = 0;
         Pages next = early.at[RING];                             // (asked for a step before they are needed)
         Kept later = kept_at(w, first);

@@ -262,7 +262,6 @@ class Case:
         if spread:                                     # channels of all sizes
             q *= np.exp2(rng.integers(-spread, 1, q.shape).astype(float))
         self.q, self.qh = rows_on_gpu(q, dtype, layout, pad=1)
-        self.spread = spread
         self.there = np.ones((B, reach), bool)
         self.q_len = None if q_len is None else np.asarray(q_len, np.int32)
         self.keep = keep
@@ -293,11 +292,6 @@ class Case:
             want, wl_, size, score = ref.attend(self.qh[b], self.K[b], self.V[b], self.there[b], n, nq, self.scale,
                                                 None if self.keep is None else self.keep[b, :self.K.shape[1]])
             assert (out[b, nq:] == 7).all() and (lse[b, :, nq:] == 7).all(), f"sample {b}: rows behind the last were written"
-            if self.spread and self.dtype == BF16 and self.d == 128:
-                # a channel below 2^-14 of its row's largest is off by 2^-22 of that at most: so much times |k| more per score, where
-                # attend_bounds counts (d + 4) 2^-24 of sum |q||k|
-                most = np.abs(self.qh[b]).max(-1) * self.scale * np.abs(self.K[b]).sum(-1).max()
-                score = score + most * 2.0 ** -22 / ((self.d + 4) * 2.0 ** -24)
             bound, lbound = ref.attend_bounds(want, wl_, size, score, self.d, n, step, part)
             got = out[b, :nq]
             assert np.array_equal(np.isnan(got), np.isnan(want[:nq])), f"sample {b}: NaN"
@@ -369,6 +363,29 @@ def test_attend(i):
     c.check(out, lse)
     again, lse2 = c.call(md)
     assert np.array_equal(out, again) and np.array_equal(lse, lse2)             # the same bits
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_are_exact_where_fp32_sums_are(d, dtype):
+    """Integers whose products and partial sums stay below 2^24 have the same sum in fp32 in any order: a row that sees one key has its score
+    as lse but for six roundings of 2^-24 each (log2(e), its product with the scale, that with the score, the sum with log2 of a sum near 1, ln 2, its
+    product) and a unit each of exp2 and log2 near 1, 2^-22 together."""
+    rng = np.random.default_rng(d)
+    c = Case(5, [1] * 40, 1, 8, 4, d, 16, dtype)
+    q = rng.integers(-127, 128, c.qh.shape) * np.exp2(rng.integers(0, 3, c.qh.shape))
+    q[..., rng.integers(0, d)] = 2.0 ** 14                       # a product of 12 * 2^14 beside sums of many small ones
+    c.q, c.qh = rows_on_gpu(q, dtype)
+    assert np.array_equal(c.qh, q)
+    for b in range(40):
+        for h in range(4):
+            k = rng.integers(-12, 13, d).astype(float)
+            ref.put(c.pool, int(c.table[b, 0]) * 16, h, k, k, 16)
+            c.K[b, 0, h] = ref.values(*ref.quantise(k))
+    assert np.array_equal(c.K[:, 0], np.round(c.K[:, 0] * 4) / 4) and (np.abs(c.K[:, 0]).max() * np.abs(q)).sum(-1).max() * 4 < 2 ** 24
+    _, lse = c.call(__import__("paper_2411_10803_amd"))
+    want = np.einsum("bhd,bhd->bh", c.qh[:, 0], np.repeat(c.K[:, 0], 2, axis=1)) * np.float64(np.float32(c.scale))
+    assert (np.abs(lse[:, :, 0] - want) <= 6 * 2.0 ** -24 * np.abs(want) + 2.0 ** -22).all()
 
 
 def test_attend_over_lengths_out_of_range_and_bad_pages():
