@@ -441,6 +441,14 @@ def _here(stream, *tensors) -> int:
     return torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
 
 
+def _made_on(stream):
+    """What a call makes for itself is made on the stream that it runs on: memory of another one could be in use there until the
+    call's own stream writes it, or be given away while that still reads it."""
+    import contextlib
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def _pool(cache, d):
     """(pages, heads, tokens of a page) of a cache held in 4 bits, uint8 [n_pages, H, page * (d + d / 16)]."""
     import torch
@@ -512,7 +520,8 @@ def mustdrop_cache4_pages(new_len, length, table, free_pages, n_free, missing, p
     _shaped("slots", slots, (B, N))
     raw = _here(stream, new_len, length, table, free_pages, n_free, missing, slots, workspace)
     if workspace is None:
-        workspace = cache4_pages_workspace(B, table.device)
+        with _made_on(stream):
+            workspace = cache4_pages_workspace(B, table.device)
     _call("mustdrop_cache4_pages",
         _ptr(new_len), _ptr(length), _ptr(table), _ptr(free_pages), _ptr(n_free), _ptr(slots), _ptr(missing),
         B, max_pages, free_pages.shape[0], int(page), N,
@@ -564,7 +573,8 @@ def mustdrop_cache4_attend(q, cache, table, length, softmax_scale, out=None, lse
     n_pages, H, page = _pool(cache, d)
     max_pages = table.shape[-1]
     if out is None:
-        out = torch.zeros((B, N, Hq, d), dtype=q.dtype, device=q.device)
+        with _made_on(stream):
+            out = torch.zeros((B, N, Hq, d), dtype=q.dtype, device=q.device)
     _typed(torch.int32, table=table, length=length, q_len=q_len)
     if lse is not None:
         _typed(torch.float32, lse=lse)
@@ -579,7 +589,8 @@ def mustdrop_cache4_attend(q, cache, table, length, softmax_scale, out=None, lse
     _shaped("q_len", q_len, (B,))
     raw = _here(stream, q, cache, table, length, out, lse, q_len, keep, workspace)
     if workspace is None:
-        workspace = cache4_workspace(q, cache, table)
+        with _made_on(stream):
+            workspace = cache4_workspace(q, cache, table)
     qp, lq = _rows(q, "q")
     op, lo = _rows(out, "out")
     _call("mustdrop_cache4_attend",

@@ -8,7 +8,8 @@
 //   cache4_pages_kernel, cache4_slots_kernel   lengths -> pages taken and released, table entries, slots
 //   cache4_write_kernel                        rows -> codes and scales, at their slots
 //   cache4_read_kernel                         pages -> rows
-//   cache4_attend_kernel                       softmax(scale Q K^T) V over the pages
+//   cache4_attend_kernel                       softmax(scale Q K^T) V over the pages, a block per tile of query rows
+//   cache4_attend_runs_kernel, cache4_join_*   the same in runs of equal work, whose parts are added up behind
 #include "md_device.hpp"
 #include "md_host.hpp"
 #include "cache4_plan.hpp"
@@ -22,8 +23,6 @@ constexpr float kLog2eC = 1.4426950408889634f, kLn2C = 0.6931471805599453f;
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 struct Pool {
@@ -328,7 +327,7 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(
 // ------------------------------------------------------------------------------------------------ attention
 
 constexpr int kRing = 2;                         // steps that a wave of the attention has on their way
-struct AttendDims { int B, N, G, tiles; };           // G: query heads of a K/V head; tiles: of query rows, in the longest case
+struct AttendDims { int B, N, G, tiles; };       // G: query heads of a K/V head; tiles: of query rows, in the longest case
 
 struct AttendArgs {
     const void* q;
@@ -1175,8 +1174,8 @@ int check_dtype(const char* who, int dtype) {
     return dtype == MD_F32 || dtype == MD_BF16 ? MD_OK : fail(MD_EDTYPE, "%s: unknown dtype %d", who, dtype);
 }
 
-constexpr long kMaxGrid = 0x7FFFFFFFl;
-constexpr long kMaxRows = (1l << 28) - 16;            // 16 threads per row, and a launch has fewer than 2^32 along x
+// A launch has fewer than 2^32 threads along x: of the copies 16 per row, of the attention up to 512 per tile of query rows.
+constexpr long kMaxRows = (1l << 28) - 16, kMaxUnits = (1l << 23) - 1;
 
 struct Range { const void* p; size_t n; };
 // None of the first `outs` ranges may share a byte with any other range.
@@ -1345,7 +1344,7 @@ int attend_impl(const void* q, int dtype, const void* cache, const int32_t* tabl
     if ((long)N * G > 0x7FFFFFFFl - 128) return fail(MD_ESHAPE, "cache4_attend: too many query rows");
     const AttendPlan plan = attend_plan(workspace, dtype == MD_F32, B, N, Hq, d, p);
     const long units = (long)B * H * plan.cut.tiles, rows = (long)B * Hq * N;
-    if (units > kMaxGrid / 2 || rows > kMaxGrid) return fail(MD_ESHAPE, "cache4_attend: too many query rows");
+    if (units > kMaxUnits) return fail(MD_ESHAPE, "cache4_attend: %ld tiles of query rows are too many for one call", units);
     const size_t need = attend_bytes(B, N, Hq, H, d, max_pages, page);
     const Range r[] = {{out, rows_bytes(ol, B, N, Hq, d, dtype)}, {lse, lse ? (size_t)B * Hq * N * 4 : 0}, {workspace, workspace ? need : 0},
                        {q, rows_bytes(ql, B, N, Hq, d, dtype)}, {cache, pool_bytes(p)}, {table, (size_t)B * max_pages * 4}, {len, (size_t)B * 4},
@@ -1356,7 +1355,8 @@ int attend_impl(const void* q, int dtype, const void* cache, const int32_t* tabl
         return fail(MD_EWORKSPACE, "cache4_attend: workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(MD_EALIGN, "cache4_attend: workspace must be 256-byte aligned");
     const AttendArgs A{q, static_cast<const uint8_t*>(cache), table, len, q_len, keep, out, lse, p, AttendDims{B, N, G, plan.cut.tiles}, softmax_scale, ql, ol};
-    // a pool beyond half of the 256 MB Infinity Cache is streamed (64 x up to 4096 keys, 32 heads: 128 us, 141 with plain loads)
+    // a pool beyond half of the 256 MB Infinity Cache is streamed.  us so / with plain loads: 64 x up to 4096 keys, 32 heads (680 MB) 120 / 130,
+    // 16 x 4096 (300 MB) 53 / 58, 4 x 4096 (75 MB) 25.8 / 25.3
     const bool stream_once = pool_bytes(p) > (size_t)128 << 20;
     hipStream_t st = static_cast<hipStream_t>(stream);
 #define MD_C4_ATTEND(D_, F_, NT_, S_, PT_)                                                                                                  \

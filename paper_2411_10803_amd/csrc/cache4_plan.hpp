@@ -83,15 +83,16 @@ MD_PLAN_FN int c4_part_place(int p, int unit_begin, int total, int runs) { retur
 //   tile_rows  query rows of a unit.  Of the G query heads of a K/V head and the N tokens, sixteen fill a matrix tile.  Two tiles to a
 //              unit convert each key once for 32 rows instead of 16, but leave half as many units and three blocks to a CU instead of four:
 //              they pay from about two units per CU on.  us with 16 / 32 rows: 4 x 512 tokens of 32 heads on 8, up to 5888 keys
-//              317 / 222, 16 x 128 of 32 heads, 704 keys 77 / 57, 1 x 512 of 32 heads on 8, 6000 keys 119 / 89; 1 x 128 of 32 heads on 8,
-//              1000 keys (256 units) 13.2 / 16.2, 1 x 64 of 32 heads, 4000 keys (128) 41 / 50, 16 x 5 of 32 heads on 8, 2000 keys 26 / 29
+//              322 / 194, 16 x 128 of 32 heads, 704 keys 71 / 56, 1 x 512 of 32 heads on 8, 6000 keys 116 / 84, 1 x 320, 2000 keys (640
+//              units of 16) 35 / 32; 1 x 128, 1000 keys (256) 10.9 / 14.6, 1 x 64 of 32 heads, 4000 keys (128) 26 / 32
 //   runs       blocks of equal work, joined by a second kernel, instead of a block per unit.  Where there are few units, a block of
-//              eight waves takes 4.5 us + 0.165 us per 32 keys, the runs take 13 us and have all CUs; where sequences may be very
-//              long, one of them among short ones must not be left to one block.  us, a block per unit / runs: 8 units of 4000 keys 24 /
-//              16, of 16000 86 / 17, 32 units of 640 7.5 / 11, of 2000 16 / 16, of 4000 26 / 20, 128 of 4000 29 / 25, 256 of 2000 20 / 25, 512 of
-//              4000 55 / 64; 16 units of up to 100000 keys 473 / 46
-//   waves      of a block per unit: eight (four: 64 sequences of up to 4096 keys and 32 heads 124 us instead of 119, 32 units of 2000 keys
-//              22 instead of 16); four where a wave takes more registers, where a unit has no more than eight steps, and where there
+//              eight waves takes 4.5 us + 0.15 us per 32 keys, the runs take 12 us and more with their work, and have all CUs; where
+//              sequences may be very long, one of them among short ones must not be left to one block.  us, a block per unit / runs: 8
+//              units of 3200 keys 19 / 12, of 16000 77 / 17, 32 of 640 7.4 / 11, of 2000 14.6 / 16.7, of 2560 16.6 / 14.8, of 4000 24 / 19,
+//              128 of 3200 21 / 22, of 4000 26 to 30 / 24, 160 of 4000 26 / 30, 256 of 2000 18 / 24, 512 of 4000 51 / 60; 16 units of up to
+//              100000 keys 458 / 45
+//   waves      of a block per unit: eight (four: 64 sequences of up to 4000 keys and 32 heads 122 us instead of 117, 32 units of 2000 keys
+//              17.8 instead of 14.6); four where a wave takes more registers, where a unit has no more than eight steps, and where there
 //              are more units than the 512 blocks of eight waves that run at a time and no long ones.  us with four / eight: units of up
 //              to 1000 keys in tables of 2000, 640 of them 20.5 / 22.0, 1024 24 / 27.5, 2048 38 / 45.5, 512 16.6 / 16.9, 256 12.8 / 11.7; of up
 //              to 300 in 600, 2048 22 / 30; of d = 64, 1000 in 2000, 2048 29 / 36; 1024 of up to 2000 in 4000 41 / 38

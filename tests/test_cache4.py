@@ -183,6 +183,8 @@ def test_attend_refusals(lib):
     assert attend(lib, ws=C.c_void_p(P(9).value + 16)) == EALIGN
     assert attend(lib, ql=layout(3 * 1024, 1024, 4)) == EINVAL and attend(lib, ol=layout(512, 1024, 128)) == ESHAPE
     assert attend(lib, N=1 << 30, Hq=8, H=1) == ESHAPE
+    assert attend(lib, B=1 << 21, N=1, Hq=4, H=4, ql=layout(512, 512, 128), ol=layout(512, 512, 128)) == ESHAPE   # 2^23 tiles: 2^32 threads
+    assert b"tiles" in lib.mustdrop_last_error()
     size = lib.mustdrop_cache4_attend_workspace_bytes
     need = size(2, 3, 8, 4, 128, 6, 32)
     assert need > 0 and need % 256 == 0 and attend(lib, wsb=C.c_size_t(need - 1)) == EWORKSPACE

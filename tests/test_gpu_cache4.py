@@ -613,3 +613,23 @@ def test_a_given_stream_is_used():
     torch.cuda.synchronize()
     out, lse = c.call(md, stream=s)
     c.check(out, lse)
+
+
+def test_what_a_call_makes_belongs_to_its_stream():
+    """The workspace and `out` of a call on a given stream, which the call makes: the current stream may not get that memory while the call runs."""
+    import torch
+    import paper_2411_10803_amd as md
+    c = Case(22, [3000, 1700], 1, 4, 2, 128, 32, BF16, entries=600)              # in runs: with sums in the workspace
+    args = [c.q, dev(c.pool), dev(c.table), dev(np.asarray(c.lengths, np.int32)), c.scale]
+    want = md.mustdrop_cache4_attend(*args)
+    size = md.cache4_workspace(args[0], args[1], args[2]).numel()
+    s = torch.cuda.Stream()
+    busy = torch.ones(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(8):
+            busy @ busy
+    out = md.mustdrop_cache4_attend(*args, stream=s)
+    over = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)] + [torch.full_like(want, 9) for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and len(over) == 8
