@@ -1057,14 +1057,9 @@ __device__ __forceinline__ void add_parts(const Parts& parts, const Cut& c, int 
         const int p = x0 + lane * stride;
         const bool on = p <= c.p1;
         const float2 ml = on ? parts.ml[(long)c4_part_place(p, c.begin, c.total, c.runs) * tile_rows + row] : float2{kNoKey, 0.f};
-        const float top = fmaxf(m, wave_max(ml.x)), a = fast_exp2(m - top), e = on ? fast_exp2(ml.x - top) : 0.f;
-        l = l * a + wave_sum(ml.y * e);
-        m = top;
-#pragma unroll
-        for (int j = 0; j < C; ++j) acc[j] *= a;
         const int n = min(kWave, (c.p1 - x0) / stride + 1);
-        for (int y0 = 0; y0 < n; y0 += 8) {
-            float v[8][C];
+        float v[8][C];
+        const auto ask = [&](int y0) {
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
                 const int q = x0 + min(y0 + y, n - 1) * stride;
@@ -1072,6 +1067,15 @@ __device__ __forceinline__ void add_parts(const Parts& parts, const Cut& c, int 
 #pragma unroll
                 for (int j = 0; j < C; ++j) v[y][j] = from[j];
             }
+        };
+        ask(0);                                      // (on their way while the weights come and are worked out)
+        const float top = fmaxf(m, wave_max(ml.x)), a = fast_exp2(m - top), e = on ? fast_exp2(ml.x - top) : 0.f;
+        l = l * a + wave_sum(ml.y * e);
+        m = top;
+#pragma unroll
+        for (int j = 0; j < C; ++j) acc[j] *= a;
+        for (int y0 = 0; y0 < n; y0 += 8) {
+            if (y0) ask(y0);
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
                 const float f = y0 + y < n ? lane_bcast_f(e, y0 + y) : 0.f;
@@ -1359,11 +1363,14 @@ int attend_impl(const void* q, int dtype, const void* cache, const int32_t* tabl
     // 16 x 4096 (300 MB) 53 / 58, 4 x 4096 (75 MB) 25.8 / 25.3
     const bool stream_once = pool_bytes(p) > (size_t)128 << 20;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    // A wave of a row's join adds up about eight parts, which are on their way together.  us with 4 / 8 / 16 waves: 128 parts to a unit 9.1 / 7.0 /
+    // 6.6, 64 parts 7.3 / 6.3 / 6.4, 32 parts 4.7 / 5.1 / 6.4, 512 rows of 32 parts 5.4 / 6.5 / 11.6, 400 rows of 13 5.2 / 5.2 / 10.7
+    const int joiners = c4_clamp((int)(kC4Blocks / units / 8), 4, 16);
 #define MD_C4_ATTEND(D_, F_, NT_, S_, PT_)                                                                                                  \
     do {                                                                                                                                  \
         if (plan.cut.runs) {                                                                                                              \
             MD_LAUNCH("cache4_attend_runs", st, (cache4_attend_runs_kernel<D_, F_, NT_, S_, PT_>), kC4Blocks, 256, plan.lds, A, plan.parts); \
-            if (rows <= 2048) MD_LAUNCH("cache4_join", st, (cache4_join_kernel<D_, F_>), (int)rows, rows <= 512 ? 1024 : 256, 0, A, plan.parts, 16 * NT_); \
+            if (rows <= 2048) MD_LAUNCH("cache4_join", st, (cache4_join_kernel<D_, F_>), (int)rows, joiners * 64, 0, A, plan.parts, 16 * NT_);         \
             else MD_LAUNCH("cache4_join", st, (cache4_join_tiles_kernel<D_, F_>), (int)(units * NT_), 256, 0, A, plan.parts, 16 * NT_);      \
         } else {                                                                                                                          \
             MD_LAUNCH("cache4_attend", st, (cache4_attend_kernel<D_, F_, NT_, S_, PT_>), (int)units, plan.cut.waves * 64, plan.lds, A);      \
