@@ -87,10 +87,11 @@ MD_PLAN_FN int c4_part_place(int p, int unit_begin, int total, int runs) { retur
 //              units of 16) 35 / 32; 1 x 128, 1000 keys (256) 10.9 / 14.6, 1 x 64 of 32 heads, 4000 keys (128) 26 / 32
 //   runs       blocks of equal work, joined by a second kernel, instead of a block per unit.  Where there are few units, a block of
 //              eight waves takes 4.5 us + 0.15 us per 32 keys, the runs take 12 us and more with their work, and have all CUs; where
-//              sequences may be very long, one of them among short ones must not be left to one block.  us, a block per unit / runs: 8
-//              units of 3200 keys 19 / 12, of 16000 77 / 17, 32 of 640 7.4 / 11, of 2000 14.6 / 16.7, of 2560 16.6 / 14.8, of 4000 24 / 19,
-//              128 of 3200 21 / 22, of 4000 26 to 30 / 24, 160 of 4000 26 / 30, 256 of 2000 18 / 24, 512 of 4000 51 / 60; 16 units of up to
-//              100000 keys 458 / 45
+//              sequences may be very long, one of them among short ones must not be left to one block.  Lengths are often well
+//              below the tables' capacity, which is all that the host knows.  us, a block per unit / runs: 8 units of 3200 keys 19 / 12, of
+//              16000 78 / 16, 32 of 640 7.4 / 10, of 2000 14.7 / 14.8, of 2560 16.7 / 12.9, of 4000 24 / 17, of 1000 in tables of 4096 9.6 /
+//              10.5, 128 of 2560 18 / 23, of 4000 25 / 23, of up to 2000 in tables of 4096 15 / 20, 160 of 6000 40 / 38, of 9000 52 / 48, 256 of
+//              2000 18 / 23, 512 of 4000 53 / 58; 16 units of up to 100000 keys 458 / 45
 //   waves      of a block per unit: eight (four: 64 sequences of up to 4000 keys and 32 heads 122 us instead of 117, 32 units of 2000 keys
 //              17.8 instead of 14.6); four where a wave takes more registers, where a unit has no more than eight steps, and where there
 //              are more units than the 512 blocks of eight waves that run at a time and no long ones.  us with four / eight: units of up
