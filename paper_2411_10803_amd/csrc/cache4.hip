@@ -706,7 +706,7 @@ struct Sweep : Rows<D, F32, NT, PT> {
         const uint32_t at = (uint32_t)(uintptr_t)(lds_ptr_t)const_cast<char*>(slot);
         if constexpr (D == 128) {
             u32x4 k0, k1, v0, v1;
-            asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:1024\n\tds_read_b128 %2, %8 offset:2048\n\tds_read_b128 %3, %8 offset:3072\n\t"
+            asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:1024\n\tds_read_b128 %2, %8 offset:2*1024\n\tds_read_b128 %3, %8 offset:3*1024\n\t"
                          "ds_read_u8 %4, %9 offset:4096\n\tds_read_u8 %5, %9 offset:4160\n\tds_read_b32 %6, %10 offset:4224\n\tds_read_b32 %7, %10 offset:4288\n\t"
                          "s_waitcnt lgkmcnt(0)"
                          : "=&v"(k0), "=&v"(k1), "=&v"(v0), "=&v"(v1), "=&v"(r.ks[0]), "=&v"(r.ks[1]), "=&v"(r.vs[0]), "=&v"(r.vs[1])

@@ -547,11 +547,12 @@ def test_prefill_to_cache_to_decode_to_eviction():
         assert np.array_equal(host(dense["k"])[b, :n], K(b)[left]) and np.array_equal(host(dense["v"])[b, :n], V(b)[left])
 
 
-def test_decode_step_in_a_graph():
+@pytest.mark.parametrize("entries", [8, 800])                                    # of a block table; 800: attention in runs
+def test_decode_step_in_a_graph(entries):
     """Pages, rows and attention of a step in one graph, replayed with eager steps of a second program between; both agree bit for bit."""
     import torch
     import paper_2411_10803_amd as md
-    B, H, Hq, d, page, entries = 5, 2, 8, 128, 16, 8
+    B, H, Hq, d, page = 5, 2, 8, 128, 16
     made = [decode_program(md, torch, B, H, Hq, d, page, 0, 0, entries, 1) for _ in range(2)]
     k, v = (torch.zeros((B, 1, H, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
     q = torch.zeros((B, 1, Hq, d), dtype=torch.bfloat16, device="cuda")
@@ -577,6 +578,33 @@ def test_decode_step_in_a_graph():
         for name in ("cache", "table", "length", "free", "n_free", "missing", "slots", "out", "lse"):
             assert torch.equal(made[0][0][name], made[1][0][name]), (n, name)
     assert host(made[0][0]["length"]).tolist() == [41] * B
+
+
+def test_two_graphs_with_one_workspace():
+    """What a call leaves in its workspace is nobody's: two graphs that take turns on one give what eager calls give, replay after replay."""
+    import torch
+    import paper_2411_10803_amd as md
+    cases = [Case(31, [2000, 900], 1, 4, 2, 128, 32, BF16, entries=600), Case(32, [70, 4000], 2, 4, 2, 128, 32, BF16, entries=600)]
+    args = [[c.q, dev(c.pool), dev(c.table), dev(np.asarray(c.lengths, np.int32)), c.scale] for c in cases]
+    ws = max((md.cache4_workspace(a[0], a[1], a[2]) for a in args), key=lambda w: w.numel())
+    want = [md.mustdrop_cache4_attend(*a) for a in args]
+    out = [torch.zeros_like(w) for w in want]
+    graphs = []
+    for a, o in zip(args, out):
+        md.mustdrop_cache4_attend(*a, out=o, workspace=ws)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            md.mustdrop_cache4_attend(*a, out=o, workspace=ws)
+    for n in range(5):
+        for o in out:
+            o.fill_(9)
+        ws.fill_(255)
+        graphs[n % 2].replay()
+        graphs[1 - n % 2].replay()
+        md.mustdrop_cache4_attend(*args[0], workspace=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1]), n
 
 
 def test_two_programs_on_two_streams():
