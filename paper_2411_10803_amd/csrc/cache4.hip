@@ -71,7 +71,7 @@ __global__ __launch_bounds__(1024) void cache4_pages_kernel(
     __shared__ int s_red[16], s_before[1024];
     __shared__ PagePlan s_plan[1024];
     const int tid = threadIdx.x, top = c4_clamp(n_free[0], 0, n_pages);
-    int leave = 0, come = 0;                         // (the host checks that B * max_pages fits 31 bits)
+    int leave = 0, come = 0;                         // (the host checks that B * max_pages + n_pages fits 31 bits)
     for (int b = tid; b < B; b += 1024) {
         const C4Change c = c4_change(len[b], new_len[b], max_pages, page_shift);
         if (c.held > c.need) leave += c.held - c.need;
@@ -1199,7 +1199,9 @@ int pages_impl(const int32_t* new_len, int32_t* len, int32_t* table, int32_t* fr
     if (rc != MD_OK) return rc;
     if (B <= 0 || N < 0) return fail(MD_EINVAL, "cache4_pages: B must be positive and N not negative");
     if (B > 65535) return fail(MD_ESHAPE, "cache4_pages: B=%d out of range", B);
-    if ((long)B * max_pages > 0x7FFFFFFFl) return fail(MD_ESHAPE, "cache4_pages: a table of %d x %d entries is too large", B, max_pages);
+    // (places of the stack are counted in 31 bits, beyond its height by all that the tables could release, and the kernel looks 4096 ahead)
+    if ((long)B * max_pages + n_pages > 0x7FFFFFFFl - 8192)
+        return fail(MD_ESHAPE, "cache4_pages: a table of %d x %d entries and %d pages are too many", B, max_pages, n_pages);
     if (!new_len || !len || !table || !free_pages || !n_free || !missing || (N > 0 && !slots))
         return fail(MD_EINVAL, "cache4_pages: null pointer among the required arguments");
     if (!slots) N = 0;

@@ -107,6 +107,7 @@ def test_pages_refusals(lib):
     assert pages(lib, n_pages=1 << 27, page=16) == ESHAPE                        # 2^31 slots
     assert pages(lib, max_pages=(1 << 30) // 32) == ESHAPE                       # 2^30 entries per request
     assert pages(lib, B=65535, max_pages=40000) == ESHAPE                        # a table of more than 2^31 entries
+    assert pages(lib, B=1024, max_pages=(1 << 21) - 9, n_pages=1 << 24) == ESHAPE     # places of the stack beyond 31 bits
     assert pages(lib, len=P(1)) == EALIAS and pages(lib, free=P(3)) == EALIAS and pages(lib, ws=P(3)) == EALIAS
     assert pages(lib, slots=P(7)) == EALIAS
     assert pages(lib, ws=None) == EWORKSPACE and pages(lib, wsb=C.c_size_t(8)) == EWORKSPACE
