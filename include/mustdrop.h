@@ -374,7 +374,7 @@ size_t mustdrop_cache4_bytes(int n_pages, int page, int H, int d);      /* 0 for
  *   slots    [B, N]: slots of the new entries, slots[b][i] that of entry len[b] + i (len as it was), -1 from new_len[b] on; NULL if N = 0
  *   missing  [1]: pages that the pool is short of.  If not 0, nothing else is changed, and the slots are all -1.
  * One page per entry of the stack and the tables: a page named twice is handed out twice.  Errors: MD_EINVAL, MD_ESHAPE
- * (limits, B > 65535, B * max_pages + n_pages > 2^31 - 8193), MD_EALIAS, MD_EALIGN, MD_EWORKSPACE, MD_EHIP. */
+ * (limits, B > 65535, N > 2^30, B * max_pages + n_pages > 2^31 - 8193), MD_EALIAS, MD_EALIGN, MD_EWORKSPACE, MD_EHIP. */
 size_t mustdrop_cache4_pages_workspace_bytes(int B);
 
 int mustdrop_cache4_pages(

@@ -49,9 +49,9 @@ __device__ __forceinline__ int owner_of(const int* before, int x) {
 }
 
 __device__ __forceinline__ void write_slot(const PagePlan& p, int i, const int32_t* row, const int32_t* free_pages, int n_pages, int page_shift, int32_t* slot) {
-    const int at = p.old_len + i;
     int s = -1;
-    if (at < p.new_len) {
+    if (i < p.new_len - p.old_len) {
+        const int at = p.old_len + i;
         const int e = at >> page_shift, held = c4_pages_of(p.old_len, page_shift), j = p.first - (e - held);
         const int id = c4_page_id(e < held ? row[e] : (j >= 0 && j < n_pages ? free_pages[j] : -1), n_pages);
         if (id >= 0) s = (int)(((uint32_t)id << page_shift) + (at & ((1 << page_shift) - 1)));
@@ -1198,7 +1198,7 @@ int pages_impl(const int32_t* new_len, int32_t* len, int32_t* table, int32_t* fr
     int rc = check_pool("cache4_pages", 1, 64, n_pages, page, max_pages, &p);
     if (rc != MD_OK) return rc;
     if (B <= 0 || N < 0) return fail(MD_EINVAL, "cache4_pages: B must be positive and N not negative");
-    if (B > 65535) return fail(MD_ESHAPE, "cache4_pages: B=%d out of range", B);
+    if (B > 65535 || N > (1 << 30)) return fail(MD_ESHAPE, "cache4_pages: B=%d or N=%d out of range", B, N);
     // (places of the stack are counted in 31 bits, beyond its height by all that the tables could release, and the kernel looks 4096 ahead)
     if ((long)B * max_pages + n_pages > 0x7FFFFFFFl - 8192)
         return fail(MD_ESHAPE, "cache4_pages: a table of %d x %d entries and %d pages are too many", B, max_pages, n_pages);

@@ -103,7 +103,7 @@ def test_pages_refusals(lib):
     assert pages(lib, N=-1) == EINVAL
     for page in (8, 24, 33, 512):
         assert pages(lib, page=page) == ESHAPE
-    assert pages(lib, B=65536) == ESHAPE
+    assert pages(lib, B=65536) == ESHAPE and pages(lib, B=1, N=(1 << 30) + 1) == ESHAPE
     assert pages(lib, n_pages=1 << 27, page=16) == ESHAPE                        # 2^31 slots
     assert pages(lib, max_pages=(1 << 30) // 32) == ESHAPE                       # 2^30 entries per request
     assert pages(lib, B=65535, max_pages=40000) == ESHAPE                        # a table of more than 2^31 entries
