@@ -509,10 +509,10 @@ __device__ __forceinline__ Kept kept_at(const Walk& w, int step) {
 // that a lane loads d/4 channels of one token: from the loads to the matrix products no lane needs another's data.
 // (The scaled 16x16x128 product would take K's codes and scales as they lie and a query as two e4m3 rows, a prompt's piece in 153 us instead of 164,
 // but its sums are not fp32 ones: lse was off 10 to 40 times as far.)
-// PT: bf16 parts of a probability in the product with V; two carry 16 bits, one is as coarse as a bf16 output.
-template <int D, bool F32, int NT, int PT>
+template <int D, bool F32, int NT>
 struct Rows {
     static constexpr int QT = F32 ? 3 : 1;           // bf16 parts of a query: fp32 has 24 bits
+    static constexpr int PT = F32 ? 3 : 2;           // of a probability in the product with V: in one part its rounding would be as large as the output's
     static constexpr int KS = D / 32;                // contraction steps of S
     static constexpr int J = D / 16;                 // 16-channel tiles of O
 
@@ -643,10 +643,10 @@ struct Rows {
 };
 
 // A wave that brings its own keys: steps of 32, straight from the pages.
-template <int D, bool F32, int NT, bool STREAM, int PT>
-struct Sweep : Rows<D, F32, NT, PT> {
-    typedef Rows<D, F32, NT, PT> R;
-    using R::KS; using R::J; using R::QT; using R::n; using R::lb; using R::q; using R::o;
+template <int D, bool F32, int NT, bool STREAM>
+struct Sweep : Rows<D, F32, NT> {
+    typedef Rows<D, F32, NT> R;
+    using R::KS; using R::J; using R::QT; using R::PT; using R::n; using R::lb; using R::q; using R::o;
     static constexpr int RING = kRing;               // steps on their way
     static constexpr int LOADS = D == 128 ? 5 : 3;   // load instructions of a step
     static constexpr int CODES = 32 * D, SLOT = CODES + 256;     // bytes of a step's codes; of its place in LDS
@@ -907,12 +907,12 @@ __device__ __forceinline__ int by_length(const AttendArgs& A, int at) {
 }
 
 // A block per tile of query rows of a (sample, K/V head); its waves take the steps in turn.
-template <int D, bool F32, int NT, bool STREAM, int PT>
+template <int D, bool F32, int NT, bool STREAM>
 __global__ __launch_bounds__(NT == 2 || (F32 && D == 128) ? 256 : 512, NT == 2 || (F32 && D == 128) ? 3 : 4) void cache4_attend_kernel(AttendArgs A0)
 {
     extern __shared__ f32x4 s_lds[];
     constexpr int ROWS = 16 * NT;
-    Sweep<D, F32, NT, STREAM, PT> sw;
+    Sweep<D, F32, NT, STREAM> sw;
     Walk w;
     Early early;
     int b;
@@ -1005,14 +1005,14 @@ __device__ __forceinline__ void each_unit(int tile_rows, int run, Each each) {
 
 // Few units, or units of unequal length: every block takes a run of as many steps, over the borders of units and samples.  A unit that
 // lies within a run is finished there, the parts of the others are joined by the next kernel.
-template <int D, bool F32, int NT, bool STREAM, int PT>
+template <int D, bool F32, int NT, bool STREAM>
 __global__ __launch_bounds__(256, NT == 2 || (F32 && D == 128) ? 3 : 4) void cache4_attend_runs_kernel(AttendArgs A0, Parts parts0)
 {
     extern __shared__ f32x4 s_lds[];
     constexpr int ROWS = 16 * NT;
     char* lds = reinterpret_cast<char*>(s_lds);
     each_unit(ROWS, blockIdx.x, [&](const AttendArgs& A, const Sample& s, int h, int r0, int first, int last, int place) {
-        Sweep<D, F32, NT, STREAM, PT> sw;
+        Sweep<D, F32, NT, STREAM> sw;
         Walk w = table_of(A, s.b);
         const Early early = early_pages(w, first + wave_id(), 4);
         sw.begin(A, s, h, r0);
@@ -1368,22 +1368,22 @@ int attend_impl(const void* q, int dtype, const void* cache, const int32_t* tabl
     // A wave of a row's join adds up about eight parts, which are on their way together.  us with 4 / 8 / 16 waves: 128 parts to a unit 9.1 / 7.0 /
     // 6.6, 64 parts 7.3 / 6.3 / 6.4, 32 parts 4.7 / 5.1 / 6.4, 512 rows of 32 parts 5.4 / 6.5 / 11.6, 400 rows of 13 5.2 / 5.2 / 10.7
     const int joiners = c4_clamp((int)(kC4Blocks / units / 8), 4, 16);
-#define MD_C4_ATTEND(D_, F_, NT_, S_, PT_)                                                                                                  \
+#define MD_C4_ATTEND(D_, F_, NT_, S_)                                                                                                     \
     do {                                                                                                                                  \
         if (plan.cut.runs) {                                                                                                              \
-            MD_LAUNCH("cache4_attend_runs", st, (cache4_attend_runs_kernel<D_, F_, NT_, S_, PT_>), kC4Blocks, 256, plan.lds, A, plan.parts); \
-            if (rows <= 2048) MD_LAUNCH("cache4_join", st, (cache4_join_kernel<D_, F_>), (int)rows, joiners * 64, 0, A, plan.parts, 16 * NT_);         \
-            else MD_LAUNCH("cache4_join", st, (cache4_join_tiles_kernel<D_, F_>), (int)(units * NT_), 256, 0, A, plan.parts, 16 * NT_);      \
+            MD_LAUNCH("cache4_attend_runs", st, (cache4_attend_runs_kernel<D_, F_, NT_, S_>), kC4Blocks, 256, plan.lds, A, plan.parts);   \
+            if (rows <= 2048) MD_LAUNCH("cache4_join", st, (cache4_join_kernel<D_, F_>), (int)rows, joiners * 64, 0, A, plan.parts, 16 * NT_);\
+            else MD_LAUNCH("cache4_join", st, (cache4_join_tiles_kernel<D_, F_>), (int)(units * NT_), 256, 0, A, plan.parts, 16 * NT_);   \
         } else {                                                                                                                          \
-            MD_LAUNCH("cache4_attend", st, (cache4_attend_kernel<D_, F_, NT_, S_, PT_>), (int)units, plan.cut.waves * 64, plan.lds, A);      \
+            MD_LAUNCH("cache4_attend", st, (cache4_attend_kernel<D_, F_, NT_, S_>), (int)units, plan.cut.waves * 64, plan.lds, A);        \
         }                                                                                                                                 \
     } while (0)
-#define MD_C4_ATTEND_S(D_, F_, NT_, PT_) do { if (stream_once) MD_C4_ATTEND(D_, F_, NT_, true, PT_); else MD_C4_ATTEND(D_, F_, NT_, false, PT_); } while (0)
-#define MD_C4_ATTEND_D(D_)                                                                                                                  \
+#define MD_C4_ATTEND_S(D_, F_, NT_) do { if (stream_once) MD_C4_ATTEND(D_, F_, NT_, true); else MD_C4_ATTEND(D_, F_, NT_, false); } while (0)
+#define MD_C4_ATTEND_D(D_)                                                                                                                \
     do {                                                                                                                                  \
-        if (dtype == MD_F32) MD_C4_ATTEND_S(D_, true, 1, 3);                                                                              \
-        else if (plan.cut.tile_rows == 16) MD_C4_ATTEND_S(D_, false, 1, 2);                                                               \
-        else MD_C4_ATTEND_S(D_, false, 2, 1);                                                                                             \
+        if (dtype == MD_F32) MD_C4_ATTEND_S(D_, true, 1);                                                                                 \
+        else if (plan.cut.tile_rows == 16) MD_C4_ATTEND_S(D_, false, 1);                                                                  \
+        else MD_C4_ATTEND_S(D_, false, 2);                                                                                                \
     } while (0)
     if (d == 128) MD_C4_ATTEND_D(128); else MD_C4_ATTEND_D(64);
 #undef MD_C4_ATTEND_D

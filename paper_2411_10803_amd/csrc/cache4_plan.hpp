@@ -82,9 +82,12 @@ MD_PLAN_FN int c4_part_place(int p, int unit_begin, int total, int runs) { retur
 // How a call of the attention is cut up: by what the host knows, which is the tables' capacity and not the samples' lengths.
 //   tile_rows  query rows of a unit.  Of the G query heads of a K/V head and the N tokens, sixteen fill a matrix tile.  Two tiles to a
 //              unit convert each key once for 32 rows instead of 16, but leave half as many units and three blocks to a CU instead of four:
-//              they pay from about two units per CU on.  us with 16 / 32 rows: 4 x 512 tokens of 32 heads on 8, up to 5888 keys
-//              322 / 194, 16 x 128 of 32 heads, 704 keys 71 / 56, 1 x 512 of 32 heads on 8, 6000 keys 116 / 84, 1 x 320, 2000 keys (640
-//              units of 16) 35 / 32; 1 x 128, 1000 keys (256) 10.9 / 14.6, 1 x 64 of 32 heads, 4000 keys (128) 26 / 32
+//              they pay from about three units per CU on, and from two to three it is one or the other.  us with 16 / 32 rows, by units of 16:
+//              4 x 512 tokens of 32 heads on 8, up to 5888 keys (4096) 313 / 233, 16 x 128 of 32 heads, 704 keys (4096) 72 / 63, 8 x 512 of 32
+//              heads, 512 keys (8192) 96 / 84, 1 x 512 of 32 heads on 8, 6000 keys (1024) 116 / 103; drafts of 4 tokens, 64 heads on 8, up to
+//              2000 keys, 128 of them (2048) 75 / 55, 64 (1024) 40 / 36; of 5 tokens, 32 heads on 4, 64 of them (768) 37 / 35; 1 x 320 of 32
+//              heads, 2000 keys (640) 36 / 38; 33 drafts of 4 tokens, 64 heads on 8 (528), up to 1000 keys 20.6 / 20.2, up to 4000 43 / 51;
+//              1 x 128, 1000 keys (256) 13 / 17, 1 x 64 of 32 heads, 4000 keys (128) 26 / 35
 //   runs       blocks of equal work, joined by a second kernel, instead of a block per unit.  Where there are few units, a block of
 //              eight waves takes 4.5 us + 0.15 us per 32 keys, the runs take 12 us and more with their work, and have all CUs; where
 //              sequences may be very long, one of them among short ones must not be left to one block.  Lengths are often well
