@@ -342,9 +342,11 @@ int mustdrop_decode_keep_strided(
  * Numbers.  32 consecutive channels of one token and head are 32 four-bit numbers (bit 3: sign, bits 0-2: index of the magnitude
  * among 0, 0.5, 1, 1.5, 2, 3, 4, 6) times one scale 2^e.  With a the largest magnitude of the 32 and k = floor(log2 a): e = k - 2,
  * or k - 1 where a >= 1.75 * 2^k (a is then rounded to 6 at most and not cut down to it), at least -100 and at most 125, and -100
- * where a = 0.  x becomes the nearest value to x / 2^e, of two as near the one of the even index.  The scale is the byte e + 127;
- * a group with an infinity or a NaN has 255 and all of it reads as NaN.  A value is off by at most a
- * fifth of the group's largest magnitude, and by at most a fifth of itself where it is no smaller than a quarter of that.
+ * where a = 0.  x becomes the nearest value to x / 2^e, of two as near the one of the even index, and 6 where it is more.  The scale
+ * is the byte e + 127; a group with an infinity or a NaN has 255 and all of it reads as NaN.  With 3.5 * 2^-100 <= a < 7 * 2^125
+ * (2.8e-30 to 2.9e38) a value is off by at most a fifth of a, and by at most a fifth of itself where it is no smaller than a / 4.
+ * Below, where e stays at -100, values are off by up to 2^-101, and those up to 2^-102 read as 0; above, where e stays at 125, what
+ * is beyond 6 * 2^125 reads as that (off by up to a quarter of itself), and the others are off by a fifth of a at most.
  *
  * Pool.  [n_pages, H] pieces of page * (d + d/16) bytes (mustdrop_cache4_bytes in all), each one after the other
  *   K codes [page, d/2] (channel 2i in the low half of byte i), K scales [page, d/32],

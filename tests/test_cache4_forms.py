@@ -1,11 +1,14 @@
-"""Which form of the attention over the cache held in 4 bits the cases of cache4_forms.py take, from csrc/cache4_plan.hpp compiled for the CPU."""
+"""The cache held in 4 bits without a GPU: which form of the attention the cases of cache4_forms.py take, from csrc/cache4_plan.hpp compiled for
+the CPU; and what include/mustdrop.h says of its numbers, on the 64-bit reference."""
 import os
 import shutil
 import subprocess
 
+import numpy as np
 import pytest
 
 import cache4_forms as forms
+import cache4_ref as ref
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -31,3 +34,35 @@ def test_many_rows_go_together(plan):
     assert [p["runs"] for p in got] == [0, 0, 1, 1, 0]
     fewer = dict(forms.MANY_ROWS[4], lengths=forms.MANY_ROWS[4]["lengths"][:32])
     assert plan([fewer])[0]["rows"] == 16                     # one sample less: sixteen rows at a time
+
+
+# ---- what the header says of a value's error, over all scales
+def groups(rng, n, low, high):
+    """[n, 32] with the largest magnitude between 2^low and 2^high, and what they are held as."""
+    x = rng.standard_normal((n, 32)) * np.exp2(rng.uniform(-6, 0, (n, 32)))
+    x *= np.exp2(rng.uniform(low, high, (n, 1))) / np.abs(x).max(-1, keepdims=True)
+    return x, ref.values(*ref.quantise(x)), np.abs(x).max(-1, keepdims=True)
+
+
+def test_errors_where_the_scale_follows_the_largest_magnitude():
+    low, high = np.log2(3.5) - 100, np.log2(7.0) + 125
+    rng = np.random.default_rng(0)
+    for a, b in ((low, high), (low, low + 3), (high - 3, high)):
+        x, y, most = groups(rng, 20000, a, b - 1e-9)
+        off = np.abs(y - x)
+        assert (off <= most / 5).all() and (off <= np.abs(x) / 5)[np.abs(x) >= most / 4].all()
+
+
+def test_errors_where_the_scale_ends():
+    rng = np.random.default_rng(1)
+    x, y, _ = groups(rng, 20000, -150, np.log2(3.5) - 100 - 1e-9)
+    assert (np.abs(y - x) <= 2.0 ** -101).all() and (y[np.abs(x) <= 2.0 ** -102] == 0).all()
+    assert (np.abs(y - x) > np.abs(x) / 5)[np.abs(x) >= np.abs(x).max(-1, keepdims=True) / 4].any()      # (no fifth here)
+    x, y, most = groups(rng, 20000, np.log2(7.0) + 125, 128 - 1e-9)
+    cut = np.abs(x) > 6 * 2.0 ** 125
+    assert (np.abs(y)[cut] == 6 * 2.0 ** 125).all() and (np.abs(y - x)[cut] <= np.abs(x)[cut] / 4).all()
+    assert (np.abs(y - x) <= most / 5)[~cut].all() and (np.abs(y - x) > most / 5).any()
+    # both ends: what the bound without a range would have promised
+    for top, off in ((3.38e38, 0.24), (6e-31, 0.3), (2.0 ** -103, 0.99)):
+        v = np.full(32, top)
+        assert np.abs(ref.values(*ref.quantise(v)) - v).max() > off * top
