@@ -354,9 +354,11 @@ int mustdrop_decode_keep_strided(
  *   V scales [page/4, d/32, 4].
  * Nothing in the pool needs clearing: what lies behind a sample's length is not used, whatever it holds.
  *
- * Block table.  table [B, max_pages] i32: entry e of sample b names the page of its entries e*page .. e*page + page-1; entries
- * behind ceil(len/page) are not read.  slot = page number * page + place in the page, i32; -1: none.  A page number outside the
- * pool names no page: its entries take no part in attention, its rows are not read out; a slot outside the pool is not written.
+ * Block table.  table [B, max_pages] i32: entry e of sample b names the page of its entries e*page .. e*page + page-1.  Entries
+ * from ceil(len/page) on may hold anything and change no result; calls may read them, and in the pages that they name, so all
+ * of the table has to be memory that can be read.  slot = page number * page + place in the page, i32; -1: none.  A page number
+ * outside the pool names no page: its entries take no part in attention, its rows are not read out; a slot outside the pool is
+ * not written.
  *
  * Limits of the cache4 calls: d in {64, 128}; page a power of two from 16 to 256; n_pages * page < 2^31,
  * max_pages * page < 2^30; a pool of at most 256 GiB; H <= 65535; rows in MD_BF16 or MD_F32, fewer than 2^28 - 15 of them

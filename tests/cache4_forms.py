@@ -9,3 +9,16 @@ MANY_ROWS = [
     dict(lengths=[(29 * b) % 80 for b in range(22)], N=20, Hq=13, H=13, d=128, page=256, dtype=BF16, entries=65),
     dict(lengths=[20 + (17 * b) % 60 for b in range(33)], N=4, Hq=64, H=8, d=128, page=16, dtype=BF16, entries=8),
 ]
+
+KINDS = ("few", "fp32", "many")                      # 16 bf16 rows, 16 fp32 rows, 32 bf16 rows together
+
+
+def form(kind, d, runs, page=16, **more):
+    """A small case of one form: by its rows, its channels, and blocks per unit or (in tables wide enough) runs."""
+    c = dict(lengths=[(29 * b) % 80 + (b > 0) for b in range(6)], N=3, Hq=4, H=2, dtype=F32 if kind == "fp32" else BF16)
+    if kind == "many":
+        c.update(lengths=[(29 * b) % 80 + (b > 0) for b in range(22)], N=60, Hq=8, H=2)
+    return dict(c, d=d, page=page, entries=(17408 if runs else 512) // page, **more)
+
+
+FORMS = [(kind, d, runs) for kind in KINDS for d in (64, 128) for runs in (0, 1)]

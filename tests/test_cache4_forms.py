@@ -36,6 +36,12 @@ def test_many_rows_go_together(plan):
     assert plan([fewer])[0]["rows"] == 16                     # one sample less: sixteen rows at a time
 
 
+@pytest.mark.parametrize("page", (16, 64, 256))
+def test_every_form_is_there(plan, page):
+    for (kind, d, runs), p in zip(forms.FORMS, plan([forms.form(*f, page=page) for f in forms.FORMS])):
+        assert (p["rows"], p["runs"]) == (32 if kind == "many" else 16, runs), (kind, d, runs)
+
+
 # ---- what the header says of a value's error, over all scales
 def groups(rng, n, low, high):
     """[n, 32] with the largest magnitude between 2^low and 2^high, and what they are held as."""

@@ -39,3 +39,23 @@ def test_probabilities_keep_16_bits_where_rows_go_together(i):
     import paper_2411_10803_amd as md
     c = Case(400 + i, **forms.MANY_ROWS[i], size=0.25, heavy=False)
     check(c, *c.call(md))
+
+
+@pytest.mark.parametrize("kind, d, runs", forms.FORMS)
+def test_entries_of_a_table_behind_the_length_change_nothing(kind, d, runs):
+    """They may name no page, other samples' pages, or pages whose rows are no numbers."""
+    import paper_2411_10803_amd as md
+    c = Case(500, **forms.form(kind, d, runs))
+    live = np.arange(c.table.shape[1]) < -(-np.asarray(c.lengths)[:, None] // c.page)
+    used = c.table[live]
+    spare = [p for p in range(len(c.pool)) if p not in set(used.tolist())]     # never written: all scales 255
+    assert spare and (c.pool[spare] == 255).all()
+    rng = np.random.default_rng(1)
+    shape, own = c.table.shape, c.table
+    results = []
+    for behind in (np.full(shape, -1), rng.choice(used, shape), rng.choice(spare, shape), rng.integers(-2 ** 31, 2 ** 31, shape)):
+        c.table = np.where(live, own, behind).astype(np.int32)
+        results.append(c.call(md))
+    check(c, *results[0])
+    for out, lse in results[1:]:
+        assert np.array_equal(out, results[0][0]) and np.array_equal(lse, results[0][1])
