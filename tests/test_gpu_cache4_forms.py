@@ -59,3 +59,104 @@ def test_entries_of_a_table_behind_the_length_change_nothing(kind, d, runs):
     check(c, *results[0])
     for out, lse in results[1:]:
         assert np.array_equal(out, results[0][0]) and np.array_equal(lse, results[0][1])
+
+
+# ------------------------------------------------------------------------------------------------ streams
+
+def busy_for_a_while(torch, stream, work):
+    """About 50 ms of products on the stream: what is put behind them there has not begun when the host has made its next calls."""
+    with torch.cuda.stream(stream):
+        for _ in range(40):
+            torch.mm(work, work, out=work)
+
+
+@pytest.mark.parametrize("name", ("pages", "write", "read", "attend", "attend runs"))
+def test_a_call_follows_what_its_stream_does_before(name):
+    """The inputs are made on the call's stream, behind 50 ms of other work, and nothing else is waited for: a call on any other stream, the current
+    one among them, would take the zeros that stand there until then."""
+    import torch
+    import paper_2411_10803_amd as md
+    c = Case(23, **forms.form("few", 128, int(name.endswith("runs"))))
+    H, d, page, B = c.H, c.d, c.page, c.B
+    table, length = dev(c.table), dev(np.asarray(c.lengths, np.int32))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rows = [torch.randn((B, 7, H, d), generator=g, device="cuda").bfloat16() for _ in range(2)]
+    slots = torch.arange(B * 7, dtype=torch.int32, device="cuda").view(B, 7)
+    entries, n_pages = 4, 4 * B
+
+    def pages(x, stream=None):
+        zero = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")  # noqa: E731
+        s = [zero(B), zero(B, entries) - 1, torch.arange(n_pages, dtype=torch.int32, device="cuda"), zero(1) + n_pages, zero(1) + 9, zero(B, 64)]
+        torch.cuda.current_stream().synchronize()
+        return s, lambda: md.mustdrop_cache4_pages(x, *s[:5], page, slots=s[5], stream=stream)
+
+    def write(x, stream=None):
+        cache = torch.zeros((n_pages, H, ref.page_bytes(page, d)), dtype=torch.uint8, device="cuda")
+        torch.cuda.current_stream().synchronize()
+        return [cache], lambda: md.mustdrop_cache4_write(x, rows[1], slots, cache, stream=stream)
+
+    def read(x, stream=None):
+        out = [torch.zeros((B, 80, H, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        torch.cuda.current_stream().synchronize()
+        return out, lambda: md.mustdrop_cache4_read(x, table, length, *out, stream=stream)
+
+    def attend(x, stream=None):
+        out, lse = torch.zeros_like(c.q, memory_format=torch.contiguous_format), torch.zeros((B, c.Hq, c.N), device="cuda")
+        torch.cuda.current_stream().synchronize()
+        return [out, lse], lambda: md.mustdrop_cache4_attend(c.q, x, table, length, c.scale, out=out, lse=lse, stream=stream)
+    make, true = {"pages": (pages, torch.tensor([(11 * b) % 64 for b in range(B)], dtype=torch.int32, device="cuda")), "write": (write, rows[0]),
+                  "read": (read, dev(c.pool)), "attend": (attend, dev(c.pool))}[name.split()[0]]
+    want, call = make(true)
+    call()
+    stale, call = make(torch.zeros_like(true))
+    call()
+    work = torch.eye(4096, device="cuda")
+    torch.mm(work, work, out=torch.empty_like(work))
+    s, other = torch.cuda.Stream(), torch.cuda.Stream()
+    x = torch.zeros_like(true)
+    torch.cuda.synchronize()
+    assert not all(torch.equal(a.nan_to_num(1e9) if a.is_floating_point() else a, b.nan_to_num(1e9) if b.is_floating_point() else b)
+                   for a, b in zip(want, stale))
+    with torch.cuda.stream(other):                   # (what the call itself makes, it makes on its own stream: not on this one)
+        got, call = make(x, stream=s)
+        busy_for_a_while(torch, s, work)
+        with torch.cuda.stream(s):
+            x.copy_(true)
+        call()
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b) or np.array_equal(host(a), host(b), equal_nan=True)
+
+
+def test_nobody_gets_the_memory_of_a_call_on_its_own_stream():
+    """What a call makes for itself on a given stream goes back to that stream: tensors made on the current one while the call has not begun
+    yet keep what is written into them."""
+    import torch
+    import paper_2411_10803_amd as md
+    c = Case(22, [3000, 1700], 1, 4, 2, 128, 32, BF16, entries=600)              # in runs: with sums in the workspace
+    args = [c.q, dev(c.pool), dev(c.table), dev(np.asarray(c.lengths, np.int32)), c.scale]
+    want = md.mustdrop_cache4_attend(*args)
+    size, pages_size = md.cache4_workspace(args[0], args[1], args[2]).numel(), md.cache4_pages_workspace(2).numel()
+    work = torch.eye(4096, device="cuda")
+    torch.mm(work, work, out=torch.empty_like(work))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    # (many samples: two launches, the first of which leaves the plan in its workspace)
+    B, entries = 2000, 2
+    state = [torch.full((B,), 20, **i32), torch.zeros(B, **i32), torch.full((B, entries), -1, **i32), torch.arange(B * entries, **i32),
+             torch.full((1,), B * entries, **i32), torch.zeros(1, **i32)]
+    slots = torch.zeros((B, 20), **i32)
+    pages_size = md.cache4_pages_workspace(B).numel()
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()                         # (what was given back before is gone: new tensors do not take it)
+    busy_for_a_while(torch, s, work)
+    out = md.mustdrop_cache4_attend(*args, stream=s)
+    md.mustdrop_cache4_pages(*state, 16, slots=slots, stream=s)
+    sizes = [size, pages_size, out.numel() * out.element_size()] * 6
+    over = [torch.full((n,), 170, dtype=torch.uint8, device="cuda") for n in sizes]
+    torch.cuda.synchronize()
+    for n, t in zip(sizes, over):
+        assert (t == 170).all(), n
+    assert torch.equal(out, want)
+    assert state[1].tolist() == [20] * B and int(state[4]) == 0 and int(state[5]) == 0
+    assert sorted(slots[:, ::16].flatten().tolist()) == list(range(0, 16 * B * entries, 16))
