@@ -42,6 +42,18 @@ def test_every_form_is_there(plan, page):
         assert (p["rows"], p["runs"]) == (32 if kind == "many" else 16, runs), (kind, d, runs)
 
 
+def test_joins_are_reached(plan):
+    for c, (rows, many) in zip(forms.JOINS, ((16, False), (16, True), (16, True), (32, True))):
+        p = plan([c])[0]
+        assert p["runs"] == 1 and p["rows"] == rows and (len(c["lengths"]) * c["Hq"] * c["N"] > 2048) == many, c
+    for dtype in (forms.BF16, forms.F32):
+        for d in (64, 128):
+            p = plan([dict(forms.LONG, dtype=dtype, d=d)])[0]
+            units, parts = len(forms.LONG["lengths"]), forms.parts_of(forms.LONG["lengths"], 1, 1, 1, 16)
+            assert p["runs"] == 1 and units > 1024 / 8 / 5           # four waves to a row: 1024 / units / 8, four at least
+            assert parts > 4 * 64, parts
+
+
 # ---- what the header says of a value's error, over all scales
 def groups(rng, n, low, high):
     """[n, 32] with the largest magnitude between 2^low and 2^high, and what they are held as."""

@@ -160,3 +160,68 @@ def test_nobody_gets_the_memory_of_a_call_on_its_own_stream():
     assert torch.equal(out, want)
     assert state[1].tolist() == [20] * B and int(state[4]) == 0 and int(state[5]) == 0
     assert sorted(slots[:, ::16].flatten().tolist()) == list(range(0, 16 * B * entries, 16))
+
+
+# ------------------------------------------------------------------------------------------------ joins, and pools that are streamed
+
+@pytest.mark.parametrize("i", range(len(forms.JOINS)))
+def test_joins(i):
+    import paper_2411_10803_amd as md
+    c = Case(600 + i, **forms.JOINS[i])
+    out, lse = c.call(md)
+    check(c, out, lse)
+    again, lse2 = c.call(md)
+    assert np.array_equal(out, again) and np.array_equal(lse, lse2)             # the same bits
+
+
+@pytest.mark.parametrize("dtype, d", ((BF16, 128), (F32, 64), (BF16, 64), (F32, 128)))
+def test_a_long_sample_among_short_ones(dtype, d):
+    """A row in more than 256 parts that four waves add up, each of them more than 64."""
+    import torch
+    import paper_2411_10803_amd as md
+    lengths, page, entries = forms.LONG["lengths"], forms.LONG["page"], forms.LONG["entries"]
+    rng = np.random.default_rng(d)
+    table, n_pages = base.scattered(rng, lengths, page, entries)
+    B, most = len(lengths), max(lengths)
+    cache = torch.full_like(md.cache4_buffer(n_pages, page, 1, d), 255)
+    K, V = np.zeros((B, most, 1, d)), np.zeros((B, most, 1, d))
+    for b, n in enumerate(lengths):                  # (rows in are tested byte by byte elsewhere)
+        k, v = rng.standard_normal((n, 1, d)) + 1.2 * (rng.random((n, 1, 1)) < 0.02), rng.standard_normal((n, 1, d))
+        at = np.arange(n)
+        rows = [torch.from_numpy(x[None]).float().cuda() for x in (k, v)]
+        md.mustdrop_cache4_write(*rows, dev((table[b, at // page] * page + at % page)[None].astype(np.int32)), cache)
+        K[b, :n], V[b, :n] = (ref.values(*ref.quantise(host(x)[0])) for x in rows)
+    q, qh = base.rows_on_gpu(rng.standard_normal((B, 1, 1, d)) + 0.3, dtype)
+    out, lse = md.mustdrop_cache4_attend(q, cache, dev(table), dev(np.asarray(lengths, np.int32)), 1 / np.sqrt(d),
+                                         lse=(l := torch.zeros((B, 1, 1), device="cuda"))), l
+    torch.cuda.synchronize()
+    out, lse = host(out).astype(np.float64), host(lse).astype(np.float64)
+    step, part = (2.0 ** -8, 2.0 ** -16) if dtype == BF16 else (2.0 ** -24, 2.0 ** -23)
+    for b, n in enumerate(lengths):
+        want, wlse, size, score = ref.attend(qh[b], K[b, :n], V[b, :n], np.ones(n, bool), n, 1, 1 / np.sqrt(d))
+        bound, lbound = ref.attend_bounds(want, wlse, size, score, d, n, step, part)
+        assert (np.abs(out[b] - want) <= bound).all() and (np.abs(lse[b].T - wlse) <= lbound).all(), b
+
+
+@pytest.mark.parametrize("kind, d, runs", forms.FORMS)
+def test_a_pool_that_is_streamed_gives_the_same_bits(kind, d, runs):
+    """Pools of more than 128 MiB are read by streaming loads: the same pages behind others, in one of 140."""
+    import torch
+    import paper_2411_10803_amd as md
+    c = Case(700, **forms.form(kind, d, runs, page=32, keep=0.8))
+    out, lse = c.call(md)
+    check(c, out, lse)
+    n_pages = (140 << 20) // (c.pool.shape[1] * c.pool.shape[2])
+    far = n_pages - len(c.pool)
+    cache = torch.full((n_pages,) + c.pool.shape[1:], 255, dtype=torch.uint8, device="cuda")
+    cache[far:] = dev(c.pool)
+    table = np.where((c.table >= 0) & (c.table < len(c.pool)), c.table + far, c.table).astype(np.int32)
+    big, lse2 = base.rows_on_gpu(np.full(out.shape, 7.0), c.dtype, c.layout, pad=1)[0], torch.full(lse.shape, 7.0, device="cuda")
+    md.mustdrop_cache4_attend(c.q, cache, dev(table), dev(np.asarray(c.lengths, np.int32)), c.scale, out=big, lse=lse2, keep=dev(c.keep))
+    torch.cuda.synchronize()
+    assert cache.numel() > 128 << 20 and np.array_equal(host(big), out) and np.array_equal(host(lse2), lse)
+
+
+def test_a_step_in_a_graph_with_eight_waves():
+    """As in a graph of short and of very long tables: tables of 512 entries, whose blocks have eight waves."""
+    base.test_decode_step_in_a_graph(32)
