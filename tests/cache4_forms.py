@@ -21,6 +21,11 @@ def form(kind, d, runs, page=16, **more):
     return dict(c, d=d, page=page, entries=(17408 if runs else 512) // page, **more)
 
 
+def nan_lengths(kind):
+    """Longer ones, so that runs cut the units of many samples: up to 500 entries."""
+    return [40 + (67 * b) % (190 if kind == "many" else 461) for b in range(22 if kind == "many" else 6)]
+
+
 FORMS = [(kind, d, runs) for kind in KINDS for d in (64, 128) for runs in (0, 1)]
 
 # Joins: fp32 rows of 128 and of 64 channels in runs, a block per row and per sixteen rows (more than 2048 rows in the call)

@@ -140,6 +140,33 @@ def attend(q, K, V, there, length, n_query, scale, keep=None):
     return out, lse, size, score
 
 
+def attend_heads(q, K, V, there, length, n_query, scale, keep=None):
+    """As attend(), all rows of a head at once.  A value that is no number reaches the rows that see it, in its channels."""
+    N, Hq, d = q.shape
+    G, j = Hq // K.shape[1], np.arange(K.shape[0])
+    out, lse = np.zeros((N, Hq, d)), np.full((N, Hq), -np.inf)
+    size, score = np.zeros((N, Hq, d)), np.zeros((N, Hq))
+    n = min(max(n_query, 0), N)
+    seen = there & (j < length) & (j <= length - n_query + np.arange(n)[:, None])
+    if keep is not None:
+        seen = seen & (keep != 0)
+    some = seen.any(1)
+    for h in range(Hq if n else 0):
+        k, v = K[:, h // G], V[:, h // G]
+        x = np.where(seen, scale * (q[:n, h] @ k.T), -np.inf)
+        m = np.where(some, x.max(1), 0)[:, None]
+        p = np.exp(x - m)
+        total = np.where(some, p.sum(1), 1)[:, None]
+        p /= total
+        none = seen.astype(float) @ np.isnan(v) > 0
+        clean = np.nan_to_num(v, nan=0.0)
+        out[:n, h] = np.where(none, np.nan, p @ clean)
+        size[:n, h] = np.where(none, np.nan, p @ np.abs(clean))
+        lse[:n, h] = np.where(some, (m + np.log(total))[:, 0], -np.inf)
+        score[:n, h] = scale * np.where(seen, np.abs(q[:n, h]) @ np.abs(k).T, 0).max(1)
+    return out, lse, size, score
+
+
 def attend_bounds(out, lse, size, score, d, length, half_step, part):
     """How far a right kernel may be off.  half_step: of the output's type, relative; part: relative error of a probability as it
     enters the product with V.

@@ -84,3 +84,18 @@ def test_errors_where_the_scale_ends():
     for top, off in ((3.38e38, 0.24), (6e-31, 0.3), (2.0 ** -103, 0.99)):
         v = np.full(32, top)
         assert np.abs(ref.values(*ref.quantise(v)) - v).max() > off * top
+
+
+# ---- the reference of all rows at once against that of a row at a time
+@pytest.mark.parametrize("n_query, length, nan", ((7, 30, False), (5, 33, True), (9, 4, True), (3, 0, False), (0, 20, False)))
+def test_reference_of_all_rows_at_once(n_query, length, nan):
+    rng = np.random.default_rng(length)
+    q, K, V = rng.standard_normal((9, 6, 64)), rng.standard_normal((36, 2, 64)), rng.standard_normal((36, 2, 64))
+    there, keep = np.arange(36) // 16 != 1, rng.integers(0, 3, 36)
+    if nan:
+        K[1, 0, 3], V[2, 1, 5], V[35, 0, 7] = np.nan, np.nan, np.nan
+        keep[1:3] = 1
+        V[max(0, length - 1), 1, 60] = np.nan
+    for mask in (None, keep):
+        for a, b in zip(ref.attend(q, K, V, there, length, n_query, 0.3, mask), ref.attend_heads(q, K, V, there, length, n_query, 0.3, mask)):
+            np.testing.assert_allclose(a, b, rtol=1e-12, atol=1e-14)

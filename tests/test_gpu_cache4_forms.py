@@ -19,7 +19,7 @@ def check(c, out, lse):
     for b in range(c.B):
         nq = c.N if c.q_len is None else int(np.clip(c.q_len[b], 0, c.N))
         n = int(np.clip(c.lengths[b], 0, c.table.shape[1] * c.page))
-        want, wlse, size, score = ref.attend(c.qh[b], c.K[b], c.V[b], c.there[b], n, nq, c.scale, None if c.keep is None else c.keep[b, :c.K.shape[1]])
+        want, wlse, size, score = ref.attend_heads(c.qh[b], c.K[b], c.V[b], c.there[b], n, nq, c.scale, None if c.keep is None else c.keep[b, :c.K.shape[1]])
         bound, lbound = ref.attend_bounds(want, wlse, size, score, c.d, n, step, part)
         assert (out[b, nq:] == 7).all() and (lse[b, :, nq:] == 7).all(), f"sample {b}: rows behind the last were written"
         got, gl, wl = out[b, :nq], lse[b, :, :nq].T, wlse[:nq]
@@ -59,6 +59,37 @@ def test_entries_of_a_table_behind_the_length_change_nothing(kind, d, runs):
     check(c, *results[0])
     for out, lse in results[1:]:
         assert np.array_equal(out, results[0][0]) and np.array_equal(lse, results[0][1])
+
+
+@pytest.mark.parametrize("page, masks", ((16, False), (64, True), (256, False), (256, True)))
+@pytest.mark.parametrize("kind, d, runs", forms.FORMS)
+def test_no_number_reaches_the_rows_that_see_it(kind, d, runs, page, masks):
+    """Groups that are no numbers in K and V, at entries that all rows of a sample see, that the last of them see, and that `keep` leaves out; in
+    any place of a page, and in parts of a unit that a join adds up."""
+    import paper_2411_10803_amd as md
+    c = Case(800 + page, **dict(forms.form(kind, d, runs, page=page, keep=0.9 if masks else None), lengths=forms.nan_lengths(kind)))
+    rng = np.random.default_rng(page + d)
+    poisoned = partly = 0
+    for b, n in enumerate(c.lengths):
+        first = max(0, n - c.N + 1)                  # from here on not all rows see an entry
+        late = [*rng.integers(first, n, 2), n - 1] if b % 3 else []
+        early = rng.integers(0, max(first, 1), 3) if b % 2 else []
+        for x, t in enumerate([*late, *early]):
+            h, g, in_k = rng.integers(0, c.H), rng.integers(0, d // 32), x == 0 and b % 4 == 1
+            kk, vv = c.K[b, t, h].copy(), c.V[b, t, h].copy()
+            kk[np.isnan(kk)], vv[np.isnan(vv)] = 1.0, 1.0
+            (kk if in_k else vv)[g * 32 + 7] = np.nan
+            ref.put(c.pool, c.table[b, t // page] * page + t % page, h, kk, vv, page)
+            c.K[b, t, h], c.V[b, t, h] = ref.values(*ref.quantise(kk)), ref.values(*ref.quantise(vv))
+            if masks:
+                c.keep[b, t] = x < 3 or x == 4       # two of the early ones are left out
+            poisoned += 1
+    out, lse = c.call(md)
+    for b in range(c.B):
+        bad = np.isnan(out[b]).any((1, 2))
+        partly += bad.any() and not bad.all()
+    assert poisoned > c.B and partly >= 2            # some rows, not all of them
+    check(c, out, lse)
 
 
 # ------------------------------------------------------------------------------------------------ streams
