@@ -407,7 +407,8 @@ int mustdrop_cache4_read(
  *   q_len    [B] i32 or NULL (= N); taken as 0 where negative, as N where larger;  len [B] i32, likewise within 0 .. max_pages*page
  *   keep     [B, max_pages*page] u8 or NULL (all): entries with keep 0 are seen by no row (they may hold anything)
  *   out      [B, N, Hq, d] (dtype; out_layout), rows >= q_len[b] untouched;  lse [B, Hq, N] f32 or NULL, likewise
- * A row that sees no entry gets out = 0 and lse = -infinity, as does one with all scores below -2e38.  Scores, sums and the
+ * softmax_scale is positive and finite, times log2(e) too.  A row that sees no entry gets out = 0 and lse = -infinity, as does one
+ * with all scores below -2e38.  Scores, sums and the
  * running maximum are fp32; a probability enters the product with V as a sum of bf16 parts that carries 24 bits for MD_F32 and 16
  * for MD_BF16.  Two calls on the same inputs with tables of the same width give the same bits.  The (N * Hq/H) rows of a sample and
  * K/V head are taken 16 at a time, or 32 for MD_BF16 where they are more than 16 and there are more than 512 tiles of 16 in the call;

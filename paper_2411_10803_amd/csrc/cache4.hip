@@ -1339,7 +1339,8 @@ int attend_impl(const void* q, int dtype, const void* cache, const int32_t* tabl
     if (B <= 0 || N <= 0 || Hq <= 0) return fail(MD_EINVAL, "cache4_attend: sizes must be positive");
     if (Hq % H || Hq > 65535) return fail(MD_ESHAPE, "cache4_attend: Hq=%d must be a multiple of H=%d", Hq, H);
     if (!q || !cache || !table || !len || !out) return fail(MD_EINVAL, "cache4_attend: null pointer among the required arguments");
-    if (!(softmax_scale > 0.f) || std::isinf(softmax_scale)) return fail(MD_EINVAL, "cache4_attend: softmax_scale must be positive and finite");
+    // (the kernels take scores to base 2: an infinite factor would make a score of 0 no number)
+    if (!(softmax_scale > 0.f) || std::isinf(softmax_scale * kLog2eC)) return fail(MD_EINVAL, "cache4_attend: softmax_scale must be positive and finite, times log2(e) too");
     KvLayout ql, ol;
     rc = read_layout("cache4_attend", "q", q_layout, B, N, Hq, d, &ql);
     if (rc == MD_OK) rc = read_layout("cache4_attend", "out", out_layout, B, N, Hq, d, &ol);

@@ -9,6 +9,7 @@ import pytest
 
 import cache4_forms as forms
 import cache4_ref as ref
+import test_cache4 as refusals
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -99,3 +100,14 @@ def test_reference_of_all_rows_at_once(n_query, length, nan):
     for mask in (None, keep):
         for a, b in zip(ref.attend(q, K, V, there, length, n_query, 0.3, mask), ref.attend_heads(q, K, V, there, length, n_query, 0.3, mask)):
             np.testing.assert_allclose(a, b, rtol=1e-12, atol=1e-14)
+
+
+# ---- refusals
+def test_a_scale_that_is_infinite_to_base_2_is_refused():
+    import ctypes as C
+    import paper_2411_10803_amd as md
+    lib = md.library()
+    for scale in (2.4e38, 3.4e38):
+        assert refusals.attend(lib, scale=C.c_float(scale)) == refusals.EINVAL and b"softmax_scale" in lib.mustdrop_last_error()
+    # the largest one that is taken, as far as the next check: no workspace
+    assert refusals.attend(lib, scale=C.c_float(2.3e38), ws=None) == refusals.EWORKSPACE
