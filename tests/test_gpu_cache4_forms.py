@@ -92,6 +92,26 @@ def test_no_number_reaches_the_rows_that_see_it(kind, d, runs, page, masks):
     check(c, out, lse)
 
 
+@pytest.mark.parametrize("kind, d, runs", forms.FORMS)
+def test_a_query_that_is_no_number_reaches_its_own_rows(kind, d, runs):
+    import torch
+    import paper_2411_10803_amd as md
+    c = Case(900, **dict(forms.form(kind, d, runs), lengths=forms.nan_lengths(kind)))
+    rng = np.random.default_rng(d)
+    bad = np.zeros((c.B, c.N, c.Hq), bool)
+    for b in range(1, c.B):
+        i, h = rng.integers(0, c.N), rng.integers(0, c.Hq)
+        if c.lengths[b] - c.N + i < 30:              # (many keys: an infinite query then has scores of both signs)
+            i = c.N - 1
+        c.q[b, i, h, rng.integers(0, d)] = float("nan") if b % 2 else float("inf")
+        bad[b, i, h] = True
+    with np.errstate(invalid="ignore"):
+        out, lse = c.call(md)
+        c.qh = np.where(bad[..., None], np.nan, c.qh)
+        check(c, out, lse)
+    assert np.array_equal(np.isnan(out).all(3), bad) and np.array_equal(np.isnan(lse.transpose(0, 2, 1)), bad)
+
+
 # ------------------------------------------------------------------------------------------------ streams
 
 def busy_for_a_while(torch, stream, work):
