@@ -22,7 +22,7 @@
  *   - Tensors are row-major with the last dimension contiguous.  Base pointers of the large
  *     tensors must be 16-byte aligned and their rows (D, dc, d, C elements) a multiple of 16 bytes.
  *   - Indices are int32, 0-based, in the coordinates of that call's input; index lists ascend.
- *   - Inputs are never written, except the in/out state of mustdrop_decode_evict.
+ *   - Inputs are never written, except what is marked in/out and the in/out state of mustdrop_decode_evict.
  *   - Return value: MD_OK or an error code.  Argument errors are detected on the host before any
  *     kernel is launched; mustdrop_last_error() returns a thread-local description.
  *   - `workspace` must hold at least mustdrop_<stage>_workspace_bytes(...) bytes, 256-byte aligned.
@@ -360,10 +360,14 @@ int mustdrop_decode_keep_strided(
  * outside the pool names no page: its entries take no part in attention, its rows are not read out; a slot outside the pool is
  * not written.
  *
+ * The stages above do not read this cache.  mustdrop_decode_evict and mustdrop_decode_keep take dense rows: read the cache out, evict,
+ * write what is left.  The `keep` of the attention comes from the caller; nothing here makes one from the pages.
+ *
  * Limits of the cache4 calls: d in {64, 128}; page a power of two from 16 to 256; n_pages * page < 2^31,
  * max_pages * page < 2^30; a pool of at most 256 GiB; H <= 65535; rows in MD_BF16 or MD_F32, fewer than 2^28 - 15 of them
  * (B*N) in or out in a call; base pointers 16-byte aligned.  md_kv_layout as above
- * (elements of the rows' type); NULL = dense token-major.
+ * (elements of the rows' type); NULL = dense token-major.  MD_EALIAS goes by a tensor's first and last element: an output whose rows
+ * lie between those of another tensor (K and V side by side in one buffer) is refused, inputs may lie so.
  */
 size_t mustdrop_cache4_bytes(int n_pages, int page, int H, int d);      /* 0 for sizes that no call takes */
 

@@ -111,3 +111,16 @@ def test_a_scale_that_is_infinite_to_base_2_is_refused():
         assert refusals.attend(lib, scale=C.c_float(scale)) == refusals.EINVAL and b"softmax_scale" in lib.mustdrop_last_error()
     # the largest one that is taken, as far as the next check: no workspace
     assert refusals.attend(lib, scale=C.c_float(2.3e38), ws=None) == refusals.EWORKSPACE
+
+
+def test_outputs_between_other_rows_are_refused_and_inputs_are_not():
+    """K and V side by side in one buffer [B, N, 2, H, d]: as inputs (far enough for the next check to be reached), not as outputs."""
+    import ctypes as C
+    import paper_2411_10803_amd as md
+    lib = md.library()
+    k, H, d, N = refusals.P(1), 4, 128, 3
+    v, lay = C.c_void_p(k.value + H * d * 2), refusals.layout(N * 2 * H * d, 2 * H * d, d)
+    assert refusals.read(lib, k=k, v=v, lay=lay) == refusals.EALIAS
+    assert refusals.write(lib, k=k, v=v, lay=lay, slots=refusals.P(4)) == refusals.EALIAS and b"overlap" in lib.mustdrop_last_error()   # (slots over the pool)
+    assert refusals.attend(lib, q=k, out=v, Hq=H, ql=lay, ol=lay) == refusals.EALIAS
+    assert refusals.attend(lib, q=k, Hq=H, ql=lay, ws=None) == refusals.EWORKSPACE

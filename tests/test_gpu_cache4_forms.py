@@ -112,6 +112,26 @@ def test_a_query_that_is_no_number_reaches_its_own_rows(kind, d, runs):
     assert np.array_equal(np.isnan(out).all(3), bad) and np.array_equal(np.isnan(lse.transpose(0, 2, 1)), bad)
 
 
+@pytest.mark.parametrize("dtype, d", ((BF16, 128), (F32, 64)))
+def test_rows_from_one_buffer_of_queries_keys_and_values(dtype, d):
+    """[B, N, (Hq + 2 H) d], as one projection gives it: rows in and queries as views of it."""
+    import torch
+    import paper_2411_10803_amd as md
+    B, N, Hq, H, page = 3, 9, 6, 2, 16
+    g = torch.Generator(device="cuda").manual_seed(d)
+    one = torch.randn((B, N, Hq + 2 * H, d), generator=g, device="cuda").to(torch.bfloat16 if dtype == BF16 else torch.float32)
+    q, k, v = one[:, :, :Hq], one[:, :, Hq:Hq + H], one[:, :, Hq + H:]
+    slots = torch.arange(B * page, dtype=torch.int32, device="cuda").view(B, page)[:, :N].contiguous()
+    table, length = torch.arange(B, dtype=torch.int32, device="cuda")[:, None].contiguous(), torch.full((B,), N, dtype=torch.int32, device="cuda")
+    got = []
+    for x in ((q, k, v), (q.contiguous(), k.contiguous(), v.contiguous())):
+        cache = md.cache4_buffer(B, page, H, d)
+        md.mustdrop_cache4_write(x[1], x[2], slots, cache)
+        got.append((cache, md.mustdrop_cache4_attend(x[0], cache, table, length, 0.1)))
+    torch.cuda.synchronize()
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and bool(got[0][1].any())
+
+
 # ------------------------------------------------------------------------------------------------ streams
 
 def busy_for_a_while(torch, stream, work):
