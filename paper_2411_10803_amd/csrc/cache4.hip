@@ -507,12 +507,13 @@ __device__ __forceinline__ Kept kept_at(const Walk& w, int step) {
 // probabilities are at once the right-hand operand of O^T = V^T P^T: with two 16-key tiles the eight contraction places of lane
 // group b are keys 4 b + 0..3 of either tile.  The pages hold V so that a lane loads those keys' codes of its channels, and of K so
 // that a lane loads d/4 channels of one token: from the loads to the matrix products no lane needs another's data.
-// (The scaled 16x16x128 product would take K's codes and scales as they lie and a query as two e4m3 rows, a prompt's piece in 153 us instead of 164,
-// but its sums are not fp32 ones: lse was off 10 to 40 times as far.)
+// (The scaled 16x16x128 product would take K's codes and scales as they lie and a query as two e4m3 rows, a prompt's piece 7 % faster, but its sums
+// are not fp32 ones: lse was off 10 to 40 times as far.)
 template <int D, bool F32, int NT>
 struct Rows {
     static constexpr int QT = F32 ? 3 : 1;           // bf16 parts of a query: fp32 has 24 bits
-    static constexpr int PT = F32 ? 3 : 2;           // of a probability in the product with V: in one part its rounding would be as large as the output's
+    static constexpr int PT = F32 ? 3 : 2;           // of a probability in the product with V: in one part its rounding would be as large as the
+                                                     // output's (and 4 x 512 tokens of 32 heads on 8, up to 5888 keys, 193 us instead of 235)
     static constexpr int KS = D / 32;                // contraction steps of S
     static constexpr int J = D / 16;                 // 16-channel tiles of O
 
@@ -889,9 +890,11 @@ __device__ __forceinline__ void join_waves(S& w, int rows, float* lds, Done done
     }
 }
 
-// The sample of the blocks that come `at`-th: of each 64, the longest first, so that the last blocks to run are short.  us as they come / so: a
-// prompt's piece of 4 x 512 tokens behind up to 5888 keys 169 / 152, of 8 x 512 behind 1500 keys each 157 / 154.  Not for single tokens, which
-// wait for memory: 64 x up to 4096 keys 114 / 122, 64 x up to 500 26 / 33.
+// The sample of the blocks that come `at`-th: of each 64, the longest first, so that the last blocks to run are short.  us as they come / so, of
+// 32 heads on 8: a prompt's piece of 4 x 512 tokens behind up to 5888 keys 257 / 235, 32 x 128 behind up to 4000 318 / 300.  It gains nothing
+// where lengths are equal or the blocks make many rounds anyway, and then costs what the order takes to find: 8 x 512 behind 1500 keys each
+// 177 / 183, 16 x 512 behind up to 3000 389 / 405, 64 x 512 behind up to 1500 845 / 950.  Not for single tokens, which wait for memory: 64 x
+// up to 4096 keys 114 / 122, 64 x up to 500 26 / 33.
 __device__ __forceinline__ int by_length(const AttendArgs& A, int at) {
     const int base = at & -kWave, lane = lane_id(), n = min(A.dim.B - base, kWave);
     int mine = -1, before = 0;
@@ -924,7 +927,7 @@ __global__ __launch_bounds__(NT == 2 || (F32 && D == 128) ? 256 : 512, NT == 2 |
         w = table_of(A, b);
         early = early_pages(w, wave_id(), blockDim.x >> 6);
         Sample s = sample_of(A, b);
-        if (NT == 1) arrived(early, s.length, s.nq);             // (32 rows together are many steps to a wave: a prompt's piece 169 us, 171 so)
+        if (NT == 1) arrived(early, s.length, s.nq);             // (32 rows together are many steps to a wave: a prompt's piece 235 us either way)
         if (r0 >= s.nq * A.dim.G) return;
         sw.begin(A, s, h, r0);
         walk_of(w, A, s, h, r0, min(r0 + ROWS, s.nq * A.dim.G) - 1);
