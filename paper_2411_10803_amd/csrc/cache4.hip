@@ -356,6 +356,10 @@ typedef const __attribute__((address_space(1))) void* global_ptr_t;
 constexpr float kNoKey = -3.0e38f;                   // running maximum before the first key (below every score that matters)
 // A running maximum may lag behind by this much (base 2) before the sums are scaled anew: probabilities up to 2^8 cost no accuracy.
 constexpr float kLag = 8.f;
+// A running maximum m is a rounded product of a score and the scale, and score * scale - m in one fma has that rounding in it: half a unit in
+// the last place of m, which every probability of the row is off by as a power of two, in numerator and sum alike.  Up to here that
+// is 2^4 at most; beyond 2^31 it would be more than fp32 holds, and the product is rounded as the maximum was.
+constexpr float kFar = 67108864.f;
 
 __device__ __forceinline__ uint32_t fp4_pair(uint32_t w, float s, int byte) {       // byte: a constant
     switch (byte) {
@@ -374,6 +378,13 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t (&part)[TE
         part[i] = as_u32(__builtin_convertvector(f32x2{x, y}, bf16x2));
         if (i + 1 < TERMS) { x -= bf16_lo(part[i]); y -= bf16_hi(part[i]); }
     }
+}
+
+// A product that no addition is fused with.
+__device__ __forceinline__ float rounded_product(float x, float y) {
+    float r = x * y;
+    asm("" : "+v"(r));
+    return r;
 }
 
 // The larger of a value over the four lanes of one query (lane ^ 16, lane ^ 32), and the sum.
@@ -522,16 +533,21 @@ struct Rows {
     f32x4 o[NT][J];
     int limit[NT];                                   // keys that the lane's row sees: up to its own position
     int n, lb;
+    // What a probability's exponent is made of: score * by - off.  The scale to base 2 and the running maximum; once a maximum of the wave is
+    // beyond kFar, 1 and 0, and the scores of every step are made the exponents themselves where the maxima are looked after (`lag` then lets no step by).
+    float off[NT], by, lag;
 
     __device__ __forceinline__ void begin(const AttendArgs& A, const Sample& s, int h, int r0) {
         n = lane_id() & 15;
         lb = lane_id() >> 4;
+        by = A.scale * kLog2eC;
+        lag = kLag;
         const int G = A.dim.G, live = s.nq * G;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int r = r0 + 16 * t + n, i = r / G, hq = h * G + (r - i * G);
             limit[t] = r < live ? min(max(s.length - s.nq + i + 1, 0), s.length) : 0;
-            m[t] = kNoKey;
+            m[t] = off[t] = kNoKey;
             l[t] = 0.f;
 #pragma unroll
             for (int j = 0; j < J; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -616,22 +632,33 @@ struct Rows {
     }
 
     // Probabilities of tile t's scores, in PT parts; the running maximum follows where the scores have outgrown it.
-    __device__ __forceinline__ void softmax(int t, const f32x4 (&st)[2], float c, bf16x8 (&p)[PT]) {
+    __device__ __forceinline__ void softmax(int t, f32x4 (&st)[2], float c, bf16x8 (&p)[PT]) {
         float most = st[0][0];
 #pragma unroll
         for (int x = 1; x < 8; ++x) most = fmaxf(most, st[x >> 2][x & 3]);
         most *= c;
-        if (__any(most > m[t] + kLag)) {
+        if (__any(most > m[t] + lag)) {
             const float m2 = fmaxf(m[t], max_over_groups(most)), a = fast_exp2(m[t] - m2);
-            m[t] = m2;
+            m[t] = off[t] = m2;
             l[t] *= a;
 #pragma unroll
             for (int j = 0; j < J; ++j) o[t][j] *= a;
+            if (lag < 0.f || __any(fabsf(m2) > kFar && m2 > kNoKey)) {
+                lag = -INFINITY;
+                by = 1.f;
+#pragma unroll
+                for (int z = 0; z < NT; ++z) off[z] = 0.f;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const float s = st[x >> 2][x & 3], near = fmaf(s, c, -m2), beyond = rounded_product(s, c) - m2;
+                    st[x >> 2][x & 3] = fabsf(m2) > kFar ? beyond : near;
+                }
+            }
         }
         uint32_t w[PT][4];
 #pragma unroll
         for (int x = 0; x < 8; x += 2) {
-            const float p0 = fast_exp2(fmaf(st[x >> 2][x & 3], c, -m[t])), p1 = fast_exp2(fmaf(st[x >> 2][(x & 3) + 1], c, -m[t]));
+            const float p0 = fast_exp2(fmaf(st[x >> 2][x & 3], by, -off[t])), p1 = fast_exp2(fmaf(st[x >> 2][(x & 3) + 1], by, -off[t]));
             l[t] += p0 + p1;
             uint32_t part[PT];
             split_pair<PT>(p0, p1, part);

@@ -112,6 +112,66 @@ def test_a_query_that_is_no_number_reaches_its_own_rows(kind, d, runs):
     assert np.array_equal(np.isnan(out).all(3), bad) and np.array_equal(np.isnan(lse.transpose(0, 2, 1)), bad)
 
 
+@pytest.mark.parametrize("entries", (8, 1100))       # of a table with pages of 16: blocks, runs
+@pytest.mark.parametrize("dtype", (BF16, F32))
+def test_scores_at_the_ends_of_the_range(dtype, entries):
+    """Rows that see one key whose only channel is 1: their score is the query's.  Beyond 2.3e38 it is infinite to base 2 and the row NaN, below
+    -2e38 the row is as one that sees nothing; in between lse is the score, but for five roundings of 2^-24 each (log2(e), its product with the score,
+    the sum with log2 of a sum near 1, ln 2, its product) and a unit each of exp2 and log2 near 1, 2^-22 together."""
+    import paper_2411_10803_amd as md
+    d, scores = 64, np.array([2.2e38, 3e38, -1.9e38, -2.2e38, -3e38, 1.0, 0.0, 1e30])
+    c = Case(950, [1] * 4, 1, len(scores), 1, d, 16, dtype, entries=entries)
+    k = np.zeros(d)
+    k[5] = 1.0
+    for b in range(4):
+        ref.put(c.pool, int(c.table[b, 0]) * 16, 0, k, c.V[b, 0, 0], 16)
+    q = np.zeros(c.qh.shape)
+    q[..., 5] = scores
+    c.q, c.qh = base.rows_on_gpu(q, dtype)
+    c.scale = 1.0
+    out, lse = c.call(md)
+    want = np.where(scores > 2.3e38, np.nan, np.where(scores < -2e38, -np.inf, c.qh[0, 0, :, 5]))
+    for b in range(4):
+        assert np.array_equal(np.isnan(lse[b, :, 0]), np.isnan(want)) and np.array_equal(np.isneginf(lse[b, :, 0]), np.isneginf(want))
+        ok = np.isfinite(want)
+        assert (np.abs(lse[b, ok, 0] - want[ok]) <= 5 * 2.0 ** -24 * np.abs(want[ok]) + 2.0 ** -22).all()
+        assert np.isnan(out[b, 0, np.isnan(want)]).all() and (out[b, 0, np.isneginf(want)] == 0).all()
+        assert (out[b, 0, ok] == c.V[b, 0, 0]).all()             # (one probability of 1: V itself, exact in bf16)
+
+
+@pytest.mark.parametrize("masks", (False, True))
+@pytest.mark.parametrize("kind, d, runs", forms.FORMS)
+def test_scores_of_every_size(kind, d, runs, masks):
+    """Queries of one channel, from 1 to 2^120: a score is one exact product, so keys of one value tie at any size, and where scores are large only those
+    of the largest count.  Off by: the factor to base 2, 2^-23 of a difference of scores of which no more than 150 count, 2^-21 for exp2, the
+    sums over the keys, 2^-16 or 2^-23 for the parts of a probability (twice each, in the product and in the sum), and the output's rounding."""
+    import paper_2411_10803_amd as md
+    c = Case(970, **dict(forms.form(kind, d, runs, keep=0.9 if masks else None), lengths=forms.nan_lengths(kind)))
+    rng = np.random.default_rng(d + runs)
+    for b, n in enumerate(c.lengths):
+        for t in range(n):
+            for h in range(c.H):
+                k = np.zeros(d)
+                k[3] = rng.choice([6, 4, 3, 2, 1.5, 1, 0.5, 0, -1, -6])
+                ref.put(c.pool, c.table[b, t // c.page] * c.page + t % c.page, h, k, c.V[b, t, h], c.page)
+                c.K[b, t, h] = k
+    q = np.zeros(c.qh.shape)
+    q[..., 3] = np.exp2(rng.integers(0, 121, q.shape[:3]).astype(float)) * rng.choice([1, -1, 1.5, 1.25], q.shape[:3])
+    c.q, c.qh = base.rows_on_gpu(q, c.dtype)
+    assert np.array_equal(c.qh, q)
+    c.scale = float(np.float32(c.scale))
+    out, lse = c.call(md)
+    step, part = (2.0 ** -8, 2.0 ** -16) if c.dtype == BF16 else (2.0 ** -24, 2.0 ** -23)
+    for b, n in enumerate(c.lengths):
+        want, wlse, size, _ = ref.attend_heads(c.qh[b], c.K[b], c.V[b], c.there[b], n, c.N, c.scale, None if c.keep is None else c.keep[b, :c.K.shape[1]])
+        bound = step * np.abs(want) + 2 * (150 * 2.0 ** -23 + 2.0 ** -21 + (n / 32 + 64) * 2.0 ** -24 + part) * size + 1e-37
+        assert (np.abs(out[b] - want) <= bound).all(), b
+        gl, empty = lse[b].T, np.isneginf(wlse)
+        assert np.array_equal(np.isneginf(gl), empty)
+        gl, wlse = gl[~empty], wlse[~empty]
+        assert (np.abs(gl - wlse) <= 6 * 2.0 ** -24 * np.abs(wlse) + 150 * 2.0 ** -23 + 2.0 ** -21 + (n / 32 + 64) * 2.0 ** -24).all(), b
+
+
 @pytest.mark.parametrize("dtype, d", ((BF16, 128), (F32, 64)))
 def test_rows_from_one_buffer_of_queries_keys_and_values(dtype, d):
     """[B, N, (Hq + 2 H) d], as one projection gives it: rows in and queries as views of it."""
