@@ -415,7 +415,8 @@ int mustdrop_cache4_read(
  * with all scores below -2e38.  A row whose query or scores are no numbers, or with a score beyond 2.3e38, is NaN, and so are the
  * channels of a group of V that is, in the rows that see it; no other row is.  Scores, sums and the running maximum are fp32 (the sum of
  * p_j v_j is up to 2^12 times as large before it is divided: a V below 8e34 / len cannot overflow); a probability enters the product
- * with V as a sum of bf16 parts that carries 24 bits for MD_F32 and 16 for MD_BF16.  Two calls on the same inputs with tables of
+ * with V as a sum of bf16 parts that carries 24 bits for MD_F32 and 16 for MD_BF16.  An fp32 query is a sum of three bf16 parts: all of its
+ * 24 bits from 2^-110 on, what is above 2^-134 below that; beyond 3.39e38 its row is NaN.  Two calls on the same inputs with tables of
  * the same width give the same bits.  The (N * Hq/H) rows of a sample and K/V head are taken 16 at a time, or 32 for MD_BF16 where
  * they are more than 16 and there are more than 512 tiles of 16 in the call; a call takes fewer than 2^23 such tiles.  Errors: MD_EINVAL,
  * MD_ESHAPE, MD_EDTYPE, MD_EALIGN (keep 4-byte aligned), MD_EALIAS, MD_EWORKSPACE, MD_EHIP. */

@@ -172,6 +172,88 @@ def test_scores_of_every_size(kind, d, runs, masks):
         assert (np.abs(gl - wlse) <= 6 * 2.0 ** -24 * np.abs(wlse) + 150 * 2.0 ** -23 + 2.0 ** -21 + (n / 32 + 64) * 2.0 ** -24).all(), b
 
 
+@pytest.mark.parametrize("entries", (8, 1100))
+@pytest.mark.parametrize("d", (64, 128))
+def test_fp32_queries_at_the_ends_of_their_range(d, entries):
+    """One key of 2^k in one channel, queries of 24 bits: a score is one exact product.  Off by five roundings of 2^-24, a unit each of exp2 and log2
+    near 1, and by what a query has below 2^-134 (half the smallest bf16 number)."""
+    import paper_2411_10803_amd as md
+    for k, queries in ((125, np.exp2([-110.0, -109, -100, -112, -120, -126, -133]) * (2 - 2.0 ** -23)), (-90, np.array([3.389e38, -3.389e38, 1e38, 3.4e38]))):
+        c = Case(990, [1] * 2, 1, len(queries), 1, d, 16, F32, entries=entries)
+        key = np.zeros(d)
+        key[9] = 2.0 ** k
+        for b in range(2):
+            ref.put(c.pool, int(c.table[b, 0]) * 16, 0, key, c.V[b, 0, 0], 16)
+        q = np.zeros(c.qh.shape)
+        q[..., 9] = queries.astype(np.float32)
+        c.q, c.qh = base.rows_on_gpu(q, F32)
+        c.scale = 1.0
+        out, lse = c.call(md)
+        want = c.qh[0, 0, :, 9] * 2.0 ** k
+        over = np.abs(queries) > 3.3895e38
+        assert np.array_equal(np.isnan(lse[0, :, 0]), over) and np.isnan(out[:, 0, over]).all()
+        bound = 5 * 2.0 ** -24 * np.abs(want) + 2.0 ** -22 + 2.0 ** (k - 134)
+        assert (np.abs(lse[:, :, 0] - want) <= bound)[:, ~over].all() and np.isfinite(out[:, 0, ~over]).all()
+
+
+@pytest.mark.parametrize("scale", (1e-44, 1e-20, 1e20))
+@pytest.mark.parametrize("kind, d, runs", [f for f in forms.FORMS if f[1] == 64])
+def test_scales_of_every_size(kind, d, runs, scale):
+    """Tiny ones (a factor that fp32 holds with few bits): all keys count alike.  A large one, with queries that make up for it."""
+    import paper_2411_10803_amd as md
+    c = Case(980, **forms.form(kind, d, runs))
+    if scale > 1:
+        c.q, c.qh = base.rows_on_gpu(c.qh * 2.0 ** -67, c.dtype)
+    c.scale = float(np.float32(scale))
+    check(c, *c.call(md))
+
+
+def test_a_sample_of_seventy_million_entries():
+    """4.8 GB of one sample's pages; its keys are 0, so that a row's output is the mean of the values.  The sums of a part are exact (multiples of 1/2
+    below 2^22), the join of at most 1024 parts and four waves adds them up: 2^-24 of all of it each."""
+    import torch
+    import paper_2411_10803_amd as md
+    n, d, page = 70_000_001, 64, 256
+    n_pages = -(-n // page)
+    cache = md.cache4_buffer(n_pages, page, 1, d)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    at = page * (d // 2 + d // 32)                   # codes of V: [page / 4, 16, 4, d / 32], magnitudes without a sign
+    cache[:, 0, page * d // 2:at] = 127
+    cache[:, 0, at + page * d // 2:] = 127
+    codes = cache[:, 0, at:at + page * d // 2].view(n_pages, page // 4, 16, 4, d // 32)
+    levels = torch.tensor(ref.LEVELS, dtype=torch.float64, device="cuda")
+    total = torch.zeros((16, d // 32, 2), dtype=torch.float64, device="cuda")
+    for i in range(0, n_pages, 8192):
+        part = torch.randint(0, 256, codes[i:i + 8192].shape, generator=g, dtype=torch.uint8, device="cuda") & 0x77
+        codes[i:i + 8192] = part
+        live = (torch.arange(i * page, i * page + part.shape[0] * page, device="cuda") < n).view(part.shape[0], page // 4, 1, 4, 1)
+        for half in range(2):
+            total[..., half] += (levels[((part >> (4 * half)) & 7).int()] * live).sum((0, 1, 3))
+    mean = (total / n).reshape(d).cpu().numpy()
+    ends = cache[0].clone()
+    cache[0], cache[-1] = cache[-1].clone(), ends
+    order = torch.arange(n_pages, dtype=torch.int32, device="cuda")
+    order[0], order[-1] = n_pages - 1, 0             # entry 0 in the last page of the pool, the last entry in its first
+    table = order[None].contiguous()
+    length = torch.full((1,), n, dtype=torch.int32, device="cuda")
+    q = torch.randn((1, 1, 3, d), generator=g, device="cuda")
+    lse = torch.zeros((1, 3, 1), device="cuda")
+    out = md.mustdrop_cache4_attend(q, cache, table, length, 0.125, lse=lse)
+    torch.cuda.synchronize()
+    assert (np.abs(host(out)[0, 0] - mean) <= 1100 * 2.0 ** -24 * mean).all()
+    assert (np.abs(host(lse) - np.log(n)) <= 1100 * 2.0 ** -24 + 2.0 ** -22 * np.log(n)).all()
+    # rows out of its end, and one more in
+    rows = [torch.zeros((1, 4, 1, d), device="cuda") for _ in range(2)]
+    md.mustdrop_cache4_read(cache, table, length, *rows, first=length - 2)
+    slot = torch.tensor([[int(order[n // page]) * page + n % page]], dtype=torch.int32, device="cuda")
+    new = torch.full((1, 1, 1, d), 6.0, device="cuda")
+    md.mustdrop_cache4_write(new, new, slot, cache)
+    after = [torch.zeros((1, 1, 1, d), device="cuda") for _ in range(2)]
+    md.mustdrop_cache4_read(cache, table, length + 1, *after, first=length)
+    torch.cuda.synchronize()
+    assert (rows[0] == 0).all() and rows[1][0, :2].any() and not rows[1][0, 2:].any() and all(torch.equal(x, new) for x in after)
+
+
 @pytest.mark.parametrize("dtype, d", ((BF16, 128), (F32, 64)))
 def test_rows_from_one_buffer_of_queries_keys_and_values(dtype, d):
     """[B, N, (Hq + 2 H) d], as one projection gives it: rows in and queries as views of it."""
