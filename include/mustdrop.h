@@ -6,7 +6,8 @@
  *   mustdrop_encode_merge    Sec. 3.3  Local Spatial Merging (Eq. 5) + Key Retaining (Eq. 6-7)
  *   mustdrop_prefill_filter  Sec. 3.4  dual-attention filtering (Eq. 8-10) + token drop
  *   mustdrop_decode_evict    Sec. 3.5  output-aware cache policy, one decode step
- * and, behind them, a paged cache held in 4 bits with the attention that reads it (mustdrop_cache4_*).
+ * and, behind them, a paged cache held in 4 bits with the attention that reads it, all of it or the pages that a cheap score
+ * chooses (mustdrop_cache4_*), and the rotation of queries and keys by positions with several axes (mustdrop_rotate).
  *
  * Conventions common to all calls
  *   - Every data pointer is DEVICE memory owned by the caller (inputs, outputs and the workspace).
@@ -425,6 +426,97 @@ size_t mustdrop_cache4_attend_workspace_bytes(int B, int N, int Hq, int H, int d
 int mustdrop_cache4_attend(
     const void* q, md_dtype dtype, const void* cache, const int32_t* table, const int32_t* len, const int32_t* q_len, const uint8_t* keep,
     int B, int N, int Hq, int H, int d, int n_pages, int page, int max_pages, float softmax_scale,
+    void* out, float* lse, const md_kv_layout* q_layout, const md_kv_layout* out_layout,
+    void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Rotation of queries and keys by their positions.  A token of an image or a video has a place on several axes (time, height, width),
+ * and what the stages above keep are rows whose places are not consecutive any more.
+ *
+ * Of a row's d channels the first 2 * pairs turn in pairs: pair i is channels (i, i + pairs), or (2i, 2i + 1) where `adjacent`; the
+ * others stay.  Pair i has an axis; with p the row's position on it and (c, s) = table[p][i], (x, y) becomes (x c - y s, y c + x s), or
+ * with -s in the place of s where `inverse` (the gradient; where c^2 + s^2 = 1 the way back, too).  In fp32: the products are rounded, then their sum, then
+ * the result to the rows' type.  What the angles are (base, scaling, any factor) is the table's business.
+ *   pairs      a multiple of 4 (8 for mustdrop_cache4_append), 2 * pairs <= d
+ *   axes       1 to 4;  axis[i] < axes for i < pairs
+ *   table      [n_pos, pairs, 2] f32: cosine and sine of each position's angles
+ *   positions  [axes, B, L] i32;  index [B, N] i32 or NULL: row (b, i) is at positions[.][b][index[b][i]], or [i] without index (then
+ *              L >= N).  A position outside 0 .. n_pos-1 turns its pairs into NaN, an index outside 0 .. L-1 all pairs of its row.
+ */
+typedef struct md_rotary {
+    int32_t pairs, axes, adjacent;
+    uint8_t axis[128];
+} md_rotary;
+
+/* Rows turned: q [B, N, Hq, d] into q_out, and k [B, N, H, d] into k_out in the same launch (k = k_out = NULL: only q).  An output may be
+ * its input, with the same layout; no other overlap.  rows [B] i32 or NULL (= N): rows (b, i) with i >= rows[b] are not read and
+ * not written.  d a multiple of 8, at most 256; layouts as md_kv_layout, NULL = dense token-major; B * N <= 2^28 - 16 and fewer than 2^32
+ * groups of 16 channels.  Errors: MD_EINVAL, MD_ESHAPE, MD_EDTYPE, MD_EALIGN, MD_EALIAS, MD_EHIP. */
+int mustdrop_rotate(
+    const void* q, const void* k, md_dtype dtype, const int32_t* positions, const int32_t* index, const float* table, const int32_t* rows,
+    int B, int N, int L, int Hq, int H, int d, int n_pos, const md_rotary* rotary, int inverse,
+    void* q_out, void* k_out,
+    const md_kv_layout* q_layout, const md_kv_layout* k_layout, const md_kv_layout* q_out_layout, const md_kv_layout* k_out_layout,
+    void* stream);
+
+/* Rows into the cache held in 4 bits (mustdrop_cache4_write), k_new [B, N, H, d] turned on the way: the turned fp32 numbers are what is
+ * rounded to 4 bits.  q [B, N, Hq, d] is turned too, into q_out (which may be q, with the same layout), in the same launch; q = q_out =
+ * NULL: no queries.  A row whose slot names no place of the pool takes no part, its query neither.  k_new and v_new have rows_layout;
+ * no two rows of a call may have the same slot.  Errors as for mustdrop_cache4_write and mustdrop_rotate. */
+int mustdrop_cache4_append(
+    const void* q, const void* k_new, const void* v_new, md_dtype dtype, const int32_t* positions, const int32_t* index, const float* table,
+    const int32_t* slots, void* cache,
+    int B, int N, int L, int Hq, int H, int d, int n_pos, int n_pages, int page, const md_rotary* rotary,
+    void* q_out, const md_kv_layout* q_layout, const md_kv_layout* rows_layout, const md_kv_layout* q_out_layout, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Attention over a part of the cache held in 4 bits: over the pages that a cheap score chooses for each token and K/V head.  For pools,
+ * block tables and their limits see above.
+ *
+ * Bounds of a page's keys, per head.  With a the largest magnitude among the page's keys and e = floor(log2 a) - 6 (a = 0: -126), at
+ * least -126: bounds [n_pages, H, 2, d] i8, every channel's largest value over 2^e rounded up, then every channel's smallest one rounded
+ * down (within -96 and 96); scales [n_pages, H] u8 the byte e + 127, or 255 where a group of the page's keys has a scale beyond 252 (the
+ * write makes no other than 255: a key that is no number), whose bounds are then 0.  Values of 4 bits whose group has a scale of at least an eighth of the largest one's are held exactly.
+ */
+
+/* Bounds of the pages that hold the entries first[b] .. min(first[b] + N, len[b]) - 1 of every sample, each over all of the page's
+ * entries below len[b]: what else the page holds does not count.  A page that several entries of the tables name has to be as full
+ * for each of them (its bounds may be parts of theirs otherwise).  first [B] i32 or NULL (0); negative ones are taken as 0.
+ * Errors: MD_EINVAL, MD_ESHAPE (limits, more than 2^25 pages and heads to go through), MD_EALIGN, MD_EALIAS, MD_EHIP. */
+int mustdrop_cache4_bounds(
+    const void* cache, const int32_t* table, const int32_t* len, const int32_t* first, int8_t* bounds, uint8_t* scales,
+    int B, int N, int H, int d, int n_pages, int page, int max_pages, void* stream);
+
+/* The pages that a token's attention is to read, for each of the last q_len[b] entries of every sample (which see entries as in
+ * mustdrop_cache4_attend) and each K/V head.
+ * The G = Hq / H queries of a token and K/V head become whole numbers: with a their largest magnitude, those of 2^(floor(log2 a) - 6),
+ * the nearest (of two as near the even one), within -127 and 127; all 0 where a is 0 or no finite number.  A page's score is
+ *   2^e * sum over the G queries and the channels of max(q * largest, q * smallest)
+ * with the page's bounds, summed in whole numbers and rounded to fp32 once: no key of the page has a larger sum of its scores with the
+ * rounded queries.  Where scales is 255 the score is +infinity; where the table names no page, -infinity.
+ * Of the P pages that the token sees, the first first_pages and the last last_pages are taken, then those with the highest scores, of
+ * equal ones the first, until there are min(budget, P).
+ *   q [B, N, Hq, d] (dtype; q_layout);  q_len [B] i32 or NULL (= N)
+ *   chosen [B, N, H, budget] i32: entries of the block table in ascending order, then -1; rows i >= q_len[b] untouched
+ * first_pages, last_pages >= 0 with a sum of at most budget; N * G <= 2^20.  The same inputs give the same pages, whatever else differs.
+ * Errors: MD_EINVAL, MD_ESHAPE (limits, more than 2^23 - 1 tokens and heads), MD_EDTYPE, MD_EALIGN, MD_EALIAS, MD_EWORKSPACE, MD_EHIP. */
+size_t mustdrop_cache4_choose_workspace_bytes(int B, int N, int Hq, int H, int d, int max_pages, int page);
+
+int mustdrop_cache4_choose(
+    const void* q, md_dtype dtype, const int8_t* bounds, const uint8_t* scales, const int32_t* table, const int32_t* len, const int32_t* q_len,
+    int B, int N, int Hq, int H, int d, int n_pages, int page, int max_pages, int first_pages, int last_pages, int budget,
+    int32_t* chosen, const md_kv_layout* q_layout, void* workspace, size_t workspace_bytes, void* stream);
+
+/* mustdrop_cache4_attend over chosen pages: query row (b, i) sees, for K/V head h, those of the entries that it sees there which lie in
+ * the pages that chosen[b][i][h][0 .. budget-1] names.  An entry of chosen that is not in 0 .. max_pages-1, or not above every such entry
+ * before it in its list, takes no part: a page counts once.  With all pages chosen the two calls mean the same.  Everything else
+ * (values that are no numbers, rows that see nothing, limits of scores) as for mustdrop_cache4_attend; two calls on the same inputs with
+ * the same budget give the same bits.  Errors likewise, and MD_ESHAPE for 2^23 or more tiles of 16 query heads or parts of them. */
+size_t mustdrop_cache4_attend_chosen_workspace_bytes(int B, int N, int Hq, int H, int d, int budget, int page);
+
+int mustdrop_cache4_attend_chosen(
+    const void* q, md_dtype dtype, const void* cache, const int32_t* table, const int32_t* len, const int32_t* q_len, const uint8_t* keep,
+    const int32_t* chosen, int B, int N, int Hq, int H, int d, int n_pages, int page, int max_pages, int budget, float softmax_scale,
     void* out, float* lse, const md_kv_layout* q_layout, const md_kv_layout* out_layout,
     void* workspace, size_t workspace_bytes, void* stream);
 

@@ -13,6 +13,8 @@ from .binding import (  # noqa: F401
     mustdrop_prefill_filter_strided,
     cache4_buffer, cache4_pages_workspace, cache4_workspace, mustdrop_cache4_attend, mustdrop_cache4_pages, mustdrop_cache4_read,
     mustdrop_cache4_write,
+    Rotary, cache4_attend_chosen_workspace, cache4_bounds_buffer, cache4_choose_workspace, mustdrop_cache4_append, mustdrop_cache4_attend_chosen,
+    mustdrop_cache4_bounds, mustdrop_cache4_choose, mustdrop_rotate, rotary, rotary_table,
 )
 
 __all__ = [
@@ -24,4 +26,7 @@ __all__ = [
     "mustdrop_decode_keep_strided",
     "cache4_buffer", "cache4_pages_workspace", "cache4_workspace", "mustdrop_cache4_pages", "mustdrop_cache4_write",
     "mustdrop_cache4_read", "mustdrop_cache4_attend",
+    "Rotary", "rotary", "rotary_table", "mustdrop_rotate", "mustdrop_cache4_append",
+    "cache4_bounds_buffer", "cache4_choose_workspace", "cache4_attend_chosen_workspace",
+    "mustdrop_cache4_bounds", "mustdrop_cache4_choose", "mustdrop_cache4_attend_chosen",
 ]

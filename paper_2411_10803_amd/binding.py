@@ -23,6 +23,8 @@ EXPORTS = [
     "mustdrop_decode_keep_strided",
     "mustdrop_cache4_bytes", "mustdrop_cache4_pages_workspace_bytes", "mustdrop_cache4_pages", "mustdrop_cache4_write",
     "mustdrop_cache4_read", "mustdrop_cache4_attend_workspace_bytes", "mustdrop_cache4_attend",
+    "mustdrop_rotate", "mustdrop_cache4_append", "mustdrop_cache4_bounds", "mustdrop_cache4_choose_workspace_bytes", "mustdrop_cache4_choose",
+    "mustdrop_cache4_attend_chosen_workspace_bytes", "mustdrop_cache4_attend_chosen",
     "mustdrop_profile_start", "mustdrop_profile_stop",
 ]
 
@@ -30,6 +32,11 @@ EXPORTS = [
 class KvLayout(C.Structure):
     """md_kv_layout: element strides of the batch, token and head axes."""
     _fields_ = [("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class Rotary(C.Structure):
+    """md_rotary: how many pairs of channels turn, on how many axes, which channels a pair is, and each pair's axis."""
+    _fields_ = [("pairs", C.c_int32), ("axes", C.c_int32), ("adjacent", C.c_int32), ("axis", C.c_uint8 * 128)]
 
 
 class MustDropError(RuntimeError):
@@ -54,12 +61,14 @@ def library() -> C.CDLL:
         lib.mustdrop_version.restype = C.c_int
         for n in ("mustdrop_encode_merge_workspace_bytes", "mustdrop_prefill_filter_workspace_bytes",
                   "mustdrop_decode_evict_workspace_bytes", "mustdrop_cache4_bytes", "mustdrop_cache4_pages_workspace_bytes",
-                  "mustdrop_cache4_attend_workspace_bytes"):
+                  "mustdrop_cache4_attend_workspace_bytes", "mustdrop_cache4_choose_workspace_bytes",
+                  "mustdrop_cache4_attend_chosen_workspace_bytes"):
             getattr(lib, n).restype = C.c_size_t
         for n in ("mustdrop_encode_merge", "mustdrop_encode_merge_adaptive", "mustdrop_encode_merge_noalloc", "mustdrop_prefill_filter", "mustdrop_decode_evict", "mustdrop_decode_append",
                   "mustdrop_decode_keep", "mustdrop_prefill_filter_strided", "mustdrop_decode_evict_strided",
                   "mustdrop_decode_append_strided", "mustdrop_decode_keep_strided", "mustdrop_cache4_pages",
-                  "mustdrop_cache4_write", "mustdrop_cache4_read", "mustdrop_cache4_attend"):
+                  "mustdrop_cache4_write", "mustdrop_cache4_read", "mustdrop_cache4_attend", "mustdrop_rotate", "mustdrop_cache4_append",
+                  "mustdrop_cache4_bounds", "mustdrop_cache4_choose", "mustdrop_cache4_attend_chosen"):
             getattr(lib, n).restype = C.c_int
         _lib = lib
     return _lib
@@ -89,6 +98,11 @@ _SIGNATURES = {
     "mustdrop_cache4_write": "ppipp" + "i" * 6 + "pp",
     "mustdrop_cache4_read": "p" * 6 + "i" * 8 + "pp",
     "mustdrop_cache4_attend": "pi" + "p" * 5 + "i" * 8 + "f" + "p" * 4 + "pzp",
+    "mustdrop_rotate": "ppi" + "p" * 4 + "i" * 7 + "pipp" + "p" * 4 + "p",
+    "mustdrop_cache4_append": "pppi" + "p" * 5 + "i" * 9 + "pp" + "p" * 3 + "p",
+    "mustdrop_cache4_bounds": "p" * 6 + "i" * 7 + "p",
+    "mustdrop_cache4_choose": "pi" + "p" * 5 + "i" * 11 + "pp" + "pzp",
+    "mustdrop_cache4_attend_chosen": "pi" + "p" * 6 + "i" * 9 + "f" + "p" * 4 + "pzp",
 }
 _functions: Dict[str, object] = {}
 
@@ -596,6 +610,213 @@ def mustdrop_cache4_attend(q, cache, table, length, softmax_scale, out=None, lse
     _call("mustdrop_cache4_attend",
         qp, _dtype_code(q), _ptr(cache), _ptr(table), _ptr(length), _ptr(q_len), _ptr(keep),
         B, N, Hq, H, d, n_pages, page, max_pages, softmax_scale,
+        op, _ptr(lse), lq and C.byref(lq), lo and C.byref(lo),
+        _ptr(workspace), workspace.numel(), raw)
+    return out
+
+
+def rotary(sections, adjacent=False, axis=None) -> Rotary:
+    """How rows turn: sections[a] pairs of channels by axis a, one axis after the other, or pair i by axis[i] (0, 1, ..: as many entries as
+    there are pairs; sections then says how many axes there are and pairs in all).  A program keeps it."""
+    pairs = sum(int(n) for n in sections)
+    which = [a for a, n in enumerate(sections) for _ in range(int(n))] if axis is None else [int(a) for a in axis]
+    if len(which) != pairs or not 0 < pairs <= 128 or min(which) < 0 or max(which) >= len(sections) or min(sections) < 0:
+        raise ValueError(f"sections {list(sections)} and axis {axis} do not name an axis for each of 1 to 128 pairs")
+    return Rotary(pairs, len(sections), int(bool(adjacent)), (C.c_uint8 * 128)(*which))
+
+
+def rotary_table(n_pos, pairs, base=10000.0, device="cuda"):
+    """Cosines and sines [n_pos, pairs, 2] f32 of the angles p * base^(-i / pairs), worked out in 64 bits; a program keeps it.  (Any other
+    table of that shape will do, for other frequencies or scalings.)"""
+    import numpy as np
+    import torch
+    at = np.arange(n_pos, dtype=np.float64)[:, None] * float(base) ** (-np.arange(pairs, dtype=np.float64) / pairs)
+    return torch.from_numpy(np.stack([np.cos(at), np.sin(at)], axis=-1).astype(np.float32)).to(device)
+
+
+def _angles(positions, table, turn, index, B, N):
+    """Checks positions [axes, B, L], table [n_pos, pairs, 2] and index [B, N]; returns (L, n_pos)."""
+    import torch
+    _typed(torch.int32, positions=positions, index=index)
+    _typed(torch.float32, table=table)
+    L, n_pos = positions.shape[-1], table.shape[0]
+    _shaped("positions", positions, (turn.axes, B, L))
+    _shaped("table", table, (n_pos, turn.pairs, 2))
+    _shaped("index", index, (B, N))
+    return L, n_pos
+
+
+def _side(t, out, names):
+    """Pointers and layouts of rows [B, N, H, d] and of what they become (None: themselves)."""
+    if out is None:
+        out = t
+    _typed(t.dtype, **{names[1]: out})
+    _shaped(names[1], out, t.shape)
+    (p, lay), (o, out_lay) = _rows(t, names[0]), _rows(out, names[1])
+    return out, p, lay and C.byref(lay), o, out_lay and C.byref(out_lay)
+
+
+def mustdrop_rotate(q, positions, table, turn, k=None, q_out=None, k_out=None, index=None, rows=None, inverse=False, stream=None):
+    """Rows q [B, N, Hq, d] and k [B, N, H, d] or None (bf16 / f32, any layout) turned by their positions [axes, B, L] int32 (row (b, i) at
+    [:, b, index[b, i]], or [:, b, i] without index [B, N] int32), with table [n_pos, pairs, 2] f32 (rotary_table) and turn = rotary(..).  q_out and
+    k_out: None for in place.  rows [B] int32: rows from there on stay.  inverse: the way back.  Returns (q_out, k_out)."""
+    import torch
+    B, N, Hq, d = q.shape
+    if k is None and k_out is not None:
+        raise ValueError("k_out without k")
+    L, n_pos = _angles(positions, table, turn, index, B, N)
+    _typed(torch.int32, rows=rows)
+    _shaped("rows", rows, (B,))
+    q_out, qp, ql, qo, qol = _side(q, q_out, ("q", "q_out"))
+    H, kp, kl, ko, kol = 0, None, None, None, None
+    if k is not None:
+        H = k.shape[2]
+        _typed(q.dtype, k=k)
+        _shaped("k", k, (B, N, H, d))
+        k_out, kp, kl, ko, kol = _side(k, k_out, ("k", "k_out"))
+    raw = _here(stream, q, k, positions, table, q_out, k_out, index, rows)
+    _call("mustdrop_rotate",
+        qp, kp, _dtype_code(q), _ptr(positions), _ptr(index), _ptr(table), _ptr(rows),
+        B, N, L, Hq, H, d, n_pos, C.byref(turn), int(bool(inverse)), qo, ko, ql, kl, qol, kol, raw)
+    return q_out, k_out
+
+
+def mustdrop_cache4_append(q, k_new, v_new, positions, table, turn, slots, cache, q_out=None, index=None, stream=None):
+    """Rows k_new, v_new [B, N, H, d] (bf16 / f32 views of one layout) into the cache at slots [B, N], k_new turned on the way; q
+    [B, N, Hq, d] (or None) turned into q_out (None: in place), which is returned.  Rows without a slot stay out, and their queries.  For
+    positions, table, turn and index see mustdrop_rotate."""
+    import torch
+    B, N, H, d = k_new.shape
+    n_pages, heads, page = _pool(cache, d)
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
+    L, n_pos = _angles(positions, table, turn, index, B, N)
+    _typed(torch.int32, slots=slots)
+    _shaped("slots", slots, (B, N))
+    kp, vp, lay = _row_pair(k_new, v_new, ("k_new", "v_new"))
+    if heads != H:
+        raise ValueError(f"rows of {H} heads for a cache of {heads} heads")
+    Hq, qp, ql, qo, qol = 0, None, None, None, None
+    if q is not None:
+        Hq = q.shape[2]
+        _typed(k_new.dtype, q=q)
+        _shaped("q", q, (B, N, Hq, d))
+        q_out, qp, ql, qo, qol = _side(q, q_out, ("q", "q_out"))
+    raw = _here(stream, k_new, v_new, q, q_out, positions, table, slots, cache, index)
+    _call("mustdrop_cache4_append",
+        qp, kp, vp, _dtype_code(k_new), _ptr(positions), _ptr(index), _ptr(table), _ptr(slots), _ptr(cache),
+        B, N, L, Hq, H, d, n_pos, n_pages, page, C.byref(turn), qo, ql, lay, qol, raw)
+    return q_out
+
+
+def cache4_bounds_buffer(n_pages, H, d, device="cuda"):
+    """What mustdrop_cache4_bounds writes: bounds int8 [n_pages, H, 2, d] and scales uint8 [n_pages, H]."""
+    import torch
+    return torch.zeros((n_pages, H, 2, d), dtype=torch.int8, device=device), torch.zeros((n_pages, H), dtype=torch.uint8, device=device)
+
+
+def _bounds(bounds, scales):
+    """(pages, heads, channels) of a cache's bounds."""
+    import torch
+    _typed(torch.int8, bounds=bounds)
+    _typed(torch.uint8, scales=scales)
+    n_pages, H, two, d = bounds.shape
+    _shaped("bounds", bounds, (n_pages, H, 2, d))
+    _shaped("scales", scales, (n_pages, H))
+    return n_pages, H, d
+
+
+def mustdrop_cache4_bounds(cache, table, length, n, bounds, scales, first=None, stream=None):
+    """Bounds of the keys of the pages that hold entries first .. first + n - 1 (below length) of every sample, into bounds int8
+    [n_pages, H, 2, d] and scales uint8 [n_pages, H] (cache4_bounds_buffer)."""
+    import torch
+    pages, H, d = _bounds(bounds, scales)
+    n_pages, heads, page = _pool(cache, d)
+    if (pages, H) != (n_pages, heads):
+        raise ValueError(f"bounds of {pages} pages and {H} heads for a cache of {n_pages} and {heads}")
+    B, max_pages = table.shape
+    _typed(torch.int32, table=table, length=length, first=first)
+    _shaped("length", length, (B,))
+    _shaped("first", first, (B,))
+    raw = _here(stream, cache, table, length, bounds, scales, first)
+    _call("mustdrop_cache4_bounds",
+        _ptr(cache), _ptr(table), _ptr(length), _ptr(first), _ptr(bounds), _ptr(scales), B, int(n), H, d, n_pages, page, max_pages, raw)
+
+
+def cache4_choose_workspace(q, bounds, table, page=16):
+    """Workspace of mustdrop_cache4_choose for queries [B, N, Hq, d] on these bounds with block tables [B, max_pages]."""
+    B, N, Hq, d = q.shape
+    n = library().mustdrop_cache4_choose_workspace_bytes(B, N, Hq, bounds.shape[1], d, table.shape[1], page)
+    return _workspace(n, q.device)
+
+
+def mustdrop_cache4_choose(q, bounds, scales, table, length, page, chosen, q_len=None, first_pages=0, last_pages=1, workspace=None, stream=None):
+    """The pages that each of the last q_len tokens of every sample is to read, for each K/V head: chosen [B, N, H, budget] int32
+    receives entries of the block table in ascending order, then -1.  q [B, N, Hq, d] (bf16 / f32, any layout); bounds and scales from
+    mustdrop_cache4_bounds; the first first_pages and the last last_pages are always among them.  Returns chosen."""
+    import torch
+    B, N, Hq, d = q.shape
+    n_pages, H, channels = _bounds(bounds, scales)
+    if channels != d:
+        raise ValueError(f"bounds of {channels} channels for queries of {d}")
+    max_pages, budget = table.shape[-1], chosen.shape[-1]
+    _typed(torch.int32, table=table, length=length, chosen=chosen, q_len=q_len)
+    _shaped("table", table, (B, max_pages))
+    _shaped("length", length, (B,))
+    _shaped("q_len", q_len, (B,))
+    _shaped("chosen", chosen, (B, N, H, budget))
+    raw = _here(stream, q, bounds, scales, table, length, chosen, q_len, workspace)
+    if workspace is None:
+        with _made_on(stream):
+            workspace = cache4_choose_workspace(q, bounds, table, int(page))
+    qp, lq = _rows(q, "q")
+    _call("mustdrop_cache4_choose",
+        qp, _dtype_code(q), _ptr(bounds), _ptr(scales), _ptr(table), _ptr(length), _ptr(q_len),
+        B, N, Hq, H, d, n_pages, int(page), max_pages, int(first_pages), int(last_pages), budget,
+        _ptr(chosen), lq and C.byref(lq), _ptr(workspace), workspace.numel(), raw)
+    return chosen
+
+
+def cache4_attend_chosen_workspace(q, cache, chosen):
+    """Workspace of mustdrop_cache4_attend_chosen for queries [B, N, Hq, d] on this pool with lists [B, N, H, budget]."""
+    B, N, Hq, d = q.shape
+    _, H, page = _pool(cache, d)
+    n = library().mustdrop_cache4_attend_chosen_workspace_bytes(B, N, Hq, H, d, chosen.shape[3], page)
+    return _workspace(n, q.device)
+
+
+def mustdrop_cache4_attend_chosen(q, cache, table, length, chosen, softmax_scale, out=None, lse=None, q_len=None, keep=None, workspace=None, stream=None):
+    """mustdrop_cache4_attend over the pages that chosen [B, N, H, budget] int32 names for each token and K/V head (ascending; what does
+    not ascend or is no entry of the table does not count).  Returns out (made as zeros if None)."""
+    import torch
+    B, N, Hq, d = q.shape
+    n_pages, H, page = _pool(cache, d)
+    max_pages, budget = table.shape[-1], chosen.shape[-1]
+    if out is None:
+        with _made_on(stream):
+            out = torch.zeros((B, N, Hq, d), dtype=q.dtype, device=q.device)
+    _typed(torch.int32, table=table, length=length, q_len=q_len, chosen=chosen)
+    if lse is not None:
+        _typed(torch.float32, lse=lse)
+        _shaped("lse", lse, (B, Hq, N))
+    if keep is not None:
+        _typed(torch.uint8, keep=keep)
+        _shaped("keep", keep, (B, max_pages * page))
+    _typed(q.dtype, out=out)
+    _shaped("out", out, q.shape)
+    _shaped("table", table, (B, max_pages))
+    _shaped("length", length, (B,))
+    _shaped("q_len", q_len, (B,))
+    _shaped("chosen", chosen, (B, N, H, budget))
+    raw = _here(stream, q, cache, table, length, chosen, out, lse, q_len, keep, workspace)
+    if workspace is None:
+        with _made_on(stream):
+            workspace = cache4_attend_chosen_workspace(q, cache, chosen)
+    qp, lq = _rows(q, "q")
+    op, lo = _rows(out, "out")
+    _call("mustdrop_cache4_attend_chosen",
+        qp, _dtype_code(q), _ptr(cache), _ptr(table), _ptr(length), _ptr(q_len), _ptr(keep), _ptr(chosen),
+        B, N, Hq, H, d, n_pages, page, max_pages, budget, softmax_scale,
         op, _ptr(lse), lq and C.byref(lq), lo and C.byref(lo),
         _ptr(workspace), workspace.numel(), raw)
     return out

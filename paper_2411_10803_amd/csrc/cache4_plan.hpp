@@ -115,5 +115,23 @@ inline C4Attend c4_attend(bool f32, int B, int N, int G, int H, int d, int64_t c
     return a;
 }
 
+// Pages that N consecutive entries may lie in.
+inline int c4_span(int N, int page, int max_pages) {
+    const int64_t most = ((int64_t)N + page - 2) / page + 1;
+    return most < max_pages ? (int)most : max_pages;
+}
+
+// How the attention over chosen pages is cut: `splits` parts of a list of `budget` pages, a block each; `most` entries of the list to a
+// part.  `units`: tiles of 16 query heads of all tokens and K/V heads.
+struct C4Chosen { int splits, most; };
+constexpr int kC4ListMost = 1024;                    // entries of a part, which lie in LDS
+inline C4Chosen c4_chosen(int64_t units, int budget, int page) {
+    C4Chosen c;
+    c.splits = (budget + kC4ListMost - 1) / kC4ListMost;
+    c.most = (budget + c.splits - 1) / c.splits;
+    (void)units; (void)page;
+    return c;
+}
+
 }  // namespace
 }  // namespace md
