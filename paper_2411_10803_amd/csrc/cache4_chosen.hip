@@ -18,26 +18,37 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------------------------------------ bounds
 
-// Maxima over lanes that differ in bit S, of 2 S numbers: lanes with the bit set go on with the upper S, the others with the lower.
-template <int S>
-__device__ __forceinline__ void halve(float (&v)[64], int lane) {
+// Of 2 S numbers S: maxima over lanes that differ in bit BIT; lanes with the bit set go on with the upper half, the others with the lower.
+template <int BIT, int S>
+__device__ __forceinline__ void halve(float (&v)[16], int lane) {
 #pragma unroll
     for (int c = 0; c < S; ++c) {
-        const bool up = lane & S;
-        const float keep = up ? v[c + S] : v[c], give = up ? v[c] : v[c + S];
-        v[c] = fmaxf(keep, __shfl_xor(give, S, kWave));
+        uint32_t x = __float_as_uint(v[c]), y = __float_as_uint(v[c + S]);
+        if constexpr (BIT == 8) {
+            const bool up = lane & 8;
+            const uint32_t give = up ? x : y;
+            x = up ? y : x;
+            y = (uint32_t)dpp_i<0x128>((int)give, (int)give);
+        } else {                                     // the two registers change halves: one instruction
+            const auto r = BIT == 32 ? __builtin_amdgcn_permlane32_swap(x, y, false, false) : __builtin_amdgcn_permlane16_swap(x, y, false, false);
+            x = r[0];
+            y = r[1];
+        }
+        v[c] = fmaxf(__uint_as_float(x), __uint_as_float(y));
     }
 }
 
-// A wave per page and head.  A lane loads 16 bytes, 32 channels of one scale, of every 16th (d = 64: 32nd) token, and keeps the largest
-// of their values and of the values with their signs turned: 64 numbers.  The lanes of one group then halve these among them, until each
-// has 4 (2) channels of the one kind, which is a word (half of one) of the result.
+// A wave per page and head.  Sixteen (d = 64: eight) lanes side by side have the channels of one token, eight each: of all tokens they keep the
+// largest values and the largest with the sign turned, 16 numbers.  The four (eight) lanes of the same channels then halve these among
+// them until each has 4 (2) of the one kind, which is a word (half of one) of the result.  (Sixteen bytes to a lane are fewer loads, but 64
+// numbers to halve over sixteen lanes: 22 us for the bounds of 16 x up to 5888 entries of 8 heads instead of @@.)
+constexpr int kBoundsAhead = 8;                      // tokens of a lane that are on their way together
 template <int D>
 __global__ __launch_bounds__(256) void cache4_bounds_kernel(
     const uint8_t* __restrict__ cache, const int32_t* __restrict__ table, const int32_t* __restrict__ len, const int32_t* __restrict__ first,
     int8_t* __restrict__ bounds, uint8_t* __restrict__ scales, Pool p, int units, int N, FastDiv heads, FastDiv span)
 {
-    constexpr int GROUPS = D / 32, TOKENS = kWave / GROUPS;
+    constexpr int PARTS = D / 8, TOKENS = kWave / PARTS;
     const int unit = (int)blockIdx.x * 4 + wave_id(), lane = lane_id();
     if (unit >= units) return;
     const int bx = heads.div(unit), h = unit - bx * heads.d, b = span.div(bx), x = bx - b * span.d;
@@ -48,39 +59,44 @@ __global__ __launch_bounds__(256) void cache4_bounds_kernel(
     if (id < 0) return;
     const int live = min(length - (int)(e << p.page_shift), p.page);
     const uint8_t* base = cache + ((long)id * p.H + h) * p.stride;
-    const int group = lane & (GROUPS - 1), t0 = lane / GROUPS;
-    float v[64];                                     // largest, then largest of the negative, of 32 channels
+    const int part = lane & (PARTS - 1), t0 = lane / PARTS;
+    float v[16];                                     // largest, then largest of the negative, of 8 channels
 #pragma unroll
-    for (int c = 0; c < 64; ++c) v[c] = -INFINITY;
-    bool bad = false;
-    for (int t = t0; t < live; t += TOKENS) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(base + c4_k_codes(t, D) + group * 16);
-        const uint32_t code = base[c4_k_scales(p.page, t, D) + group];
-        const float s = scale_of(code);
-        bad |= code >= 253;                          // (6 * 2^126 is no number of fp32)
+    for (int c = 0; c < 16; ++c) v[c] = -INFINITY;
+    uint32_t top = 0;                                // the largest scale
+    for (int t = t0; t - t0 < live; t += TOKENS * kBoundsAhead) {
+        uint32_t w[kBoundsAhead], code[kBoundsAhead];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const f32x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[j], s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[j], s, 1),
-                                __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[j], s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[j], s, 3)};
+        for (int y = 0; y < kBoundsAhead; ++y) {     // (the last token in the place of those behind it)
+            const int at = min(t + y * TOKENS, live - 1);
+            w[y] = *reinterpret_cast<const uint32_t*>(base + c4_k_codes(at, D) + part * 4);
+            code[y] = base[c4_k_scales(p.page, at, D) + part / 4];
+        }
+#pragma unroll
+        for (int y = 0; y < kBoundsAhead; y += 2) {
+            const float s = scale_of(code[y]), s2 = scale_of(code[y + 1]);
+            top = max(top, max(code[y], code[y + 1]));
+            const f32x2 a[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[y], s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[y], s, 1),
+                                __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[y], s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[y], s, 3)};
+            const f32x2 z[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[y + 1], s2, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[y + 1], s2, 1),
+                                __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[y + 1], s2, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[y + 1], s2, 3)};
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
-                const float f = y[c >> 1][c & 1];
-                v[j * 8 + c] = fmaxf(v[j * 8 + c], f);
-                v[32 + j * 8 + c] = fmaxf(v[32 + j * 8 + c], -f);
+                const float f = a[c >> 1][c & 1], g = z[c >> 1][c & 1];
+                asm("v_max3_f32 %0, %0, %1, %2" : "+v"(v[c]) : "v"(f), "v"(g));
+                asm("v_max3_f32 %0, %0, -%1, -%2" : "+v"(v[8 + c]) : "v"(f), "v"(g));
             }
         }
     }
-    halve<32>(v, lane);
-    halve<16>(v, lane);
-    halve<8>(v, lane);
-    halve<4>(v, lane);
-    if (D == 64) halve<2>(v, lane);
+    halve<32, 8>(v, lane);
+    halve<16, 4>(v, lane);
+    if (D == 64) halve<8, 2>(v, lane);
     constexpr int LEFT = D == 128 ? 4 : 2;
     float most = v[0];
 #pragma unroll
     for (int c = 1; c < LEFT; ++c) most = fmaxf(most, v[c]);
     most = wave_max(most);                           // the largest magnitude: of a channel's largest and smallest value one has it
-    const bool none = __any(bad);
+    const bool none = __any(top >= 253);             // (6 * 2^126 is no number of fp32)
     const int ex = most > 0.f ? max((int)(__float_as_uint(most) >> 23) - 127 - 6, -126) : -126;
     const bool least = lane & 32;
     uint32_t word = 0;
@@ -89,7 +105,7 @@ __global__ __launch_bounds__(256) void cache4_bounds_kernel(
         const int up = none ? 0 : (int)ceilf(__builtin_amdgcn_ldexpf(v[c], -ex));
         word |= (uint32_t)((least ? -up : up) & 0xFF) << (8 * c);
     }
-    const int channel = group * 32 + (lane & 16) + (lane & 8) + (lane & 4) + (D == 64 ? (lane & 2) : 0);
+    const int channel = part * 8 + (lane & 16 ? 4 : 0) + (D == 64 && (lane & 8) ? 2 : 0);
     int8_t* to = bounds + ((long)id * p.H + h) * (2 * D) + (least ? D : 0) + channel;
     if (D == 128) *reinterpret_cast<uint32_t*>(to) = word;
     else *reinterpret_cast<uint16_t*>(to) = (uint16_t)word;
@@ -118,165 +134,469 @@ __device__ __forceinline__ int pages_seen(const Choose& A, int b, int i) {
     return c4_pages_of(min(max(length - nq + i + 1, 0), length), A.page_shift);
 }
 
-// The whole numbers of a lane's 16 channels of one query, as bytes: those above 0, and those below.
-__device__ __forceinline__ void whole_bytes(const float (&x)[16], int shift, bool ok, i32x4& above, i32x4& below) {
+// W channels of a query as they lie in memory.
+template <int W, bool F32>
+struct Raw {
+    static constexpr int WORDS = F32 ? W : W / 2;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(const void* base, long at) {
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(static_cast<const char*>(base) + at * (F32 ? 4 : 2));
+        if constexpr (WORDS == 2) {
+            const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+            w[0] = v[0];
+            w[1] = v[1];
+        } else {
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        uint32_t a = 0, b = 0;
+            for (int i = 0; i < WORDS / 4; ++i) {
+                const u32x4 v = reinterpret_cast<const u32x4*>(p)[i];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int n = ok ? c4_clamp((int)rintf(__builtin_amdgcn_ldexpf(x[4 * w + j], shift)), -127, 127) : 0;
-            a |= (uint32_t)max(n, 0) << (8 * j);
-            b |= (uint32_t)(min(n, 0) & 0xFF) << (8 * j);
-        }
-        above[w] = (int)a;
-        below[w] = (int)b;
-    }
-}
-
-template <bool F32>
-__device__ __forceinline__ void load_16(const void* base, long at, float (&x)[16]) {
-    if (F32) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4 v = *reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + at + 4 * i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[4 * i + j] = v[j];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const u32x4 v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + at + 8 * i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { x[8 * i + 2 * j] = bf16_lo(v[j]); x[8 * i + 2 * j + 1] = bf16_hi(v[j]); }
-        }
-    }
-}
-
-// A wave: 16 query rows (the G heads of some tokens, filled up with zeros to a power of two) against TILES tiles of 16 pages.  Lane (n, lb)
-// has bytes lb * 16 .. + 15 of every 64 of row n of either operand.
-constexpr int kScoreTiles = 4;
-template <int D, bool F32>
-__global__ __launch_bounds__(256) void cache4_score_kernel(Choose A, FastDiv tiles, FastDiv heads)
-{
-    constexpr int Y = D / 64;
-    const int lane = lane_id(), n = lane & 15, lb = lane >> 4;
-    const int bh = tiles.div(blockIdx.x), tile = blockIdx.x - bh * tiles.d, b = heads.div(bh), h = bh - b * heads.d;
-    const int nq = A.q_len ? c4_clamp(A.q_len[b], 0, A.N) : A.N;
-    const int i = tile * A.per + n / A.lanes, g0 = n & (A.lanes - 1), last = min(nq, (tile + 1) * A.per) - 1;
-    if (tile * A.per >= nq) return;
-    const int seen = pages_seen(A, b, last), first = ((int)blockIdx.y * 4 + wave_id()) * kScoreTiles;
-    if (first * 16 >= seen) return;
-    // the largest magnitude of a token's queries
-    uint32_t most = 0;
-    for (int s = 0; s < A.subs; ++s) {
-        const int g = s * 16 + g0;
-        if (i >= nq || g >= A.G) continue;
-#pragma unroll
-        for (int y = 0; y < Y; ++y) {
-            float x[16];
-            load_16<F32>(A.q, (long)b * A.ql.batch + (long)i * A.ql.token + (long)(h * A.G + g) * A.ql.head + y * 64 + lb * 16, x);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) most = max(most, __float_as_uint(x[j]) & 0x7FFFFFFFu);
-        }
-    }
-    most = max(most, (uint32_t)__shfl_xor((int)most, 16, kWave));
-    most = max(most, (uint32_t)__shfl_xor((int)most, 32, kWave));
-    for (int x = 1; x < A.lanes; x <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, x, kWave));
-    const bool ok = most > 0 && most < 0x7F800000u;
-    const int shift = 7 - __builtin_amdgcn_frexp_expf(__uint_as_float(most));
-    i32x4 acc[kScoreTiles] = {};
-    int code[kScoreTiles];                           // of the lane's page n in each tile: its scale; 256: no page
-#pragma unroll
-    for (int t = 0; t < kScoreTiles; ++t) code[t] = 256;
-    for (int s = 0; s < A.subs; ++s) {
-        const int g = s * 16 + g0;
-        i32x4 above[Y], below[Y];
-#pragma unroll
-        for (int y = 0; y < Y; ++y) {
-            float x[16] = {};
-            if (i < nq && g < A.G) load_16<F32>(A.q, (long)b * A.ql.batch + (long)i * A.ql.token + (long)(h * A.G + g) * A.ql.head + y * 64 + lb * 16, x);
-            whole_bytes(x, shift, ok, above[y], below[y]);
-        }
-#pragma unroll
-        for (int t = 0; t < kScoreTiles; ++t) {
-            const int e = (first + t) * 16 + n;
-            i32x4 hi[Y] = {}, lo[Y] = {};
-            if (e < seen) {
-                const int id = c4_page_id(A.table[(long)b * A.max_pages + e], A.n_pages);
-                if (id >= 0) {
-                    const long at = (long)id * A.H + h;
-                    code[t] = A.scales[at];
-                    const int8_t* from = A.bounds + at * (2 * D) + lb * 16;
-#pragma unroll
-                    for (int y = 0; y < Y; ++y) {
-                        hi[y] = *reinterpret_cast<const i32x4*>(from + y * 64);
-                        lo[y] = *reinterpret_cast<const i32x4*>(from + D + y * 64);
-                    }
-                }
+                for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
             }
+        }
+    }
+    __device__ __forceinline__ float at(int j) const { return F32 ? __uint_as_float(w[j]) : j & 1 ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]); }
+    __device__ __forceinline__ uint32_t largest() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < W; ++j) m = max(m, __float_as_uint(at(j)) & 0x7FFFFFFFu);
+        return m;
+    }
+    // Their whole numbers as bytes: those above 0, and those below with their sign turned.  (The hardware's conversion to a byte takes what
+    // is below 0 as 0.)
+    __device__ __forceinline__ void whole(int shift, uint32_t ok, uint32_t (&above)[W / 4], uint32_t (&below)[W / 4]) const {
+#pragma unroll
+        for (int x = 0; x < W / 4; ++x) {
+            uint32_t a = 0, b = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float n = __builtin_amdgcn_fmed3f(__builtin_rintf(__builtin_amdgcn_ldexpf(at(4 * x + j), shift)), -127.f, 127.f);
+                a = __builtin_amdgcn_cvt_pk_u8_f32(n, j, a);
+                b = __builtin_amdgcn_cvt_pk_u8_f32(-n, j, b);
+            }
+            above[x] = a & ok;
+            below[x] = b & ok;
+        }
+    }
+};
+// The step of numbers whose largest magnitude has these bits, as a shift; and whether they count at all.
+__device__ __forceinline__ int whole_shift(uint32_t most) { return 7 - __builtin_amdgcn_frexp_expf(__uint_as_float(most)); }
+__device__ __forceinline__ uint32_t whole_ok(uint32_t most) { return most > 0 && most < 0x7F800000u ? ~0u : 0u; }
+
+// Of lanes side by side, `lanes` (a power of two up to 16) of them: the largest, the sum.  `m`: all ones for as many steps as that takes.
+struct Steps {
+    uint32_t m[4];
+    __device__ __forceinline__ explicit Steps(int lanes) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) m[x] = lanes > 1 << x ? ~0u : 0u;
+    }
+    __device__ __forceinline__ uint32_t largest(uint32_t v) const {
+        v = max(v, (uint32_t)dpp_i<0xB1>((int)v, (int)v) & m[0]);
+        v = max(v, (uint32_t)dpp_i<0x4E>((int)v, (int)v) & m[1]);
+        v = max(v, (uint32_t)dpp_i<0x141>((int)v, (int)v) & m[2]);
+        return max(v, (uint32_t)dpp_i<0x140>((int)v, (int)v) & m[3]);
+    }
+    __device__ __forceinline__ int sum(int v) const {
+        v += dpp_i<0xB1>(v, v) & (int)m[0];
+        v += dpp_i<0x4E>(v, v) & (int)m[1];
+        v += dpp_i<0x141>(v, v) & (int)m[2];
+        return v + (dpp_i<0x140>(v, v) & (int)m[3]);
+    }
+};
+
+// 16 query rows (the G heads of some tokens, filled up with zeros to a power of two; MULTI, more than 16 heads: one 16 after the other) against
+// T tiles of 16 pages at a time, by a wave of a block of 256 threads.  Lane (n, lb) has bytes lb * 16 .. + 15 of every 64 of row n of either
+// operand.  A block's waves turn the queries into whole numbers together and share them through LDS (each for itself: 64 x up to 4096 entries
+// of 32 heads 13.2 us); MULTI: each for itself.
+// There are few instructions to a byte, and nothing else to do while a wave waits: what does not depend on the sample's length is asked for
+// together with it, and nothing is loaded under a condition of a lane (rows and pages that are not there are others' in their place, and
+// count as nothing).
+template <int D, bool F32, bool MULTI, int T>
+struct Scorer {
+    static constexpr int Y = D / 64, W = D / 16, PITCH = D + 16;     // channels of a thread's share; bytes of a row in LDS
+    static constexpr int LDS = 16 * 4 + 2 * 16 * PITCH;
+    const Choose& A;
+    Steps steps;
+    int b, h, tile, i, g0, n, lb, length, nq;
+    Raw<W, F32> share;                               // of row threadIdx.x / 16
+    int entry[T], mine[T];                           // of the block table, for the tiles that come next: of page n, and of 4 lb + n % 4
+    i32x4 above[Y], below[Y], hi[T][Y], lo[T][Y];
+    int code[T];                                     // of page 4 lb + n % 4 in each tile: its scale; 256: no page
+
+    __device__ __forceinline__ Scorer(const Choose& A_, int b_, int h_, int tile_, int first) : A(A_), steps(A_.lanes), b(b_), h(h_), tile(tile_) {
+        const int lane = lane_id();
+        n = lane & 15;
+        lb = lane >> 4;
+        i = tile * A.per + n / A.lanes;
+        g0 = n & (A.lanes - 1);
+        length = uniform(A.len)[b];
+        nq = uniform(A.q_len ? A.q_len : A.len)[b];
+        if (!MULTI) share.load(A.q, query_at((int)threadIdx.x >> 4, 0) + (threadIdx.x & 15) * W);
+        ask(first);
+        asm volatile("" : "+s"(length), "+s"(nq));   // (asked for here, and not where a condition lets them)
+#pragma unroll
+        for (int t = 0; t < T; ++t) asm volatile("" : "+v"(entry[t]), "+v"(mine[t]));
+        length = c4_clamp(length, 0, A.max_pages << A.page_shift);
+        nq = A.q_len ? c4_clamp(nq, 0, A.N) : A.N;
+    }
+    // Pages that row `row` sees.
+    __device__ __forceinline__ int seen_by(int row) const { return c4_pages_of(min(max(length - nq + row + 1, 0), length), A.page_shift); }
+    // Where a row's query begins, or another one's where there is no such row.
+    __device__ __forceinline__ long query_at(int row, int sub) const {
+        const int token = min(tile * A.per + row / A.lanes, A.N - 1), g = min(sub * 16 + (row & (A.lanes - 1)), A.G - 1);
+        return (long)b * A.ql.batch + (long)token * A.ql.token + (long)(h * A.G + g) * A.ql.head;
+    }
+    __device__ __forceinline__ bool there(int row, int sub) const { return tile * A.per + row / A.lanes < nq && sub * 16 + (row & (A.lanes - 1)) < A.G; }
+
+    __device__ __forceinline__ void ask(int first) {
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const int32_t* row = A.table + (long)b * A.max_pages;
+            entry[t] = row[min((first + t) * 16 + n, A.max_pages - 1)];
+            mine[t] = row[min((first + t) * 16 + 4 * lb + (n & 3), A.max_pages - 1)];
+        }
+    }
+    // Bounds of the tiles whose entries have been asked for, on their way; then the entries of tiles next ..
+    __device__ __forceinline__ void fetch(int next) {
+        const auto page = [&](int e) { return (long)((uint32_t)e < (uint32_t)A.n_pages ? e : 0) * A.H + h; };
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const int8_t* from = A.bounds + page(entry[t]) * (2 * D) + lb * 16;
+            code[t] = A.scales[page(mine[t])] | ((uint32_t)mine[t] < (uint32_t)A.n_pages ? 0 : 256);
 #pragma unroll
             for (int y = 0; y < Y; ++y) {
-                acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(hi[y], above[y], acc[t], 0, 0, 0);
-                acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(lo[y], below[y], acc[t], 0, 0, 0);
+                hi[t][y] = *reinterpret_cast<const i32x4*>(from + y * 64);
+                lo[t][y] = *reinterpret_cast<const i32x4*>(from + D + y * 64);
             }
         }
+        ask(next);
+        __builtin_amdgcn_sched_barrier(0);
     }
-    float* to = A.scores + ((long)bh * A.N + i) * A.pitch;
+    // The queries' whole numbers: by all of the block, or by the wave for itself.  `lds`: LDS bytes.
+    __device__ __forceinline__ void queries(char* lds) {
+        uint32_t* s_most = reinterpret_cast<uint32_t*>(lds);
+        char* s_whole = lds + 64;
+        const int row = (int)threadIdx.x >> 4, part = threadIdx.x & 15;
+        uint32_t most = there(row, 0) ? share.largest() : 0u;
+        most = Steps(16).largest(most);
+        if (part == 0) s_most[row] = most;
+        block_sync_lds();
+        most = steps.largest(s_most[n]);
+        most = (uint32_t)__shfl((int)most, row & 15, kWave);
+        uint32_t a[W / 4], c[W / 4];
+        share.whole(whole_shift(most), there(row, 0) ? whole_ok(most) : 0u, a, c);
+        uint32_t* to = reinterpret_cast<uint32_t*>(s_whole + row * PITCH + part * W);
 #pragma unroll
-    for (int t = 0; t < kScoreTiles; ++t) {
-        const int e0 = (first + t) * 16 + 4 * lb;    // acc[t][x]: page e0 + x, query n
-        f32x4 score;
+        for (int x = 0; x < W / 4; ++x) { to[x] = a[x]; to[16 * PITCH / 4 + x] = c[x]; }
+        block_sync_lds();
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            int sum = acc[t][x];
-            for (int m = 1; m < A.lanes; m <<= 1) sum += __shfl_xor(sum, m, kWave);
-            const int c = __shfl(code[t], 4 * lb + x, kWave);
-            score[x] = c == 256 ? -INFINITY : c == 255 ? INFINITY : __builtin_amdgcn_ldexpf((float)sum, c - 127);
+        for (int y = 0; y < Y; ++y) {
+            above[y] = *reinterpret_cast<const i32x4*>(s_whole + n * PITCH + lb * 16 + y * 64);
+            below[y] = *reinterpret_cast<const i32x4*>(s_whole + (16 + n) * PITCH + lb * 16 + y * 64);
         }
-        if (i < nq && g0 == 0 && e0 < seen) *reinterpret_cast<f32x4*>(to + e0) = score;
     }
+    __device__ __forceinline__ void multiply(i32x4 (&up)[T], i32x4 (&down)[T]) const {
+#pragma unroll
+        for (int y = 0; y < Y; ++y)
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
+                up[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(hi[t][y], above[y], up[t], 0, 0, 0);
+                down[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(lo[t][y], below[y], down[t], 0, 0, 0);
+            }
+    }
+    __device__ __forceinline__ void multiply_many(i32x4 (&up)[T], i32x4 (&down)[T]) {
+        Raw<16, F32> x;
+        uint32_t most = 0;
+        for (int s = 0; s < A.subs; ++s)
+            for (int y = 0; y < Y; ++y) {
+                x.load(A.q, query_at(n, s) + lb * 16 + y * 64);
+                most = max(most, there(n, s) ? x.largest() : 0u);
+            }
+        most = max(most, (uint32_t)__shfl_xor((int)most, 16, kWave));
+        most = max(most, (uint32_t)__shfl_xor((int)most, 32, kWave));
+        most = steps.largest(most);
+        for (int s = 0; s < A.subs; ++s) {
+#pragma unroll
+            for (int y = 0; y < Y; ++y) {
+                uint32_t a[4], c[4];
+                x.load(A.q, query_at(n, s) + lb * 16 + y * 64);
+                x.whole(whole_shift(most), there(n, s) ? whole_ok(most) : 0u, a, c);
+                above[y] = i32x4{(int)a[0], (int)a[1], (int)a[2], (int)a[3]};
+                below[y] = i32x4{(int)c[0], (int)c[1], (int)c[2], (int)c[3]};
+            }
+            multiply(up, down);
+        }
+    }
+
+    // Scores of the pages of tiles first .. first + T - 1 (below `seen`), whose bounds have been fetched: each(token, page, four scores), by one
+    // lane of a token's and for four pages at a time.
+    template <class Each>
+    __device__ __forceinline__ void score(int first, int seen, Each each) {
+        i32x4 up[T] = {}, down[T] = {};
+        if (MULTI) multiply_many(up, down);
+        else multiply(up, down);
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const int e0 = (first + t) * 16 + 4 * lb;                // up[t][x]: page e0 + x, query n
+            i32x4 sum = up[t] - down[t];
+            if (A.lanes > 1) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) sum[x] = steps.sum(sum[x]);
+            }
+            const int c[4] = {dpp_i<0x00>(code[t], code[t]), dpp_i<0x55>(code[t], code[t]), dpp_i<0xAA>(code[t], code[t]), dpp_i<0xFF>(code[t], code[t])};
+            f32x4 score;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const float v = __builtin_amdgcn_ldexpf((float)sum[x], c[x] - 127);
+                score[x] = c[x] < 255 ? v : c[x] == 255 ? INFINITY : -INFINITY;
+            }
+            if (i < nq && g0 == 0 && e0 < seen) each(i, e0, score);
+        }
+    }
+};
+
+// Scores into the workspace: a wave takes kScoreTiles tiles of pages.
+constexpr int kScoreTiles = 2;
+template <int D, bool F32, bool MULTI>
+__global__ __launch_bounds__(256, 4) void cache4_score_kernel(Choose A, FastDiv tiles, FastDiv heads)
+{
+    typedef Scorer<D, F32, MULTI, kScoreTiles> S;
+    __shared__ f32x4 s_lds[MULTI ? 1 : S::LDS / 16];
+    const int bh = tiles.div(blockIdx.x), tile = blockIdx.x - bh * tiles.d, b = heads.div(bh), h = bh - b * heads.d;
+    const int first = ((int)blockIdx.y * 4 + wave_id()) * kScoreTiles;
+    S sc(A, b, h, tile, first);
+    if (tile * A.per >= sc.nq) return;
+    const int seen = sc.seen_by(min(sc.nq, (tile + 1) * A.per) - 1);
+    if ((int)blockIdx.y * 4 * kScoreTiles * 16 >= seen) return;
+    sc.fetch(first);
+    if (!MULTI) sc.queries(reinterpret_cast<char*>(s_lds));
+    sc.score(first, seen, [&](int i, int e0, f32x4 score) {
+        *reinterpret_cast<f32x4*>(A.scores + ((long)bh * A.N + i) * A.pitch + e0) = score;
+    });
 }
 
 // ------------------------------------------------------------------------------------------------ choice
 
-// Larger scores first, of equal ones the first page; never 0.
-__device__ __forceinline__ uint64_t page_key(float score, int e) {
-    const uint32_t u = __float_as_uint(score + 0.f), up = u & 0x80000000u ? ~u : u | 0x80000000u;       // (-0 is 0)
-    return ((uint64_t)up << 32) | (uint32_t)(0x7FFFFFFF - e);
+// A score as a whole number of the same order; above 0, and below all ones.
+__device__ __forceinline__ uint32_t ordered(float score) {
+    const uint32_t u = __float_as_uint(score + 0.f);     // (-0 is 0)
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// A block per token and K/V head.
-__global__ __launch_bounds__(256) void cache4_choose_kernel(Choose A, FastDiv tokens, FastDiv heads)
+// The choice by one wave, whose lane l has the scores of pages l, l + 64, .. in registers: the largest number that as many scores as there
+// are to take are no smaller than, bit by bit, with a vote for each; then the first of those that are equal to it.
+template <int K>
+__device__ __forceinline__ void choose_by_wave(const Choose& A, const float* score, int P, int32_t* to) {
+    const int lane = lane_id();
+    const int hi = P - A.last, taken = A.budget;
+    if (P <= A.budget) {
+        for (int x = lane; x < A.budget; x += kWave) to[x] = x < P ? x : -1;
+        return;
+    }
+    uint32_t key[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        const int e = j * kWave + lane;
+        key[j] = e >= P ? 0u : e < A.first || e >= hi ? 0xFFFFFFFFu : ordered(score[e]);
+    }
+    // from the first bit on that differs
+    uint32_t least = 0xFFFFFFFFu, most = 0;
+#pragma unroll
+    for (int j = 0; j < K; ++j) { least = min(least, key[j] ? key[j] : 0xFFFFFFFFu); most = max(most, key[j] != 0xFFFFFFFFu ? key[j] : 0u); }
+    least = wave_min_u32(least);
+    most = max(~wave_min_u32(~most), least);         // (there may be nothing but pages that are always taken)
+    const int from = 31 - __clz((int)((least ^ most) | 1u));
+    uint32_t bound = (most >> from >> 1) << 1 << from;
+    int above = P;                                   // that are no smaller
+    for (int bit = from; bit >= 0 && above != taken; --bit) {
+        const uint32_t next = bound | (1u << bit);
+        int count = 0;
+#pragma unroll
+        for (int j = 0; j < K; ++j) count += __popcll(__ballot(key[j] >= next));
+        if (count >= taken) { bound = next; above = count; }
+    }
+    int ties = above - taken;                        // of the smallest, as many are too many: the last ones
+    if (ties > 0) {
+        int equal = 0;
+#pragma unroll
+        for (int j = 0; j < K; ++j) equal += __popcll(__ballot(key[j] == bound));
+        ties = equal - ties;                         // that stay
+    }
+    const bool all = above == taken;
+    int done = 0;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        const unsigned long long same = __ballot(key[j] == bound);
+        bool in = all ? key[j] >= bound && key[j] != 0u : key[j] > bound || (key[j] == bound && lanes_below(same) < ties);
+        if (!all) ties -= __popcll(same);
+        const unsigned long long on = __ballot(in);
+        if (in) to[done + lanes_below(on)] = j * kWave + lane;
+        done += __popcll(on);
+    }
+}
+
+// Scores and choice in one: a block per tile of 16 query rows, scores in LDS ([tokens][pitch]), a wave per token for the choice.
+template <int D, bool F32, int K>
+__global__ __launch_bounds__(256, 4) void cache4_score_choose_kernel(Choose A, FastDiv tiles, FastDiv heads)
 {
-    __shared__ int s_hist[kSelectHistInts], s_red[4];
+    extern __shared__ f32x4 s_lds[];
+    float* s_score = reinterpret_cast<float*>(s_lds);
+    const int bh = tiles.div(blockIdx.x), tile = blockIdx.x - bh * tiles.d, b = heads.div(bh), h = bh - b * heads.d;
+    const int i0 = tile * A.per, waves = blockDim.x >> 6;
+    int first = wave_id() * kScoreTiles;
+    typedef Scorer<D, F32, false, kScoreTiles> S;
+    S sc(A, b, h, tile, first);
+    if (i0 >= sc.nq) return;
+    const int last = min(sc.nq, i0 + A.per) - 1, seen = sc.seen_by(last);
+    if (seen > A.budget) {
+        sc.fetch(first + waves * kScoreTiles);
+        sc.queries(reinterpret_cast<char*>(s_lds));
+        s_score += S::LDS / 4;
+        while (first * 16 < seen) {
+            sc.score(first, seen, [&](int i, int e0, f32x4 score) {
+                *reinterpret_cast<f32x4*>(s_score + (i - i0) * A.pitch + e0) = score;
+            });
+            first += waves * kScoreTiles;
+            if (first * 16 < seen) sc.fetch(first + waves * kScoreTiles);
+        }
+        __syncthreads();
+    }
+    for (int i = i0 + wave_id(); i <= last; i += waves)
+        choose_by_wave<K>(A, s_score + (i - i0) * A.pitch, sc.seen_by(i), A.chosen + (((long)b * A.N + i) * A.H + h) * A.budget);
+}
+
+// The same by the four waves of a block, of up to 2048 scores in the workspace: wave w's lane l has those of pages (4 j + w) * 64 + l.  Two bits
+// at a time: the waves' votes are added up through LDS, a barrier for each.
+__global__ __launch_bounds__(256) void cache4_choose_block_kernel(Choose A, FastDiv tokens, FastDiv heads)
+{
+    constexpr int K = 8;
+    __shared__ i32x4 s_votes[2][4];
+    __shared__ uint32_t s_least[4], s_most[4];
+    __shared__ int s_count[4 * K];
     const int bh = tokens.div(blockIdx.x), i = blockIdx.x - bh * tokens.d, b = heads.div(bh), h = bh - b * heads.d;
+    const int lane = lane_id(), wv = wave_id();
+    const float* score = A.scores + (long)blockIdx.x * A.pitch;
+    float f[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) f[j] = score[min((4 * j + wv) * kWave + lane, A.pitch - 1)];     // (on their way with the length)
+    int length = uniform(A.len)[b], nq = uniform(A.q_len ? A.q_len : A.len)[b];
+    asm volatile("" : "+s"(length), "+s"(nq));
+#pragma unroll
+    for (int j = 0; j < K; ++j) asm volatile("" : "+v"(f[j]));
+    length = c4_clamp(length, 0, A.max_pages << A.page_shift);
+    nq = A.q_len ? c4_clamp(nq, 0, A.N) : A.N;
+    if (i >= nq) return;
+    const int P = c4_pages_of(min(max(length - nq + i + 1, 0), length), A.page_shift), hi = P - A.last, taken = A.budget;
+    int32_t* to = A.chosen + (((long)b * A.N + i) * A.H + h) * A.budget;
+    if (P <= taken) {
+        for (int x = threadIdx.x; x < taken; x += 256) to[x] = x < P ? x : -1;
+        return;
+    }
+    uint32_t key[K], least = 0xFFFFFFFFu, most = 0;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        const int e = (4 * j + wv) * kWave + lane;
+        key[j] = e >= P ? 0u : e < A.first || e >= hi ? 0xFFFFFFFFu : ordered(f[j]);
+        least = min(least, key[j] ? key[j] : 0xFFFFFFFFu);
+        most = max(most, key[j] != 0xFFFFFFFFu ? key[j] : 0u);
+    }
+    least = wave_min_u32(least);
+    most = ~wave_min_u32(~most);
+    if (lane == 0) { s_least[wv] = least; s_most[wv] = most; }
+    block_sync_lds();
+    least = min(min(s_least[0], s_least[1]), min(s_least[2], s_least[3]));
+    most = max(max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3])), least);
+    int bit = (31 - __clz((int)((least ^ most) | 1u))) | 1;          // the upper one of two bits
+    uint32_t bound = (uint32_t)((uint64_t)most >> (bit + 1) << (bit + 1));
+    int above = P, turn = 0;                         // that are no smaller
+    for (; bit > 0 && above != taken; bit -= 2, turn ^= 1) {
+        const uint32_t unit = 1u << (bit - 1);
+        i32x4 votes{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+#pragma unroll
+            for (int x = 0; x < 3; ++x) votes[x] += (int)__popcll(__ballot(key[j] >= bound + unit * (x + 1)));
+        if (lane == 0) s_votes[turn][wv] = votes;
+        block_sync_lds();
+        votes = (s_votes[turn][0] + s_votes[turn][1]) + (s_votes[turn][2] + s_votes[turn][3]);
+        const int x = votes[2] >= taken ? 3 : votes[1] >= taken ? 2 : votes[0] >= taken ? 1 : 0;
+        if (x) { bound += unit * x; above = votes[x - 1]; }
+        bound = (uint32_t)__builtin_amdgcn_readfirstlane((int)bound);
+        above = __builtin_amdgcn_readfirstlane(above);
+    }
+    // larger ones and equal ones of 64 at a time, and before them
+    const bool all = above == taken;                 // (then those that are equal count as larger)
+    int mine[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        const int larger = (int)__popcll(__ballot(all ? key[j] >= bound && key[j] != 0u : key[j] > bound));
+        mine[j] = larger | (all ? 0 : (int)__popcll(__ballot(key[j] == bound)) << 16);
+        if (lane == 0) s_count[4 * j + wv] = mine[j];
+    }
+    block_sync_lds();
+    const int count = lane < 4 * K ? s_count[lane] : 0, upto = wave_incl_scan_i(count);
+    const int ties = taken - (__builtin_amdgcn_readlane(upto, kWave - 1) & 0xFFFF);
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        const int before = __builtin_amdgcn_readlane(upto, 4 * j + wv) - mine[j];
+        const bool larger = all ? key[j] >= bound && key[j] != 0u : key[j] > bound, same = !all && key[j] == bound;
+        const int equal = (before >> 16) + lanes_below(__ballot(same));
+        if (larger || (same && equal < ties)) to[(before & 0xFFFF) + lanes_below(__ballot(larger)) + min(equal, ties)] = (4 * j + wv) * kWave + lane;
+    }
+}
+
+// Larger scores first, of equal ones the first page; never 0.
+__device__ __forceinline__ uint64_t page_key(float score, int e) { return ((uint64_t)ordered(score) << 32) | (uint32_t)(0x7FFFFFFF - e); }
+
+// The choice from scores in the workspace, a block per token and K/V head.  IPT: keys that a thread holds, 0: any number, looked up again
+// and again.
+template <int IPT, int THREADS>
+__global__ __launch_bounds__(THREADS) void cache4_choose_kernel(Choose A, FastDiv tokens, FastDiv heads)
+{
+    __shared__ int s_hist[kSelectHistInts], s_red[16];
+    const int bh = tokens.div(blockIdx.x), i = blockIdx.x - bh * tokens.d, b = heads.div(bh), h = bh - b * heads.d, tid = threadIdx.x;
     const int P = pages_seen(A, b, i);
     if (P < 0) return;
     const float* score = A.scores + (long)blockIdx.x * A.pitch;
     int32_t* to = A.chosen + (((long)b * A.N + i) * A.H + h) * A.budget;
-    const int lo = min(A.first, P), hi = max(P - A.last, lo), always = lo + P - hi;      // pages lo .. hi - 1 are ranked
-    int taken = P;
-    SelectBound bound{0, 63};
-    if (P > A.budget) {
-        for (int x = threadIdx.x; x < kSelectHistInts; x += 256) s_hist[x] = 0;
-        __syncthreads();
-        bound = block_select_keys([&](auto f) {
-            for (int e = lo + (int)threadIdx.x; e < hi; e += 256) f(page_key(score[e], e));
-        }, A.budget - always, s_hist);
-        taken = A.budget;
+    if (P <= A.budget) {
+        for (int x = tid; x < A.budget; x += THREADS) to[x] = x < P ? x : -1;
+        return;
     }
+    const int lo = A.first, hi = P - A.last, always = lo + P - hi;       // pages lo .. hi - 1 are ranked
+    uint64_t key[IPT ? IPT : 1];
+    if constexpr (IPT > 0) {
+#pragma unroll
+        for (int t = 0; t < IPT; ++t) {
+            const int e = t * THREADS + tid;
+            key[t] = e >= lo && e < hi ? page_key(score[e], e) : 0;
+        }
+    }
+    for (int x = tid; x < kSelectHistInts; x += THREADS) s_hist[x] = 0;
+    __syncthreads();
+    SelectBound bound;
+    if constexpr (IPT > 0) bound = block_select_topk<IPT>(key, A.budget - always, s_hist);
+    else
+        bound = block_select_keys([&](auto f) {
+            for (int e = lo + tid; e < hi; e += THREADS) f(page_key(score[e], e));
+        }, A.budget - always, s_hist);
     int done = 0;
-    for (int e0 = 0; e0 < P; e0 += 256) {
-        const int e = e0 + threadIdx.x;
-        bool in = e < P;
-        if (in && P > A.budget && e >= lo && e < hi) in = A.budget > always && (page_key(score[e], e) >> bound.shift) >= bound.bound;
+    const auto place = [&](int e, uint64_t k) {
+        const bool in = e < P && (e < lo || e >= hi || (A.budget > always && (k >> bound.shift) >= bound.bound));
         int total;
         const int at = block_rank(in, s_red, total);
         if (in && done + at < A.budget) to[done + at] = e;
         done += total;
+    };
+    if constexpr (IPT > 0) {
+#pragma unroll
+        for (int t = 0; t < IPT; ++t)
+            if (t * THREADS < P) place(t * THREADS + tid, key[t]);
+    } else {
+        for (int e0 = 0; e0 < P; e0 += THREADS) {
+            const int e = e0 + tid;
+            place(e, e >= lo && e < hi ? page_key(score[e], e) : 0);
+        }
     }
-    for (int x = taken + threadIdx.x; x < A.budget; x += 256) to[x] = -1;
 }
 
 // ------------------------------------------------------------------------------------------------ attention
@@ -541,12 +861,32 @@ int choose_impl(const void* q, int dtype, const int8_t* bounds, const uint8_t* s
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int tiles = (N + A.per - 1) / A.per, chunks = (max_pages + 64 * kScoreTiles - 1) / (64 * kScoreTiles);
     if (chunks > 65535) return fail(MD_ESHAPE, "cache4_choose: %d pages are too many for one request", max_pages);
-#define MD_C4_SCORE(D_, F_)                                                                                                               \
-    MD_LAUNCH("cache4_score", st, (cache4_score_kernel<D_, F_>), dim3(B * H * tiles, chunks), 256, 0, A, FastDiv::make(tiles), FastDiv::make(H))
+    const long blocks = (long)B * H * tiles;
+    const size_t lds = 64 + 32 * (d + 16) + (size_t)A.per * A.pitch * 4;
+    if (A.subs == 1 && c4_choose_together(blocks, A.pitch, lds)) {
+        const int threads = 256;
+#define MD_C4_CHOOSE2(D_, F_, K_)                                                                                                         \
+    MD_LAUNCH("cache4_score_choose", st, (cache4_score_choose_kernel<D_, F_, K_>), (int)blocks, threads, lds, A, FastDiv::make(tiles), FastDiv::make(H))
+#define MD_C4_CHOOSE(D_, F_)                                                                                                              \
+    do { if (max_pages <= 256) MD_C4_CHOOSE2(D_, F_, 4); else if (max_pages <= 768) MD_C4_CHOOSE2(D_, F_, 12); else MD_C4_CHOOSE2(D_, F_, 32); } while (0)
+        if (d == 128) { if (dtype == MD_F32) MD_C4_CHOOSE(128, true); else MD_C4_CHOOSE(128, false); }
+        else { if (dtype == MD_F32) MD_C4_CHOOSE(64, true); else MD_C4_CHOOSE(64, false); }
+#undef MD_C4_CHOOSE
+#undef MD_C4_CHOOSE2
+        return check_launch(who);
+    }
+#define MD_C4_SCORE2(D_, F_, M_)                                                                                                          \
+    MD_LAUNCH("cache4_score", st, (cache4_score_kernel<D_, F_, M_>), dim3((int)blocks, chunks), 256, 0, A, FastDiv::make(tiles), FastDiv::make(H))
+#define MD_C4_SCORE(D_, F_) do { if (A.subs > 1) MD_C4_SCORE2(D_, F_, true); else MD_C4_SCORE2(D_, F_, false); } while (0)
     if (d == 128) { if (dtype == MD_F32) MD_C4_SCORE(128, true); else MD_C4_SCORE(128, false); }
     else { if (dtype == MD_F32) MD_C4_SCORE(64, true); else MD_C4_SCORE(64, false); }
 #undef MD_C4_SCORE
-    MD_LAUNCH("cache4_choose", st, (cache4_choose_kernel), B * H * N, 256, 0, A, FastDiv::make(N), FastDiv::make(H));
+#undef MD_C4_SCORE2
+#define MD_C4_PICK(I_, T_) MD_LAUNCH("cache4_choose", st, (cache4_choose_kernel<I_, T_>), B * H * N, T_, 0, A, FastDiv::make(N), FastDiv::make(H))
+    if (max_pages <= 2048) MD_LAUNCH("cache4_choose", st, (cache4_choose_block_kernel), B * H * N, 256, 0, A, FastDiv::make(N), FastDiv::make(H));
+    else if (max_pages <= 8192) MD_C4_PICK(8, 1024);
+    else MD_C4_PICK(0, 1024);
+#undef MD_C4_PICK
     return check_launch(who);
 }
 

@@ -121,6 +121,11 @@ inline int c4_span(int N, int page, int max_pages) {
     return most < max_pages ? (int)most : max_pages;
 }
 
+// Whether a call of the choice scores and chooses in one launch: up to 2048 pages, whose scores a block has in LDS.
+inline bool c4_choose_together(int64_t blocks, int pitch, size_t lds) {
+    return pitch <= 2048 && lds <= 32768 && (blocks >= 256 || pitch <= 256);
+}
+
 // How the attention over chosen pages is cut: `splits` parts of a list of `budget` pages, a block each; `most` entries of the list to a
 // part.  `units`: tiles of 16 query heads of all tokens and K/V heads.
 struct C4Chosen { int splits, most; };
