@@ -4,7 +4,8 @@
 //   cache4_score_kernel           bounds and queries -> a score for each token, K/V head and page
 //   cache4_choose_kernel          scores -> the pages to read
 //   cache4_attend_chosen_kernel   softmax(scale Q K^T) V over them
-//   cache4_attend_chosen_join_kernel   the same where a list is cut into parts
+//   cache4_attend_shared_kernel   the same for several tokens together, over all of their pages
+//   cache4_attend_chosen_join_kernel   what parts of a list have given, put together
 //
 // The score of a page is the sum over the G query heads of max over [smallest, largest] of q . k, which is no less than the sum of any of its
 // keys' own scores: max(q a, q b) = max(q, 0) a + min(q, 0) b for a >= b, so that it is one matrix product with twice the channels.
@@ -604,103 +605,177 @@ __global__ __launch_bounds__(THREADS) void cache4_choose_kernel(Choose A, FastDi
 // A walk over the pages of a list, which lies in LDS: page numbers and entries of the block table.  Positions of the walk count the
 // list's tokens, one page after the other.
 struct Listed : Walk {
-    const int2* list;
+    uint32_t list;                                   // in LDS
     int last;                                        // of the list
 };
-__device__ __forceinline__ int2 listed_at(const Listed& w, int t) {
-    const int2 v = w.list[min(t >> w.page_shift, w.last)];
-    return int2{__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y)};
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(lds_ptr_t)const_cast<void*>(p); }
+// Of a step's two 16-key tiles (to the compiler a read of LDS is one of what the loads on their way write there, and would wait for them all)
+struct Entries { int id[2], entry[2]; };
+__device__ __forceinline__ Entries listed_at(const Listed& w, int step) {
+    u32x2 a, b;
+    asm volatile("ds_read_b64 %0, %2\n\tds_read_b64 %1, %3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(a), "=&v"(b)
+                 : "v"(w.list + 8 * min((step * 32) >> w.page_shift, w.last)), "v"(w.list + 8 * min((step * 32 + 16) >> w.page_shift, w.last)) : "memory");
+    return Entries{{__builtin_amdgcn_readfirstlane((int)a.x), __builtin_amdgcn_readfirstlane((int)b.x)},
+                   {__builtin_amdgcn_readfirstlane((int)a.y), __builtin_amdgcn_readfirstlane((int)b.y)}};
 }
 __device__ __forceinline__ Pages pages_at(const Listed& w, int step) {
-    Pages r;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) r.id[u] = listed_at(w, step * 32 + 16 * u).x;
-    return r;
+    const Entries e = listed_at(w, step);
+    return Pages{{e.id[0], e.id[1]}};
 }
-__device__ __forceinline__ int entry_of(const Listed& w, int t) { return (listed_at(w, t).y << w.page_shift) + (t & (w.page - 1)); }
 __device__ __forceinline__ Kept kept_at(const Listed& w, int step) {
     Kept r;
+    if (w.keep) {
+        const Entries e = listed_at(w, step);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        if (w.keep) {
-            const int at = entry_of(w, step * 32 + 16 * u) >> 2;
+        for (int u = 0; u < 2; ++u) {
+            const int at = ((e.entry[u] << w.page_shift) + ((step * 32 + 16 * u) & (w.page - 1))) >> 2;
 #pragma unroll
             for (int x = 0; x < 4; ++x) r.w[u][x] = w.keep[at + x];
-        } else {
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int x = 0; x < 4; ++x) r.w[u][x] = 0x01010101u;
-        }
     }
     return r;
 }
 __device__ __forceinline__ bool left_out(const Listed& w, int t) {
     if (!w.keep) return false;
-    const int at = entry_of(w, t);
+    const Entries e = listed_at(w, t >> 5);
+    const int at = ((t & 16 ? e.entry[1] : e.entry[0]) << w.page_shift) + (t & (w.page - 1));
     return ((w.keep[at >> 2] >> (8 * (at & 3))) & 0xFF) == 0;
 }
 
-struct Chosen { const int32_t* list; int budget, splits, most; };
-constexpr int kChosenAt = (sizeof(AttendArgs) + 7) / 8 * 8;
+// The pages that any of several tokens has chosen; bit i: token i of them has.
+struct Shared : Listed {
+    uint32_t members;                                // in LDS
+    uint32_t all;                                    // of the tokens
+    int token;                                       // of the lane's row
+};
+struct Members { uint32_t m[2]; };
+__device__ __forceinline__ Members members_at(const Shared& w, int step) {
+    uint32_t a, b;
+    asm volatile("ds_read_u16 %0, %2\n\tds_read_u16 %1, %3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(a), "=&v"(b)
+                 : "v"(w.members + 2 * min((step * 32) >> w.page_shift, w.last)), "v"(w.members + 2 * min((step * 32 + 16) >> w.page_shift, w.last)) : "memory");
+    return Members{{(uint32_t)__builtin_amdgcn_readfirstlane((int)a), (uint32_t)__builtin_amdgcn_readfirstlane((int)b)}};
+}
+__device__ __forceinline__ bool uneven(const Shared& w, int step) {
+    const Members m = members_at(w, step);
+    return m.m[0] != w.all || m.m[1] != w.all;
+}
+__device__ __forceinline__ Sight sight_at(const Shared& w, int step) {
+    const Members m = members_at(w, step);
+    return Sight{{0u - ((m.m[0] >> w.token) & 1), 0u - ((m.m[1] >> w.token) & 1)}};
+}
 
-// What a block works on: a part of the list of one token and K/V head, and 16 of its query heads.
+// tokens: that a block takes together; splits, most: parts of a list, and entries of a part
+struct Chosen { const int32_t* list; int budget, splits, most, tokens; };
+constexpr int kChosenAt = (sizeof(AttendArgs) + 7) / 8 * 8;
+constexpr int kChosenPartsAt = (kChosenAt + (int)sizeof(Chosen) + 7) / 8 * 8;
+
+// What a block works on: 16 of the query heads of one token and K/V head and a part of its list; or all of those of several tokens.
 struct Unit { int b, i, h, g0, split; };
-__device__ __forceinline__ Unit unit_of(const AttendArgs& A, const Chosen& C) {
+__device__ __forceinline__ Unit unit_of(const AttendArgs& A, const Chosen& C, int x) {
     Unit u;
-    int x = blockIdx.x;
     u.split = x % C.splits; x /= C.splits;
     u.g0 = x % A.dim.tiles * 16; x /= A.dim.tiles;
     u.h = x % A.p.H; x /= A.p.H;
-    u.i = x % A.dim.N;
-    u.b = x / A.dim.N;
+    const int groups = (A.dim.N + C.tokens - 1) / C.tokens;
+    u.i = x % groups * C.tokens;
+    u.b = x / groups;
     return u;
 }
-// The call as one of a single token looks to the others: that token's query and outputs.
+// The call as one of the tokens from i on looks to the others: their queries and outputs.
 template <bool F32>
-__device__ __forceinline__ void only_token(AttendArgs& A, int i) {
+__device__ __forceinline__ void from_token(AttendArgs& A, int i) {
     const long q = (long)i * A.ql.token * (F32 ? 4 : 2), o = (long)i * A.ol.token * (F32 ? 4 : 2);
     A.q = static_cast<const char*>(A.q) + q;
     A.out = static_cast<char*>(A.out) + o;
     if (A.lse) A.lse += i;
 }
+// Entries that row i of a sample sees.
+__device__ __forceinline__ int entries_seen(const Sample& s, int i) { return min(max(s.length - s.nq + i + 1, 0), s.length); }
 
-// The entries of a part that count, in order, by the block's first wave: within the table, above all before them, with something that
-// the token sees, and with a page.  Returns the tokens that they hold for it.
-__device__ __forceinline__ int make_list(const AttendArgs& A, const Chosen& C, const Unit& u, int seen, int2* list, int& count) {
+// The entries of a token's list from v0 to v1 that count, by one wave: within the table, above all before them, and with something that
+// the token sees.  each(entry, whether the lane's counts).  ahead: the first 64, which the caller has asked for.
+__device__ __forceinline__ const int32_t* list_of(const AttendArgs& A, const Chosen& C, const Unit& u, int i) {
+    return C.list + (((long)u.b * A.dim.N + i) * A.p.H + u.h) * C.budget;
+}
+template <class Each>
+__device__ __forceinline__ void each_entry(const AttendArgs& A, const int32_t* from, int ahead, int seen, int v0, int v1, Each each) {
     const int lane = lane_id();
-    const int32_t* from = C.list + (((long)u.b * A.dim.N + u.i) * A.p.H + u.h) * C.budget;
-    const int32_t* row = A.table + (long)u.b * A.p.max_pages;
-    const int v0 = u.split * C.most, v1 = min(v0 + C.most, C.budget);
     const auto entry = [&](int v) {
-        const int e = v < v1 ? from[v] : -1;
-        return (uint32_t)e < (uint32_t)A.p.max_pages ? e : -1;
+        int e = ahead;
+        if (v - lane != v0) e = from[min(v, v1 - 1)];
+        return v < v1 && (uint32_t)e < (uint32_t)A.p.max_pages ? e : -1;
     };
     int before = -1;
-    for (int v = lane; v < v0; v += kWave) before = max(before, entry(v));
-    before = (int)~wave_min_u32(~(uint32_t)(before + 1)) - 1;
-    int n = 0, tokens = 0;
+    if (v0 > 0) {
+        for (int v = lane; v < v0; v += kWave) before = max(before, entry(v));
+        before = (int)~wave_min_u32(~(uint32_t)(before + 1)) - 1;
+    }
     for (int base = v0; base < v1; base += kWave) {
         const int e = entry(base + lane);
         int top = e;                                 // the largest up to here
+        if (__any(lane < kWave - 1 && base + lane < v1 - 1 && __shfl_down(e, 1, kWave) <= e)) {      // (a list that ascends is its own)
 #pragma unroll
-        for (int x = 1; x < kWave; x <<= 1) {
-            const int other = __shfl_up(top, x, kWave);
-            if (lane >= x) top = max(top, other);
+            for (int x = 1; x < kWave; x <<= 1) {
+                const int other = __shfl_up(top, x, kWave);
+                if (lane >= x) top = max(top, other);
+            }
         }
         const int prior = __shfl_up(top, 1, kWave);
-        const bool rises = e >= 0 && e > max(before, lane ? prior : -1);
-        int id = -1;
-        if (rises && ((long)e << A.p.page_shift) < seen) id = c4_page_id(row[e], A.p.n_pages);
-        const unsigned long long on = __ballot(id >= 0);
-        if (id >= 0) list[n + lanes_below(on)] = int2{id, e};
-        n += __popcll(on);
-        int mine = id >= 0 ? min(seen - (e << A.p.page_shift), A.p.page) : 0;
-        tokens += wave_sum_i(mine);
+        const bool on = e > max(before, lane ? prior : -1) && ((long)e << A.p.page_shift) < seen;
+        each(e, on);
         before = max(before, __builtin_amdgcn_readlane(top, kWave - 1));
     }
-    count = n;
-    return tokens;
 }
 
+// A part of one token's list, by one wave: pages and entries.  Returns how many, and the tokens that they hold for it.
+__device__ __forceinline__ int2 make_list(const AttendArgs& A, const int32_t* from, int ahead, const Unit& u, int seen, int v0, int v1, int2* list) {
+    const int32_t* row = A.table + (long)u.b * A.p.max_pages;
+    int n = 0, tokens = 0;
+    each_entry(A, from, ahead, seen, v0, v1, [&](int e, bool on) {
+        const int there = row[max(e, 0)], id = on ? c4_page_id(there, A.p.n_pages) : -1;
+        const unsigned long long have = __ballot(id >= 0);
+        if (id >= 0) list[n + lanes_below(have)] = int2{id, e};
+        n += (int)__popcll(have);
+        tokens += wave_sum_i(id >= 0 ? min(seen - (e << A.p.page_shift), A.p.page) : 0);
+    });
+    return int2{n, tokens};
+}
+
+// The lists of `n` tokens together, by all waves of the block.  s_any: 16 bits for each entry of the table.  Returns the number of pages.
+__device__ __forceinline__ int make_shared_list(const AttendArgs& A, const Chosen& C, const Unit& u, const Sample& s, int n, uint32_t* s_any, int2* list,
+                                                uint16_t* members, int* s_red) {
+    const int tid = threadIdx.x, threads = blockDim.x, waves = threads >> 6;
+    const int32_t* row = A.table + (long)u.b * A.p.max_pages;
+    const int entries = c4_pages_of(entries_seen(s, u.i + n - 1), A.p.page_shift);
+    for (int x = tid; x < (entries + 1) / 2; x += threads) s_any[x] = 0;
+    block_sync_lds();
+    for (int i = wave_id(); i < n; i += waves) {
+        const int32_t* from = list_of(A, C, u, u.i + i);
+        each_entry(A, from, from[min(lane_id(), C.budget - 1)], entries_seen(s, u.i + i), 0, C.budget, [&](int e, bool on) {
+            if (on) atomicOr(&s_any[e >> 1], 1u << (16 * (e & 1) + i));
+        });
+    }
+    block_sync_lds();
+    int count = 0;
+    for (int e0 = 0; e0 < entries; e0 += threads) {
+        const int e = e0 + tid;
+        const uint32_t m = e < entries ? (s_any[e >> 1] >> (16 * (e & 1))) & 0xFFFF : 0;
+        const int id = m ? c4_page_id(row[e], A.p.n_pages) : -1;
+        int total;
+        const int at = block_rank(id >= 0, s_red, total);
+        if (id >= 0) { list[count + at] = int2{id, e}; members[count + at] = (uint16_t)m; }
+        count += total;
+    }
+    block_sync_lds();
+    return count;
+}
+
+// A block per token, K/V head, 16 of its query heads and part of its list.
 template <int D, bool F32, bool STREAM>
 __global__ __launch_bounds__(F32 && D == 128 ? 256 : 512, F32 && D == 128 ? 3 : 4) void cache4_attend_chosen_kernel(AttendArgs A0, Chosen C0, Parts parts0)
 {
@@ -709,28 +784,31 @@ __global__ __launch_bounds__(F32 && D == 128 ? 256 : 512, F32 && D == 128 ? 3 : 
     Sweep<D, F32, 1, STREAM> sw;
     Listed w;
     char* lds = reinterpret_cast<char*>(s_lds);
-    int2* list = reinterpret_cast<int2*>(lds);       // (C.most entries; the rings and the join's sums are behind)
     {
-        AttendArgs A = argument<AttendArgs>(0);
+        const AttendArgs A = argument<AttendArgs>(0);
         const Chosen C = argument<Chosen>(kChosenAt);
-        const Unit u = unit_of(A, C);
-        Sample s = sample_of(A, u.b);
+        const Unit u = unit_of(A, C, blockIdx.x);
+        const int32_t* from = list_of(A, C, u, u.i);
+        const int v0 = u.split * C.most, v1 = min(v0 + C.most, C.budget);
+        int length = uniform(A.len)[u.b], nq = uniform(A.q_len ? A.q_len : A.len)[u.b], ahead = from[min(v0 + lane_id(), C.budget - 1)];
+        asm volatile("" : "+s"(length), "+s"(nq), "+v"(ahead));      // (on their way together)
+        Sample s{u.b, c4_clamp(length, 0, A.p.max_pages << A.p.page_shift), A.q_len ? c4_clamp(nq, 0, A.dim.N) : A.dim.N};
         if (u.i >= s.nq) return;
-        const int seen = min(max(s.length - s.nq + u.i + 1, 0), s.length);
+        int2* list = reinterpret_cast<int2*>(lds);   // (C.most entries; the rings and the join's sums are behind)
+        AttendArgs T = A;
+        from_token<F32>(T, u.i);
+        sw.begin(T, Sample{u.b, 0, 1}, u.h, u.g0);   // (its queries are on their way while the list is made)
         if (wave_id() == 0) {
-            int count;
-            const int tokens = make_list(A, C, u, seen, list, count);
-            if (lane_id() == 0) { s_count[0] = count; s_count[1] = tokens; }
+            const int2 made = make_list(A, from, ahead, u, entries_seen(s, u.i), v0, v1, list);
+            if (lane_id() == 0) { s_count[0] = made.x; s_count[1] = made.y; }
         }
         __syncthreads();
         s.length = __builtin_amdgcn_readfirstlane(s_count[1]);
         s.nq = 1;
+        sw.limit[0] = u.g0 + (lane_id() & 15) < A.dim.G ? s.length : 0;
         static_cast<Walk&>(w) = table_of(A, u.b);
-        only_token<F32>(A, u.i);
-        // 16 query heads from g0 on, as rows of a K/V head
-        sw.begin(A, s, u.h, u.g0);
         walk_of(w, A, s, u.h, 0, 0);
-        w.list = list;
+        w.list = lds_address(list);
         w.last = max(__builtin_amdgcn_readfirstlane(s_count[0]) - 1, 0);
         lds += (C.most + 1) / 2 * 16;
     }
@@ -739,19 +817,79 @@ __global__ __launch_bounds__(F32 && D == 128 ? 256 : 512, F32 && D == 128 ? 3 : 
     __syncthreads();
     AttendArgs A = argument<AttendArgs>(0);
     const Chosen C = argument<Chosen>(kChosenAt);
-    const Unit u = unit_of(A, C);
-    only_token<F32>(A, u.i);
+    const Unit u = unit_of(A, C, blockIdx.x);
+    from_token<F32>(A, u.i);
     const int rows = min(16, A.dim.G - u.g0);
     if (C.splits == 1) {
         join_waves<D, 1>(sw, rows, reinterpret_cast<float*>(lds), [&](int row, int part, const float (&x)[D / 16], float m, float l) {
             store_out<D, F32>(A, u.b, u.h, u.g0 + row, part, x, m, l);
         });
     } else {
-        const Parts parts = argument<Parts>((kChosenAt + (int)sizeof(Chosen) + 7) / 8 * 8);
+        const Parts parts = argument<Parts>(kChosenPartsAt);
         join_waves<D, 1>(sw, rows, reinterpret_cast<float*>(lds), [&](int row, int part, const float (&x)[D / 16], float m, float l) {
             store_part<D>(parts, blockIdx.x, 16, row, part, x, m, l);
         });
     }
+}
+
+// A block per K/V head and as many tokens as fill 16 query rows with their heads: over the pages that any of them has chosen, hidden from the
+// others.  A key is converted once for all of them; tokens next to each other often choose the same pages.
+template <int D, bool F32, bool STREAM>
+__global__ __launch_bounds__(F32 && D == 128 ? 256 : 512, F32 && D == 128 ? 3 : 4) void cache4_attend_shared_kernel(AttendArgs A0, Chosen C0)
+{
+    extern __shared__ f32x4 s_lds[];
+    __shared__ int s_red[8];
+    Sweep<D, F32, 1, STREAM> sw;
+    Shared w;
+    char* lds = reinterpret_cast<char*>(s_lds);
+    {
+        AttendArgs A = argument<AttendArgs>(0);
+        const Chosen C = argument<Chosen>(kChosenAt);
+        const Unit u = unit_of(A, C, blockIdx.x);
+        Sample s = sample_of(A, u.b);
+        if (u.i >= s.nq) return;
+        const int n = min(C.tokens, s.nq - u.i);
+        int2* list = reinterpret_cast<int2*>(lds);   // (C.most entries, then which tokens have them; the rings and the join's sums are behind, and
+                                                     // where those will be what make_shared_list goes by)
+        uint16_t* members = reinterpret_cast<uint16_t*>(lds + (C.most + 1) / 2 * 16);
+        lds += (C.most + 1) / 2 * 16 + (C.most + 7) / 8 * 16;
+        AttendArgs T = A;
+        from_token<F32>(T, u.i);
+        sw.begin(T, Sample{u.b, 0, n}, u.h, 0);      // (its queries are on their way while the list is made)
+        const int count = make_shared_list(A, C, u, s, n, reinterpret_cast<uint32_t*>(lds), list, members, s_red);
+        // What a row sees ends within the list as it does in the sequence: in the last page that begins before.
+        const int token = min((lane_id() & 15) / A.dim.G, n - 1), row_seen = entries_seen(s, u.i + token);
+        int at = 0, limit = 0;                       // pages that begin before it
+        for (int to = count; at < to;) {
+            const int x = (at + to) >> 1;
+            if ((list[x].y << A.p.page_shift) < row_seen) at = x + 1;
+            else to = x;
+        }
+        if (at > 0) limit = ((at - 1) << A.p.page_shift) + min(row_seen - (list[at - 1].y << A.p.page_shift), A.p.page);
+        static_cast<Walk&>(w) = table_of(A, u.b);
+        s.length = __builtin_amdgcn_readlane(limit, (n - 1) * A.dim.G);
+        s.nq = n;
+        sw.limit[0] = (lane_id() & 15) < n * A.dim.G ? limit : 0;
+        walk_of(w, A, s, u.h, 0, n * A.dim.G - 1);
+        w.level = __builtin_amdgcn_readlane(limit, 0);                   // (the first token sees the least)
+        w.clear = w.keep ? 0 : w.level;
+        w.list = lds_address(list);
+        w.members = lds_address(members);
+        w.all = (1u << n) - 1;
+        w.token = token;
+        w.last = max(count - 1, 0);
+    }
+    const Early early = early_pages(w, wave_id(), blockDim.x >> 6);
+    sw.run(w, wave_id(), 0x7FFFFFFF, blockDim.x >> 6, lds + wave_id() * (sw.RING * sw.SLOT), early);
+    __syncthreads();
+    AttendArgs A = argument<AttendArgs>(0);
+    const Chosen C = argument<Chosen>(kChosenAt);
+    const Unit u = unit_of(A, C, blockIdx.x);
+    const Sample s = sample_of(A, u.b);
+    from_token<F32>(A, u.i);
+    join_waves<D, 1>(sw, min(C.tokens, s.nq - u.i) * A.dim.G, reinterpret_cast<float*>(lds), [&](int row, int part, const float (&x)[D / 16], float m, float l) {
+        store_out<D, F32>(A, u.b, u.h, row, part, x, m, l);
+    });
 }
 
 // The parts of a list: a block per token, K/V head and 16 query heads, sixteen lanes per head.
@@ -759,8 +897,8 @@ template <int D, bool F32>
 __global__ __launch_bounds__(256) void cache4_attend_chosen_join_kernel(AttendArgs A, Chosen C, Parts parts)
 {
     const int unit = blockIdx.x;
-    const Chosen whole{C.list, C.budget, 1, C.budget};
-    const Unit u = unit_of(A, whole);
+    const Chosen whole{C.list, C.budget, 1, C.budget, 1};
+    const Unit u = unit_of(A, whole, unit);
     const Sample s = sample_of(A, u.b);
     const int row = threadIdx.x >> 4, part = threadIdx.x & 15;
     if (u.i >= s.nq || u.g0 + row >= A.dim.G) return;
@@ -778,7 +916,7 @@ __global__ __launch_bounds__(256) void cache4_attend_chosen_join_kernel(AttendAr
             for (int z = 0; z < 4; ++z) acc[4 * j + z] = fmaf(v[z], e, acc[4 * j + z] * a);
         }
     }
-    only_token<F32>(A, u.i);
+    from_token<F32>(A, u.i);
     store_out<D, F32>(A, u.b, u.h, u.g0 + row, part, acc, m, l);
 }
 
@@ -893,26 +1031,29 @@ int choose_impl(const void* q, int dtype, const int8_t* bounds, const uint8_t* s
 struct ChosenPlan {
     C4Chosen cut;
     Parts parts;
-    int tiles, waves;
+    int tiles;
     long units;
     size_t lds, bytes;
 };
-ChosenPlan chosen_plan(void* workspace, bool f32, int B, int N, int Hq, int d, int budget, const Pool& p) {
+// max_pages: of the block table, or 0 where only the workspace's size is asked for
+ChosenPlan chosen_plan(void* workspace, bool f32, int B, int N, int Hq, int d, int budget, int max_pages, const Pool& p) {
     ChosenPlan a;
-    const int G = Hq / p.H, few = G < 16 ? G : 16;
+    const int G = Hq / p.H;
     a.tiles = (G + 15) / 16;
-    a.units = (long)B * N * p.H * a.tiles;
-    a.cut = c4_chosen(a.units, budget, p.page);
-    a.waves = 4;
-    const size_t join = sizeof(float) * ((size_t)a.waves * few * (d + 4) + 2 * a.waves * 16), ring = (size_t)a.waves * kRing * (32 * d + 256);
-    a.lds = (size_t)(a.cut.most + 1) / 2 * 16 + (join > ring ? join : ring);
+    a.cut = c4_chosen(f32, d, B, N, G, p.H, budget, p.page, max_pages);
+    a.units = (long)B * ((N + a.cut.tokens - 1) / a.cut.tokens) * p.H * a.tiles;
+    const int rows = a.cut.tokens * G < 16 ? a.cut.tokens * G : 16;
+    const size_t join = sizeof(float) * ((size_t)a.cut.waves * rows * (d + 4) + 2 * a.cut.waves * 16), ring = (size_t)a.cut.waves * kRing * (32 * d + 256);
+    const size_t list = (size_t)(a.cut.most + 1) / 2 * 16 + (a.cut.tokens > 1 ? (size_t)(a.cut.most + 7) / 8 * 16 : 0);
+    a.lds = list + (join > ring ? join : ring);      // (the ring is more than two bytes for each entry of a table that lists are shared in)
+    // parts of lists are joined through the workspace, whose size goes by the calls that have most of them
+    const C4Chosen apart = c4_chosen(f32, d, B, N, G, p.H, budget, p.page, 0);
+    const size_t places = apart.splits > 1 ? (size_t)B * N * p.H * a.tiles * apart.splits * 16 : 0;
     Carver c(workspace);
-    const size_t places = a.cut.splits > 1 ? (size_t)a.units * a.cut.splits * 16 : 0;
     a.parts.o = c.take<float>(places * d);
     a.parts.ml = c.take<float2>(places);
     a.parts.blocks = a.parts.least = 0;
     a.bytes = c.off > 256 ? c.off : 256;
-    (void)f32;
     return a;
 }
 int check_chosen(const char* who, int B, int N, int Hq, int H, int budget) {
@@ -926,7 +1067,7 @@ int check_chosen(const char* who, int B, int N, int Hq, int H, int budget) {
 size_t attend_chosen_bytes(int B, int N, int Hq, int H, int d, int budget, int page) {
     Pool p;
     if (check_pool("cache4_attend_chosen", H, d, 1, page, 1, &p) != MD_OK || check_chosen("cache4_attend_chosen", B, N, Hq, H, budget) != MD_OK) return 0;
-    const size_t x = chosen_plan(nullptr, false, B, N, Hq, d, budget, p).bytes, y = chosen_plan(nullptr, true, B, N, Hq, d, budget, p).bytes;
+    const size_t x = chosen_plan(nullptr, false, B, N, Hq, d, budget, 0, p).bytes, y = chosen_plan(nullptr, true, B, N, Hq, d, budget, 0, p).bytes;
     return x > y ? x : y;
 }
 
@@ -951,7 +1092,7 @@ int attend_chosen_impl(const void* q, int dtype, const void* cache, const int32_
     if (rc != MD_OK) return rc;
     if (!aligned16(q) || !aligned16(out) || !aligned16(cache) || (reinterpret_cast<uintptr_t>(keep) & 3u))
         return fail(MD_EALIGN, "cache4_attend_chosen: tensors must be 16-byte aligned, keep 4-byte aligned");
-    const ChosenPlan plan = chosen_plan(workspace, dtype == MD_F32, B, N, Hq, d, budget, p);
+    const ChosenPlan plan = chosen_plan(workspace, dtype == MD_F32, B, N, Hq, d, budget, max_pages, p);
     const size_t need = attend_chosen_bytes(B, N, Hq, H, d, budget, page);
     const Range r[] = {{out, rows_bytes(ol, B, N, Hq, d, dtype)}, {lse, lse ? (size_t)B * Hq * N * 4 : 0}, {workspace, workspace ? need : 0},
                        {q, rows_bytes(ql, B, N, Hq, d, dtype)}, {cache, pool_bytes(p)}, {table, (size_t)B * max_pages * 4}, {len, (size_t)B * 4},
@@ -962,13 +1103,14 @@ int attend_chosen_impl(const void* q, int dtype, const void* cache, const int32_
         return fail(MD_EWORKSPACE, "cache4_attend_chosen: workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(MD_EALIGN, "cache4_attend_chosen: workspace must be 256-byte aligned");
     const AttendArgs A{q, static_cast<const uint8_t*>(cache), table, len, q_len, keep, out, lse, p, AttendDims{B, N, Hq / H, plan.tiles}, softmax_scale, ql, ol};
-    const Chosen C{chosen, budget, plan.cut.splits, plan.cut.most};
+    const Chosen C{chosen, budget, plan.cut.splits, plan.cut.most, plan.cut.tokens};
     const int blocks = (int)(plan.units * plan.cut.splits);
     const bool stream_once = pool_bytes(p) > (size_t)128 << 20;
     hipStream_t st = static_cast<hipStream_t>(stream);
 #define MD_C4_CHOSEN(D_, F_, S_)                                                                                                          \
     do {                                                                                                                                  \
-        MD_LAUNCH("cache4_attend_chosen", st, (cache4_attend_chosen_kernel<D_, F_, S_>), blocks, plan.waves * 64, plan.lds, A, C, plan.parts); \
+        if (C.tokens > 1) { MD_LAUNCH("cache4_attend_shared", st, (cache4_attend_shared_kernel<D_, F_, S_>), blocks, plan.cut.waves * 64, plan.lds, A, C); break; } \
+        MD_LAUNCH("cache4_attend_chosen", st, (cache4_attend_chosen_kernel<D_, F_, S_>), blocks, plan.cut.waves * 64, plan.lds, A, C, plan.parts); \
         if (C.splits > 1) MD_LAUNCH("cache4_chosen_join", st, (cache4_attend_chosen_join_kernel<D_, F_>), (int)plan.units, 256, 0, A, C, plan.parts); \
     } while (0)
 #define MD_C4_CHOSEN_S(D_, F_) do { if (stream_once) MD_C4_CHOSEN(D_, F_, true); else MD_C4_CHOSEN(D_, F_, false); } while (0)

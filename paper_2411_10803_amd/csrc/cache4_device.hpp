@@ -194,7 +194,7 @@ struct Walk {
     uniform_ptr_t row, keep;                         // of the block table; of the mask, or null
     uint32_t pitch;                                  // 64-byte units from page to page
     int n_pages, page, page_shift, last_page;        // of the pool; tokens of a page; the table's last entry
-    int end, clear;                                  // keys that any row sees; that all rows see and no mask may leave out
+    int end, level, clear;                           // keys that any row sees; that all rows see; that no mask may leave out either
     float c;                                         // softmax scale, base 2
 };
 struct Pages { int id[2]; };                         // of a step's two 16-key tiles
@@ -216,7 +216,8 @@ __device__ __forceinline__ void walk_of(Walk& w, const AttendArgs& A, const Samp
     w.n_pages = A.p.n_pages;
     w.page = A.p.page;
     w.end = min(max(s.length - s.nq + last_row / A.dim.G + 1, 0), s.length);
-    w.clear = A.keep ? 0 : min(max(s.length - s.nq + first_row / A.dim.G + 1, 0), w.end);
+    w.level = min(max(s.length - s.nq + first_row / A.dim.G + 1, 0), w.end);
+    w.clear = A.keep ? 0 : w.level;
     w.c = A.scale * kLog2eC;
 }
 // The entries as they stand in the table, which nobody looks at yet: a wave that asks for them a step ahead does not wait for them.
@@ -267,6 +268,11 @@ __device__ __forceinline__ Kept kept_at(const Walk& w, int step) {
 }
 // Whether the mask leaves an entry out.
 __device__ __forceinline__ bool left_out(const Walk& w, int t) { return w.keep && ((w.keep[t >> 2] >> (8 * (t & 3))) & 0xFF) == 0; }
+
+// Whether some row does not see a page of a step that others see; all ones for those of a step's two tiles that the lane's row sees.
+struct Sight { uint32_t u[2]; };
+__device__ __forceinline__ bool uneven(const Walk&, int) { return false; }
+__device__ __forceinline__ Sight sight_at(const Walk&, int) { return Sight{{0xFFFFFFFFu, 0xFFFFFFFFu}}; }
 
 // 16 NT query rows of one (sample, K/V head) in a wave: queries, running maxima and sums.  Row r = i * G + g is the g-th query head
 // of the K/V head at token i.
@@ -344,6 +350,8 @@ struct Rows {
         const auto first = [](int n) { return n <= 0 ? 0u : kTops >> (32 - 8 * min(n, 4)); };
         const Pages pg = pages_at(w, step);
         const bool ok[2] = {there(w, step, pg, 0), there(w, step, pg, 1)};
+        const Sight sight = sight_at(w, step);
+        const bool inside = step * 32 + 32 <= w.level && ok[0] && ok[1];         // (a prompt's piece has few steps that are not)
         uint32_t nan = 0;
 #pragma unroll
         for (int t = 0; t < NT; ++t) hides[t] = 0;
@@ -352,10 +360,17 @@ struct Rows {
             const int t = step * 32 + 16 * u + 4 * lb;
             const uint32_t w0 = kp.w[u][0], w1 = kp.w[u][1], w2 = kp.w[u][2], w3 = kp.w[u][3];
             const uint32_t even = lb & 2 ? w2 : w0, odd = lb & 2 ? w3 : w1, kept = lb & 1 ? odd : even;
-            const uint32_t on = nonzero(kept) & first((ok[u] ? w.end : 0) - t), nans = kTops & ~nonzero(~vs[u]);
-            nan |= on & nans;
+            uint32_t on = nonzero(kept);
+            const uint32_t nans = kTops & ~nonzero(~vs[u]);
+            if (inside) {
 #pragma unroll
-            for (int z = 0; z < NT; ++z) hides[z] |= (on & first(limit[z] - t)) >> (4 * u);
+                for (int z = 0; z < NT; ++z) hides[z] |= (on & (limit[z] > 0 ? sight.u[u] : 0u)) >> (4 * u);
+            } else {
+                on &= first((ok[u] ? w.end : 0) - t);
+#pragma unroll
+                for (int z = 0; z < NT; ++z) hides[z] |= (on & first(limit[z] - t) & sight.u[u]) >> (4 * u);
+            }
+            nan |= on & nans;
             const uint32_t out = (kTops & ~on) | nans, bytes = (out << 1) - (out >> 7);
             vs[u] = (vs[u] & ~bytes) | (bytes & 0x7F7F7F7Fu);
         }
@@ -370,7 +385,7 @@ struct Rows {
                 for (int x = 0; x < 32; ++x) {
                     const int t = step * 32 + x, id = x < 16 ? pg.id[0] : pg.id[1];
                     if (!(x < 16 ? ok[0] : ok[1]) || t >= w.end || left_out(w, t)) continue;
-                    if (t < limit[z] && page_base(w, id)[c4_v_scales(w.page, t & (w.page - 1), lb * D / 128, D)] == 255) poison = __builtin_nanf("");
+                    if (t < limit[z] && (x < 16 ? sight.u[0] : sight.u[1]) && page_base(w, id)[c4_v_scales(w.page, t & (w.page - 1), lb * D / 128, D)] == 255) poison = __builtin_nanf("");
                 }
 #pragma unroll
                 for (int j = 0; j < J; ++j) o[z][j] += poison;
@@ -595,7 +610,7 @@ struct Sweep : Rows<D, F32, NT> {
             __builtin_amdgcn_sched_barrier(0);                   // (what is asked for before the wait for LDS is waited for with it)
             next = pages_at(w, ahead + stride);
             later = kept_at(w, i + stride);
-            const bool masked = ((holes >> x) & 1) != 0 || i * 32 + 32 > w.clear;
+            const bool masked = ((holes >> x) & 1) != 0 || i * 32 + 32 > w.clear || uneven(w, i);
             holes &= ~(1u << x);
             if (ahead < stop) {
                 if (hole(w, ahead, pg)) holes |= 1u << x;

@@ -126,15 +126,41 @@ inline bool c4_choose_together(int64_t blocks, int pitch, size_t lds) {
     return pitch <= 2048 && lds <= 32768 && (blocks >= 256 || pitch <= 256);
 }
 
-// How the attention over chosen pages is cut: `splits` parts of a list of `budget` pages, a block each; `most` entries of the list to a
-// part.  `units`: tiles of 16 query heads of all tokens and K/V heads.
-struct C4Chosen { int splits, most; };
-constexpr int kC4ListMost = 1024;                    // entries of a part, which lie in LDS
-inline C4Chosen c4_chosen(int64_t units, int budget, int page) {
+// How the attention over chosen pages is cut.
+//   tokens   that a block takes together, as many as fill 16 query rows with their heads: over all of the pages that any of them has chosen.
+//            What a key costs is then shared, but where tokens choose different pages there are more of them to go through and fewer blocks.
+//            It pays from three tokens on where there are blocks for the chip without it.  us apart / together where tokens choose at
+//            random, and where they choose the same, 1024 keys of about 6000: 1 x 64 tokens of 40 heads 57 / 31, 56 / 14; 4 x 128 of 32 heads
+//            on 8 86 / 86, 82 / 27; 64 x 4 of 32 heads 187 / 153, 160 / 54; 4 x 16 of 32 heads, 512 keys 31 / 31, 31 / 12; but 1 x 16 of 32
+//            on 8 12 / 31, 12 / 13; 16 x 5 of 32 on 8 23 / 33, 21 / 14; two tokens, 64 x 2 of 32 on 8 31 / 36, 26 / 20
+//   splits   parts of a token's list, a block each, joined by a second launch: where there are few lists and they are long.  us in one
+//            part / in 4 / 8 / 16, of 32-key steps: 8 lists of 32 13.0 / 12.2 / 12.4 / 13.7, of 64 16.5 / 14.8 / 13.8 / 14.1, of 128 25 / 17 / 15 /
+//            16.5, of 256 45 / 23 / 19 / 18; 32 of 128 25 / 19 / 17 / 18; 128 of 128 27 / 23 / 24 / 31
+//   most     entries of a list to a part (tokens > 1: of the list of all)
+//   waves    of a block: eight while there are no more than 512 blocks.  us with four / eight: 8 lists of 32 steps 12.5 / 13.0, of 64 18.9 / 16.5,
+//            of 128 32 / 25; 512 of 32 17.8 / 17.4; 640 of 32 22.6 / 26; 5120 of 32 86 / 113
+struct C4Chosen { int tokens, splits, most, waves; };
+constexpr int kC4ListMost = 1024;                    // entries of a list in LDS
+constexpr int kC4TableMost = 4096;                   // of a block table that lists are shared in: 2 bytes each lie in LDS
+inline C4Chosen c4_chosen(bool f32, int d, int B, int N, int G, int H, int budget, int page, int max_pages) {
     C4Chosen c;
-    c.splits = (budget + kC4ListMost - 1) / kC4ListMost;
+    const int64_t apart = (int64_t)B * N * H * ((G + 15) / 16), steps = ((int64_t)budget * page + 31) / 32;
+    const int most_waves = f32 && d == 128 ? 4 : 8;
+    c.tokens = G <= 5 && N > 2 && apart >= 1536 && max_pages > 0 && max_pages <= kC4TableMost ? (N < 16 / G ? N : 16 / G) : 1;
+    const int64_t together = (int64_t)c.tokens * budget, most = together < max_pages ? together : max_pages;
+    if (c.tokens > 1 && most <= kC4ListMost) {
+        c.splits = 1;
+        c.most = (int)most;
+        c.waves = (int64_t)B * ((N + c.tokens - 1) / c.tokens) * H <= 512 ? most_waves : 4;
+        return c;
+    }
+    c.tokens = 1;
+    const int64_t parts = steps / 16 < 512 / apart ? steps / 16 : 512 / apart, need = (budget + kC4ListMost - 1) / kC4ListMost;
+    c.splits = (int)(parts > 2 ? (parts < budget ? parts : budget) : 1);
+    if (c.splits < need) c.splits = (int)need;
     c.most = (budget + c.splits - 1) / c.splits;
-    (void)units; (void)page;
+    c.splits = (budget + c.most - 1) / c.most;
+    c.waves = apart * c.splits <= 512 && c.splits == 1 ? most_waves : 4;
     return c;
 }
 

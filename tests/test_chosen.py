@@ -1,5 +1,8 @@
 """Rotation, rows rotated into the cache and pages that are chosen, without a GPU: the plain references, and every refusal."""
 import ctypes as C
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -28,6 +31,15 @@ def layout(*strides):
 @pytest.fixture(scope="module")
 def lib():
     return md.library()
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not found")
+def test_how_calls_are_cut(tmp_path):
+    exe = str(tmp_path / "cache4_chosen")
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-Wall", "-fsanitize=undefined", "-fno-sanitize-recover=all",
+                           os.path.join(os.path.dirname(os.path.abspath(__file__)), "plan", "cache4_chosen_main.cpp"), "-o", exe])
+    r = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout[-3000:]
 
 
 # ---- the references

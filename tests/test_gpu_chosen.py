@@ -379,7 +379,7 @@ class Chosen:
                 pick[rng.random(budget) < 0.3] = 2 ** 31 - 1
                 pick[rng.random(budget) < 0.1] = -(2 ** 31)
             else:
-                pick = np.arange(self.entries)
+                pick = np.arange(self.entries)[:budget]
             lists[b, i, h, :len(pick)] = pick
         self.lists = lists
 
@@ -455,6 +455,14 @@ ATTENDS = [
     dict(lengths=[3000, 700], N=2, Hq=2, H=1, d=64, page=16, budget=190, dtype=F32, keep=0.8, q_len=[2, 1]),
     dict(lengths=[700], N=1, Hq=18, H=1, d=128, page=16, budget=1500, dtype=F32, kind="any"),
     dict(lengths=[600, 90], N=1, Hq=2, H=2, d=64, page=16, budget=2100, dtype=BF16, kind="all"),
+    # several tokens together (1536 tokens and K/V heads and more, five heads to one at most): 4, 16, 3, 5 and 8 tokens
+    dict(lengths=[230, 150], N=200, Hq=16, H=4, d=128, page=16, budget=4, dtype=BF16, q_len=[200, 133]),
+    dict(lengths=[120, 70], N=65, Hq=13, H=13, d=64, page=32, budget=2, dtype=BF16, keep=0.5),
+    dict(lengths=[300, 200], N=261, Hq=15, H=3, d=64, page=64, budget=3, dtype=F32, kind="any", layout="heads"),
+    dict(lengths=[100, 391], N=390, Hq=6, H=2, d=128, page=16, budget=9, dtype=F32, keep=0.7, q_len=[-1, 390]),
+    dict(lengths=[66, 5, 33, 0], N=100, Hq=8, H=4, d=64, page=16, budget=2, dtype=BF16, kind="any", layout="heads"),     # rows before the first entry
+    dict(lengths=[3, 2], N=800, Hq=1, H=1, d=128, page=256, budget=1, dtype=F32),
+    dict(lengths=[97], N=97, Hq=16, H=16, d=128, page=16, budget=7, dtype=BF16, kind="all"),
 ]
 
 
@@ -490,6 +498,42 @@ def test_attend_chosen_nan_reaches_only_the_rows_that_see_it(dtype, d):
     out, lse = c.call(md)
     assert np.isnan(out).any() and not np.isnan(out).all()
     c.check(out, lse)
+
+
+@pytest.mark.parametrize("dtype, d", ((BF16, 64), (F32, 128)))
+def test_nan_reaches_only_the_tokens_that_have_chosen_its_page(dtype, d):
+    """Tokens that go together: a V or K that is no number counts for the tokens whose lists name its page and which see it."""
+    import paper_2411_10803_amd as md
+    c = Chosen(45, [400, 400], 97, 8, 8, d, 16, 6, dtype, keep=0.9)              # two tokens in sixteen rows at least: 8 heads of one query each
+    bad = np.full(d, 1.0)
+    bad[40] = np.nan
+    one = np.full(d, 1.0)
+    for b, t, h, k, v in ((0, 350, 0, one, bad), (0, 12, 1, bad, one), (1, 100, 2, bad, bad), (1, 399, 3, one, bad), (1, 64, 4, one, bad)):
+        slot = c.table[b, t // 16] * 16 + t % 16
+        ref.put(c.pool, slot, h, k, v, 16)
+        c.k[slot, h], c.v[slot, h] = ref.values(*ref.quantise(k)), ref.values(*ref.quantise(v))
+        c.keep[b, t] = 1
+    c.keep[1, 64] = 0
+    out, lse = c.call(md)
+    assert np.isnan(out).any() and not np.isnan(out).all()
+    c.check(out, lse)
+
+
+def test_tokens_together_are_tokens_apart():
+    """A call whose tokens go together against calls of one token each."""
+    import torch
+    import paper_2411_10803_amd as md
+    c = Chosen(46, [500, 333], 100, 16, 8, 128, 32, 5, BF16, keep=0.8)
+    a = c.args()
+    keep = dev(c.keep)
+    out, lse = torch.zeros((2, 100, 16, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, 16, 100), device="cuda")
+    md.mustdrop_cache4_attend_chosen(*a, out=out, lse=lse, keep=keep)
+    for i in range(0, 100, 9):
+        o, l = torch.zeros((2, 1, 16, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, 16, 1), device="cuda")
+        md.mustdrop_cache4_attend_chosen(a[0][:, i:i + 1], a[1], a[2], a[3] - (99 - i), a[4][:, i:i + 1].contiguous(), a[5], out=o, lse=l, keep=keep)
+        torch.cuda.synchronize()
+        x, y = host(out[:, i:i + 1]), host(o)
+        assert (np.abs(x - y) <= 2.0 ** -7 * np.abs(y) + 2.0 ** -14).all() and np.allclose(host(lse[:, :, i:i + 1]), host(l), atol=1e-5)
 
 
 def test_attend_chosen_in_a_pool_beyond_four_gigabytes():
