@@ -637,23 +637,30 @@ def rotary_table(n_pos, pairs, base=10000.0, device="cuda"):
 def _angles(positions, table, turn, index, B, N):
     """Checks positions [axes, B, L], table [n_pos, pairs, 2] and index [B, N]; returns (L, n_pos)."""
     import torch
-    _typed(torch.int32, positions=positions, index=index)
-    _typed(torch.float32, table=table)
-    L, n_pos = positions.shape[-1], table.shape[0]
-    _shaped("positions", positions, (turn.axes, B, L))
-    _shaped("table", table, (n_pos, turn.pairs, 2))
-    _shaped("index", index, (B, N))
-    return L, n_pos
+    at, angles = positions.shape, table.shape
+    if positions.dtype is not torch.int32 or table.dtype is not torch.float32 or len(at) != 3 or at != (turn.axes, B, at[2]) or \
+            len(angles) != 3 or angles != (angles[0], turn.pairs, 2):
+        _typed(torch.int32, positions=positions)
+        _typed(torch.float32, table=table)
+        _shaped("positions", positions, (turn.axes, B, at[-1]))
+        _shaped("table", table, (angles[0], turn.pairs, 2))
+    if index is not None:
+        _typed(torch.int32, index=index)
+        _shaped("index", index, (B, N))
+    return at[2], angles[0]
 
 
-def _side(t, out, names):
-    """Pointers and layouts of rows [B, N, H, d] and of what they become (None: themselves)."""
+def _side(t, out, shape, names):
+    """Pointers and layouts of rows of this shape and of what they become (None: themselves)."""
+    p, lay = _rows(t, names[0])
+    lay = lay and C.byref(lay)
     if out is None:
-        out = t
-    _typed(t.dtype, **{names[1]: out})
-    _shaped(names[1], out, t.shape)
-    (p, lay), (o, out_lay) = _rows(t, names[0]), _rows(out, names[1])
-    return out, p, lay and C.byref(lay), o, out_lay and C.byref(out_lay)
+        return t, p, lay, p, lay
+    if out.dtype is not t.dtype or out.shape != shape:
+        _typed(t.dtype, **{names[1]: out})
+        _shaped(names[1], out, shape)
+    o, out_lay = _rows(out, names[1])
+    return out, p, lay, o, out_lay and C.byref(out_lay)
 
 
 def mustdrop_rotate(q, positions, table, turn, k=None, q_out=None, k_out=None, index=None, rows=None, inverse=False, stream=None):
@@ -665,15 +672,18 @@ def mustdrop_rotate(q, positions, table, turn, k=None, q_out=None, k_out=None, i
     if k is None and k_out is not None:
         raise ValueError("k_out without k")
     L, n_pos = _angles(positions, table, turn, index, B, N)
-    _typed(torch.int32, rows=rows)
-    _shaped("rows", rows, (B,))
-    q_out, qp, ql, qo, qol = _side(q, q_out, ("q", "q_out"))
+    if rows is not None:
+        _typed(torch.int32, rows=rows)
+        _shaped("rows", rows, (B,))
+    q_out, qp, ql, qo, qol = _side(q, q_out, (B, N, Hq, d), ("q", "q_out"))
     H, kp, kl, ko, kol = 0, None, None, None, None
     if k is not None:
-        H = k.shape[2]
-        _typed(q.dtype, k=k)
-        _shaped("k", k, (B, N, H, d))
-        k_out, kp, kl, ko, kol = _side(k, k_out, ("k", "k_out"))
+        shape = k.shape
+        if k.dtype is not q.dtype or len(shape) != 4 or shape != (B, N, shape[2], d):
+            _typed(q.dtype, k=k)
+            _shaped("k", k, (B, N, shape[2], d))
+        H = shape[2]
+        k_out, kp, kl, ko, kol = _side(k, k_out, shape, ("k", "k_out"))
     raw = _here(stream, q, k, positions, table, q_out, k_out, index, rows)
     _call("mustdrop_rotate",
         qp, kp, _dtype_code(q), _ptr(positions), _ptr(index), _ptr(table), _ptr(rows),
@@ -701,7 +711,7 @@ def mustdrop_cache4_append(q, k_new, v_new, positions, table, turn, slots, cache
         Hq = q.shape[2]
         _typed(k_new.dtype, q=q)
         _shaped("q", q, (B, N, Hq, d))
-        q_out, qp, ql, qo, qol = _side(q, q_out, ("q", "q_out"))
+        q_out, qp, ql, qo, qol = _side(q, q_out, (B, N, Hq, d), ("q", "q_out"))
     raw = _here(stream, k_new, v_new, q, q_out, positions, table, slots, cache, index)
     _call("mustdrop_cache4_append",
         qp, kp, vp, _dtype_code(k_new), _ptr(positions), _ptr(index), _ptr(table), _ptr(slots), _ptr(cache),
