@@ -622,6 +622,11 @@ __device__ __forceinline__ Pages pages_at(const Listed& w, int step) {
     const Entries e = listed_at(w, step);
     return Pages{{e.id[0], e.id[1]}};
 }
+// (a list holds nothing but pages that are there)
+__device__ __forceinline__ bool there(const Listed& w, int step, const Pages&, int u) { return step * 32 + 16 * u < w.end; }
+__device__ __forceinline__ bool hole(const Listed& w, int step, const Pages&) { return step * 32 + 16 >= w.end; }
+__device__ __forceinline__ Pages pages_for_mask(const Listed&, int) { return Pages{{0, 0}}; }
+__device__ __forceinline__ Pages pages_by_number(const Listed& w, int step, const Pages&) { return pages_at(w, step); }
 __device__ __forceinline__ Kept kept_at(const Listed& w, int step) {
     Kept r;
     if (w.keep) {

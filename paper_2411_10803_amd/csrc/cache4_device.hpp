@@ -245,6 +245,9 @@ __device__ __forceinline__ bool there(const Walk& w, int step, const Pages& p, i
     return step * 32 + 16 * u < w.end && c4_page_id(p.id[u], w.n_pages) >= 0;
 }
 __device__ __forceinline__ bool hole(const Walk& w, int step, const Pages& p) { return !(there(w, step, p, 0) && there(w, step, p, 1)); }
+// A step's pages where only whether they are there is of interest, and where their numbers are.
+__device__ __forceinline__ Pages pages_for_mask(const Walk& w, int step) { return pages_at(w, step); }
+__device__ __forceinline__ Pages pages_by_number(const Walk&, int, const Pages& p) { return p; }
 // (page 0 is read in the place of one that is not there, and masked)
 __device__ __forceinline__ bytes_t page_base(const Walk& w, int id) {
     return w.base + ((uint64_t)(((uint32_t)id < (uint32_t)w.n_pages ? (uint32_t)id : 0u) * w.pitch) << 6);
@@ -348,8 +351,8 @@ struct Rows {
         constexpr uint32_t kTops = 0x80808080u;
         const auto nonzero = [](uint32_t x) { return (((x & ~kTops) + ~kTops) | x) & kTops; };
         const auto first = [](int n) { return n <= 0 ? 0u : kTops >> (32 - 8 * min(n, 4)); };
-        const Pages pg = pages_at(w, step);
-        const bool ok[2] = {there(w, step, pg, 0), there(w, step, pg, 1)};
+        const Pages known = pages_for_mask(w, step);
+        const bool ok[2] = {there(w, step, known, 0), there(w, step, known, 1)};
         const Sight sight = sight_at(w, step);
         const bool inside = step * 32 + 32 <= w.level && ok[0] && ok[1];         // (a prompt's piece has few steps that are not)
         uint32_t nan = 0;
@@ -378,6 +381,7 @@ struct Rows {
         for (int z = 0; z < NT; ++z) hides[z] = ~hides[z];
         // A NaN in V of a key that some rows see and others do not: the rows that see it get it in that group's channels here.
         if (__any(nan != 0)) {
+            const Pages pg = pages_by_number(w, step, known);
 #pragma unroll
             for (int z = 0; z < NT; ++z) {
                 float poison = 0.f;
