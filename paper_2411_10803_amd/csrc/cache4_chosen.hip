@@ -42,7 +42,7 @@ __device__ __forceinline__ void halve(float (&v)[16], int lane) {
 // A wave per page and head.  Sixteen (d = 64: eight) lanes side by side have the channels of one token, eight each: of all tokens they keep the
 // largest values and the largest with the sign turned, 16 numbers.  The four (eight) lanes of the same channels then halve these among
 // them until each has 4 (2) of the one kind, which is a word (half of one) of the result.  (Sixteen bytes to a lane are fewer loads, but 64
-// numbers to halve over sixteen lanes: 22 us for the bounds of 16 x up to 5888 entries of 8 heads instead of @@.)
+// numbers to halve over sixteen lanes: 22 us for the bounds of 16 x up to 5888 entries of 8 heads instead of 10.6.)
 constexpr int kBoundsAhead = 8;                      // tokens of a lane that are on their way together
 template <int D>
 __global__ __launch_bounds__(256) void cache4_bounds_kernel(
@@ -207,7 +207,7 @@ struct Steps {
 // 16 query rows (the G heads of some tokens, filled up with zeros to a power of two; MULTI, more than 16 heads: one 16 after the other) against
 // T tiles of 16 pages at a time, by a wave of a block of 256 threads.  Lane (n, lb) has bytes lb * 16 .. + 15 of every 64 of row n of either
 // operand.  A block's waves turn the queries into whole numbers together and share them through LDS (each for itself: 64 x up to 4096 entries
-// of 32 heads 13.2 us); MULTI: each for itself.
+// of 32 heads 13.2 us instead of 12.3); MULTI: each for itself.
 // There are few instructions to a byte, and nothing else to do while a wave waits: what does not depend on the sample's length is asked for
 // together with it, and nothing is loaded under a condition of a lane (rows and pages that are not there are others' in their place, and
 // count as nothing).
@@ -723,7 +723,8 @@ __device__ __forceinline__ void each_entry(const AttendArgs& A, const int32_t* f
     for (int base = v0; base < v1; base += kWave) {
         const int e = entry(base + lane);
         int top = e;                                 // the largest up to here
-        if (__any(lane < kWave - 1 && base + lane < v1 - 1 && __shfl_down(e, 1, kWave) <= e)) {      // (a list that ascends is its own)
+        const int after = __shfl_down(e, 1, kWave);
+        if (__any(lane < kWave - 1 && base + lane < v1 - 1 && after <= e)) {                         // (a list that ascends is its own)
 #pragma unroll
             for (int x = 1; x < kWave; x <<= 1) {
                 const int other = __shfl_up(top, x, kWave);

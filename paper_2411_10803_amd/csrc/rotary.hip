@@ -120,7 +120,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(Side q, Side k, Angles ang,
                                                      FastDiv groups, FastDiv tokens, int adjacent)
 {
     const int per = 256 / items.d, slot = items.div(threadIdx.x), item = threadIdx.x - slot * items.d;
-    const int u = (int)blockIdx.x * per + slot;      // (the host checks that this fits 31 bits)
+    const int u = (int)blockIdx.x * per + slot;      // (the host checks that this fits 31 bits, behind the last one too)
     if (slot >= per || u >= total) return;
     const int row = groups.div(u), g = u - row * groups.d, b = tokens.div(row), i = row - b * tokens.d;
     if (rows && i >= rows[b]) return;
@@ -325,7 +325,7 @@ int rotate_impl(const void* q, const void* k, int dtype, const int32_t* position
     const long all = (long)B * N;
     // wide loads where no pair's halves are split over them
     const int W = ang.turn.pairs % 8 == 0 && d % 16 == 0 ? 8 : 4, items = d / (2 * W);
-    if (all > kMaxRows || all * (Hq + H) * items > 0x7FFFFFFFl) return fail(MD_ESHAPE, "rotate: %ld rows of %d heads are too many for one call", all, Hq + H);
+    if (all > kMaxRows || all * (Hq + H) * items > 0x7FFFFFFFl - 511) return fail(MD_ESHAPE, "rotate: %ld rows of %d heads are too many for one call", all, Hq + H);
     const size_t qi = rows_bytes(a.xl, B, N, Hq, d, dtype), qo = rows_bytes(a.yl, B, N, Hq, d, dtype);
     const size_t ki = k ? rows_bytes(c.xl, B, N, H, d, dtype) : 0, ko = k ? rows_bytes(c.yl, B, N, H, d, dtype) : 0;
     const Range r[] = {{q_out, qo}, {k_out, ko}, {q, same_place(q, a.xl, q_out, a.yl) ? 0 : qi}, {k, same_place(k, c.xl, k_out, c.yl) ? 0 : ki},

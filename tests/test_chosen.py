@@ -140,6 +140,9 @@ def test_rotate_refusals(lib):
     assert rotate(lib, ko=P(7)) == EALIAS and rotate(lib, rows=P(8)) == EALIAS and rotate(lib, ko=P(1)) == EALIAS
     assert rotate(lib, ko=moved(P(10), 8)) == EALIGN
     assert rotate(lib, B=1 << 12, N=1 << 12, L=1 << 12, Hq=1 << 10) == ESHAPE    # 2^34 rows and heads
+    few = dict(k=None, ko=None, B=1 << 8, N=(1 << 20) - 1, L=1 << 20, Hq=8, d=8, turn=turn(pairs=4))      # 2^31 - 2^11 pieces of 8 channels
+    assert rotate(lib, **dict(few, N=1 << 20)) == ESHAPE and b"too many" in lib.mustdrop_last_error()
+    assert rotate(lib, **dict(few, dtype=2)) == EDTYPE and rotate(lib, **dict(few, q=moved(P(1), 8))) == EALIGN
 
 
 def test_append_refusals(lib):
