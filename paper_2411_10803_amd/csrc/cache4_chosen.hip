@@ -383,55 +383,74 @@ __device__ __forceinline__ uint32_t ordered(float score) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// The choice by one wave, whose lane l has the scores of pages l, l + 64, .. in registers: the largest number that as many scores as there
-// are to take are no smaller than, bit by bit, with a vote for each; then the first of those that are equal to it.
+// Where the chosen scores end: those above `bound`, and the first `ties` of those equal to it.
+struct Border { uint32_t bound; int ties; };
+// The border of the `need` largest of the keys that lanes have with a bit in `ranked` (there are more), all between `least` and `most`: by histograms
+// of eight bits from the first one on that differs, until a place of one is taken whole.  By a wave (hist: 256 ints of its own) or by a
+// block of 256 threads (4 x 256 ints, zeros).  us for 64 of up to 1563 scores, 80 times, a block each: 5.4; with votes instead, for two bits at
+// a time, 8.8.
+template <int K, bool BLOCK>
+__device__ __forceinline__ Border border_of(const uint32_t (&key)[K], uint32_t ranked, int need, uint32_t least, uint32_t most, int* hist) {
+    if (need <= 0) return Border{0xFFFFFFFEu, 0};
+    const int lane = lane_id(), from = 31 - __clz((int)((least ^ most) | 1u));
+    uint32_t bound = (most >> from >> 1) << 1 << from, width = 0xFFFFFFFFu >> (31 - from);       // (the width less one)
+    for (int sh = max(from - 7, 0);; sh = max(sh - 8, 0)) {
+        if (!BLOCK) reinterpret_cast<i32x4*>(hist)[lane] = i32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+            if (((ranked >> j) & 1) && key[j] - bound <= width) atomicAdd(&hist[(key[j] - bound) >> sh], 1);
+        if (BLOCK) block_sync_lds();
+        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        // places 255, 254, .. by four to a lane
+        const i32x4 c = reinterpret_cast<const i32x4*>(hist)[kWave - 1 - lane];
+        const int sum = (c[3] + c[2]) + (c[1] + c[0]), upto = wave_incl_scan_i(sum);
+        int before = upto - sum, place = -1, left = 0, in = 0;
+#pragma unroll
+        for (int x = 3; x >= 0; --x) {
+            if (before < need && before + c[x] >= need) { place = 4 * (kWave - 1 - lane) + x; left = need - before; in = c[x]; }
+            before += c[x];
+        }
+        const int at = (int)__builtin_ctzll(__ballot(place >= 0));
+        place = __builtin_amdgcn_readlane(place, at);
+        need = __builtin_amdgcn_readlane(left, at);
+        in = __builtin_amdgcn_readlane(in, at);
+        bound += (uint32_t)place << sh;
+        if (need == in) return Border{bound - 1, 0};             // (a key is never 0, and so is no bound that is taken whole)
+        if (sh == 0) return Border{bound, need};
+        width = (1u << sh) - 1;
+        if (BLOCK) hist += 256;
+    }
+}
+
+// The choice by one wave, whose lane l has the scores of pages l, l + 64, .. in registers.
 template <int K>
-__device__ __forceinline__ void choose_by_wave(const Choose& A, const float* score, int P, int32_t* to) {
-    const int lane = lane_id();
-    const int hi = P - A.last, taken = A.budget;
+__device__ __forceinline__ void choose_by_wave(const Choose& A, const float* score, int P, int32_t* to, int* hist) {
+    const int lane = lane_id(), hi = P - A.last, taken = A.budget;
     if (P <= A.budget) {
         for (int x = lane; x < A.budget; x += kWave) to[x] = x < P ? x : -1;
         return;
     }
-    uint32_t key[K];
+    uint32_t key[K], least = 0xFFFFFFFFu, most = 0, ranked = 0;
 #pragma unroll
     for (int j = 0; j < K; ++j) {
         const int e = j * kWave + lane;
-        key[j] = e >= P ? 0u : e < A.first || e >= hi ? 0xFFFFFFFFu : ordered(score[e]);
+        const bool in = e >= A.first && e < hi;
+        key[j] = in ? ordered(score[e]) : e < P ? 0xFFFFFFFFu : 0u;
+        least = min(least, in ? key[j] : 0xFFFFFFFFu);
+        most = max(most, in ? key[j] : 0u);
+        ranked |= in ? 1u << j : 0u;
     }
-    // from the first bit on that differs
-    uint32_t least = 0xFFFFFFFFu, most = 0;
-#pragma unroll
-    for (int j = 0; j < K; ++j) { least = min(least, key[j] ? key[j] : 0xFFFFFFFFu); most = max(most, key[j] != 0xFFFFFFFFu ? key[j] : 0u); }
-    least = wave_min_u32(least);
-    most = max(~wave_min_u32(~most), least);         // (there may be nothing but pages that are always taken)
-    const int from = 31 - __clz((int)((least ^ most) | 1u));
-    uint32_t bound = (most >> from >> 1) << 1 << from;
-    int above = P;                                   // that are no smaller
-    for (int bit = from; bit >= 0 && above != taken; --bit) {
-        const uint32_t next = bound | (1u << bit);
-        int count = 0;
-#pragma unroll
-        for (int j = 0; j < K; ++j) count += __popcll(__ballot(key[j] >= next));
-        if (count >= taken) { bound = next; above = count; }
-    }
-    int ties = above - taken;                        // of the smallest, as many are too many: the last ones
-    if (ties > 0) {
-        int equal = 0;
-#pragma unroll
-        for (int j = 0; j < K; ++j) equal += __popcll(__ballot(key[j] == bound));
-        ties = equal - ties;                         // that stay
-    }
-    const bool all = above == taken;
-    int done = 0;
+    const Border r = border_of<K, false>(key, ranked, taken - A.first - A.last, wave_min_u32(least), ~wave_min_u32(~most), hist);
+    int done = 0, ties = r.ties;
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-        const unsigned long long same = __ballot(key[j] == bound);
-        bool in = all ? key[j] >= bound && key[j] != 0u : key[j] > bound || (key[j] == bound && lanes_below(same) < ties);
-        if (!all) ties -= __popcll(same);
+        if (j * kWave >= P) break;
+        const unsigned long long same = __ballot(ties > 0 && key[j] == r.bound);
+        const bool in = key[j] > r.bound || (ties > 0 && key[j] == r.bound && lanes_below(same) < ties);
+        ties -= (int)__popcll(same);
         const unsigned long long on = __ballot(in);
         if (in) to[done + lanes_below(on)] = j * kWave + lane;
-        done += __popcll(on);
+        done += (int)__popcll(on);
     }
 }
 
@@ -440,6 +459,7 @@ template <int D, bool F32, int K>
 __global__ __launch_bounds__(256, 4) void cache4_score_choose_kernel(Choose A, FastDiv tiles, FastDiv heads)
 {
     extern __shared__ f32x4 s_lds[];
+    __shared__ __align__(16) int s_hist[4][256];
     float* s_score = reinterpret_cast<float*>(s_lds);
     const int bh = tiles.div(blockIdx.x), tile = blockIdx.x - bh * tiles.d, b = heads.div(bh), h = bh - b * heads.d;
     const int i0 = tile * A.per, waves = blockDim.x >> 6;
@@ -462,15 +482,14 @@ __global__ __launch_bounds__(256, 4) void cache4_score_choose_kernel(Choose A, F
         __syncthreads();
     }
     for (int i = i0 + wave_id(); i <= last; i += waves)
-        choose_by_wave<K>(A, s_score + (i - i0) * A.pitch, sc.seen_by(i), A.chosen + (((long)b * A.N + i) * A.H + h) * A.budget);
+        choose_by_wave<K>(A, s_score + (i - i0) * A.pitch, sc.seen_by(i), A.chosen + (((long)b * A.N + i) * A.H + h) * A.budget, s_hist[wave_id()]);
 }
 
-// The same by the four waves of a block, of up to 2048 scores in the workspace: wave w's lane l has those of pages (4 j + w) * 64 + l.  Two bits
-// at a time: the waves' votes are added up through LDS, a barrier for each.
+// The same by the four waves of a block, of up to 2048 scores in the workspace: wave w's lane l has those of pages (4 j + w) * 64 + l.
 __global__ __launch_bounds__(256) void cache4_choose_block_kernel(Choose A, FastDiv tokens, FastDiv heads)
 {
     constexpr int K = 8;
-    __shared__ i32x4 s_votes[2][4];
+    __shared__ __align__(16) int s_hist[4 * 256];
     __shared__ uint32_t s_least[4], s_most[4];
     __shared__ int s_count[4 * K];
     const int bh = tokens.div(blockIdx.x), i = blockIdx.x - bh * tokens.d, b = heads.div(bh), h = bh - b * heads.d;
@@ -492,56 +511,39 @@ __global__ __launch_bounds__(256) void cache4_choose_block_kernel(Choose A, Fast
         for (int x = threadIdx.x; x < taken; x += 256) to[x] = x < P ? x : -1;
         return;
     }
-    uint32_t key[K], least = 0xFFFFFFFFu, most = 0;
+    uint32_t key[K], least = 0xFFFFFFFFu, most = 0, ranked = 0;
 #pragma unroll
     for (int j = 0; j < K; ++j) {
         const int e = (4 * j + wv) * kWave + lane;
-        key[j] = e >= P ? 0u : e < A.first || e >= hi ? 0xFFFFFFFFu : ordered(f[j]);
-        least = min(least, key[j] ? key[j] : 0xFFFFFFFFu);
-        most = max(most, key[j] != 0xFFFFFFFFu ? key[j] : 0u);
+        const bool in = e >= A.first && e < hi;
+        key[j] = in ? ordered(f[j]) : e < P ? 0xFFFFFFFFu : 0u;
+        least = min(least, in ? key[j] : 0xFFFFFFFFu);
+        most = max(most, in ? key[j] : 0u);
+        ranked |= in ? 1u << j : 0u;
     }
     least = wave_min_u32(least);
     most = ~wave_min_u32(~most);
     if (lane == 0) { s_least[wv] = least; s_most[wv] = most; }
+    reinterpret_cast<i32x4*>(s_hist)[threadIdx.x] = i32x4{0, 0, 0, 0};
     block_sync_lds();
     least = min(min(s_least[0], s_least[1]), min(s_least[2], s_least[3]));
-    most = max(max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3])), least);
-    int bit = (31 - __clz((int)((least ^ most) | 1u))) | 1;          // the upper one of two bits
-    uint32_t bound = (uint32_t)((uint64_t)most >> (bit + 1) << (bit + 1));
-    int above = P, turn = 0;                         // that are no smaller
-    for (; bit > 0 && above != taken; bit -= 2, turn ^= 1) {
-        const uint32_t unit = 1u << (bit - 1);
-        i32x4 votes{0, 0, 0, 0};
-#pragma unroll
-        for (int j = 0; j < K; ++j)
-#pragma unroll
-            for (int x = 0; x < 3; ++x) votes[x] += (int)__popcll(__ballot(key[j] >= bound + unit * (x + 1)));
-        if (lane == 0) s_votes[turn][wv] = votes;
-        block_sync_lds();
-        votes = (s_votes[turn][0] + s_votes[turn][1]) + (s_votes[turn][2] + s_votes[turn][3]);
-        const int x = votes[2] >= taken ? 3 : votes[1] >= taken ? 2 : votes[0] >= taken ? 1 : 0;
-        if (x) { bound += unit * x; above = votes[x - 1]; }
-        bound = (uint32_t)__builtin_amdgcn_readfirstlane((int)bound);
-        above = __builtin_amdgcn_readfirstlane(above);
-    }
+    most = max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]));
+    const Border r = border_of<K, true>(key, ranked, taken - A.first - A.last, least, most, s_hist);
     // larger ones and equal ones of 64 at a time, and before them
-    const bool all = above == taken;                 // (then those that are equal count as larger)
     int mine[K];
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-        const int larger = (int)__popcll(__ballot(all ? key[j] >= bound && key[j] != 0u : key[j] > bound));
-        mine[j] = larger | (all ? 0 : (int)__popcll(__ballot(key[j] == bound)) << 16);
+        mine[j] = (int)__popcll(__ballot(key[j] > r.bound)) | (r.ties ? (int)__popcll(__ballot(key[j] == r.bound)) << 16 : 0);
         if (lane == 0) s_count[4 * j + wv] = mine[j];
     }
     block_sync_lds();
     const int count = lane < 4 * K ? s_count[lane] : 0, upto = wave_incl_scan_i(count);
-    const int ties = taken - (__builtin_amdgcn_readlane(upto, kWave - 1) & 0xFFFF);
 #pragma unroll
     for (int j = 0; j < K; ++j) {
         const int before = __builtin_amdgcn_readlane(upto, 4 * j + wv) - mine[j];
-        const bool larger = all ? key[j] >= bound && key[j] != 0u : key[j] > bound, same = !all && key[j] == bound;
+        const bool larger = key[j] > r.bound, same = r.ties && key[j] == r.bound;
         const int equal = (before >> 16) + lanes_below(__ballot(same));
-        if (larger || (same && equal < ties)) to[(before & 0xFFFF) + lanes_below(__ballot(larger)) + min(equal, ties)] = (4 * j + wv) * kWave + lane;
+        if (larger || (same && equal < r.ties)) to[(before & 0xFFFF) + lanes_below(__ballot(larger)) + min(equal, r.ties)] = (4 * j + wv) * kWave + lane;
     }
 }
 

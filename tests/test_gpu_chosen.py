@@ -289,6 +289,11 @@ CHOICES = [
     ([40000, 39000, 100], 1, 4, 2, 64, 16, 1, 1, 1200, BF16, "few"),             # 2500 pages
     ([33000], 2, 2, 1, 128, 16, 0, 1, 3, F32, "few"),
     ([1 << 30, -5], 1, 1, 1, 64, 16, 0, 1, 2, BF16, ""),                         # lengths out of range
+    # scores and choice in one launch: many tiles of query rows, up to 256, 768 and 2048 pages
+    ([300 * (b % 14) + b for b in range(17)], 1, 16, 16, 128, 16, 1, 1, 20, BF16, "few"),
+    ([600 * (b % 10) + 17 * b for b in range(18)], 1, 30, 15, 64, 16, 0, 1, 40, F32, ""),
+    ([1500 * (b % 12) for b in range(26)], 1, 30, 10, 128, 16, 1, 0, 130, BF16, "few heads"),
+    ([3000 + 90 * b for b in range(11)], 23, 12, 2, 64, 64, 1, 1, 8, BF16, "q_len"),
 ]
 
 
