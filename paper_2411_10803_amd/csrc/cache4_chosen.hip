@@ -125,7 +125,9 @@ struct Choose {
     KvLayout ql;
     int B, N, G, H, n_pages, max_pages, page_shift, pitch;
     int first, last, budget;
-    int lanes, subs, per;                            // query heads of a token side by side (a power of two), tiles of them, tokens of a tile
+    int lanes, subs, per, tiles;                     // query heads of a token side by side (a power of two), tiles of them, tokens of a tile, tiles of tokens
+    bool together;                                   // (what the host goes by)
+    size_t lds;
 };
 
 // Pages that row i of sample b sees; -1 where there is no such row.
@@ -971,7 +973,10 @@ int choose_plan(const char* who, int B, int N, int Hq, int H, int d, int n_pages
     A->per = 16 / A->lanes;
     if ((long)N * A->G > (1l << 20)) return fail(MD_ESHAPE, "%s: %d tokens of %d query heads are too many for one call", who, N, Hq);
     if ((long)B * H > kMaxUnits || (long)B * H * N > kMaxUnits) return fail(MD_ESHAPE, "%s: %d samples of %d tokens and %d heads are too many for one call", who, B, N, H);
-    *bytes = round_up((size_t)B * H * N * A->pitch * 4, 256);
+    A->tiles = (N + A->per - 1) / A->per;
+    A->lds = 64 + 32 * (d + 16) + (size_t)A->per * A->pitch * 4;
+    A->together = A->subs == 1 && c4_choose_together((int64_t)B * H * A->tiles, A->pitch, A->lds);
+    *bytes = A->together ? 256 : round_up((size_t)B * H * N * A->pitch * 4, 256);        // (scores of one launch for the next)
     return MD_OK;
 }
 
@@ -1005,14 +1010,12 @@ int choose_impl(const void* q, int dtype, const int8_t* bounds, const uint8_t* s
     A.scores = static_cast<float*>(workspace);
     A.first = first_pages; A.last = last_pages; A.budget = budget;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const int tiles = (N + A.per - 1) / A.per, chunks = (max_pages + 64 * kScoreTiles - 1) / (64 * kScoreTiles);
+    const int tiles = A.tiles, chunks = (max_pages + 64 * kScoreTiles - 1) / (64 * kScoreTiles);
     if (chunks > 65535) return fail(MD_ESHAPE, "cache4_choose: %d pages are too many for one request", max_pages);
     const long blocks = (long)B * H * tiles;
-    const size_t lds = 64 + 32 * (d + 16) + (size_t)A.per * A.pitch * 4;
-    if (A.subs == 1 && c4_choose_together(blocks, A.pitch, lds)) {
-        const int threads = 256;
+    if (A.together) {
 #define MD_C4_CHOOSE2(D_, F_, K_)                                                                                                         \
-    MD_LAUNCH("cache4_score_choose", st, (cache4_score_choose_kernel<D_, F_, K_>), (int)blocks, threads, lds, A, FastDiv::make(tiles), FastDiv::make(H))
+    MD_LAUNCH("cache4_score_choose", st, (cache4_score_choose_kernel<D_, F_, K_>), (int)blocks, 256, A.lds, A, FastDiv::make(tiles), FastDiv::make(H))
 #define MD_C4_CHOOSE(D_, F_)                                                                                                              \
     do { if (max_pages <= 256) MD_C4_CHOOSE2(D_, F_, 4); else if (max_pages <= 768) MD_C4_CHOOSE2(D_, F_, 12); else MD_C4_CHOOSE2(D_, F_, 32); } while (0)
         if (d == 128) { if (dtype == MD_F32) MD_C4_CHOOSE(128, true); else MD_C4_CHOOSE(128, false); }

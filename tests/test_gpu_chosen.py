@@ -289,6 +289,7 @@ CHOICES = [
     ([40000, 39000, 100], 1, 4, 2, 64, 16, 1, 1, 1200, BF16, "few"),             # 2500 pages
     ([33000], 2, 2, 1, 128, 16, 0, 1, 3, F32, "few"),
     ([1 << 30, -5], 1, 1, 1, 64, 16, 0, 1, 2, BF16, ""),                         # lengths out of range
+    ([140000, 131], 1, 2, 1, 64, 16, 0, 1, 37, BF16, "few"),                     # 8750 pages
     # scores and choice in one launch: many tiles of query rows, up to 256, 768 and 2048 pages
     ([300 * (b % 14) + b for b in range(17)], 1, 16, 16, 128, 16, 1, 1, 20, BF16, "few"),
     ([600 * (b % 10) + 17 * b for b in range(18)], 1, 30, 15, 64, 16, 0, 1, 40, F32, ""),
@@ -564,6 +565,18 @@ def test_attend_chosen_in_a_pool_beyond_four_gigabytes():
     md.mustdrop_cache4_choose(c.q, *small, dev(c.table), args[3], 32, picks[1])
     torch.cuda.synchronize()
     assert torch.equal(*picks)
+    # rows into the last pages
+    k, q = (torch.randn((1, 3, h, 128), device="cuda").bfloat16() for h in (H, 2))
+    at, table, turn = torch.tensor([[[5, 600, 31]]], dtype=torch.int32, device="cuda"), md.rotary_table(700, 64), md.rotary([64])
+    slots = torch.arange(n_pages * 32 - 3, n_pages * 32, dtype=torch.int32, device="cuda")[None].contiguous()
+    qo = md.mustdrop_cache4_append(q, k, k, at, table, turn, slots, cache, q_out=torch.zeros_like(q))
+    want, kt = md.mustdrop_rotate(q, at, table, turn, k=k.clone(), q_out=torch.zeros_like(q))
+    ko, vo = torch.zeros_like(k), torch.zeros_like(k)
+    md.mustdrop_cache4_read(cache, dev(np.array([[n_pages - 1]], np.int32)), dev(np.array([32], np.int32)), ko, vo, first=dev(np.array([29], np.int32)))
+    torch.cuda.synchronize()
+    tk = cr.turned(host(k)[0].astype(np.float32), host(at)[:, 0], host(table), np.zeros(64, np.int64))
+    assert torch.equal(qo, want) and same(host(kt)[0], rounded(tk, BF16))
+    assert same(host(ko)[0], ref.values(*ref.quantise(tk))) and same(host(vo)[0], ref.values(*ref.quantise(host(k)[0])))
 
 
 def test_all_pages_chosen_is_the_attention_over_all():
