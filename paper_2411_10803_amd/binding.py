@@ -490,8 +490,11 @@ def _rows(t, what):
 
 def _row_pair(k, v, names):
     """Pointers and the one layout of two [B, N, H, d] views of one type and shape."""
-    _typed(k.dtype, **{names[1]: v})
-    _shaped(names[1], v, k.shape)
+    if v.dtype is not k.dtype or v.shape != k.shape:
+        _typed(k.dtype, **{names[1]: v})
+        _shaped(names[1], v, k.shape)
+    if k.is_contiguous() and v.is_contiguous():
+        return k.data_ptr(), v.data_ptr(), None
     (kp, lay), (vp, other) = _rows(k, names[0]), _rows(v, names[1])
     if (lay is None) != (other is None) or (lay and (lay.batch, lay.token, lay.head) != (other.batch, other.token, other.head)):
         raise ValueError(f"{names[0]} and {names[1]} must have one layout")
@@ -634,31 +637,44 @@ def rotary_table(n_pos, pairs, base=10000.0, device="cuda"):
     return torch.from_numpy(np.stack([np.cos(at), np.sin(at)], axis=-1).astype(np.float32)).to(device)
 
 
-def _angles(positions, table, turn, index, B, N):
-    """Checks positions [axes, B, L], table [n_pos, pairs, 2] and index [B, N]; returns (L, n_pos)."""
-    import torch
+def _needed(name, t, dtype, shape):
+    """Says what is wrong with a tensor that is not contiguous, of this type and of this shape.  (The calls below look at these three
+    themselves: a function for each of a call's tensors took a third of the time that the host spends on it.)"""
+    _typed(dtype, **{name: t})
+    _shaped(name, t, shape)
+    assert t.is_contiguous(), "tensors handed to the C ABI must be contiguous"
+
+
+def _given(name, t, dtype, shape):
+    """Device pointer of a tensor that may be None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _needed(name, t, dtype, shape)
+    return t.data_ptr()
+
+
+def _angles(positions, table, turn, B, f32, i32):
+    """Checks positions [axes, B, L] and table [n_pos, pairs, 2]; returns (L, n_pos)."""
     at, angles = positions.shape, table.shape
-    if positions.dtype is not torch.int32 or table.dtype is not torch.float32 or len(at) != 3 or at != (turn.axes, B, at[2]) or \
-            len(angles) != 3 or angles != (angles[0], turn.pairs, 2):
-        _typed(torch.int32, positions=positions)
-        _typed(torch.float32, table=table)
-        _shaped("positions", positions, (turn.axes, B, at[-1]))
-        _shaped("table", table, (angles[0], turn.pairs, 2))
-    if index is not None:
-        _typed(torch.int32, index=index)
-        _shaped("index", index, (B, N))
+    if positions.dtype is not i32 or len(at) != 3 or at != (turn.axes, B, at[2]) or not positions.is_contiguous():
+        _needed("positions", positions, i32, (turn.axes, B, at[-1]))
+    if table.dtype is not f32 or len(angles) != 3 or angles != (angles[0], turn.pairs, 2) or not table.is_contiguous():
+        _needed("table", table, f32, (angles[0], turn.pairs, 2))
     return at[2], angles[0]
 
 
 def _side(t, out, shape, names):
     """Pointers and layouts of rows of this shape and of what they become (None: themselves)."""
+    if out is not None and (out.dtype is not t.dtype or out.shape != shape):
+        _typed(t.dtype, **{names[1]: out})
+        _shaped(names[1], out, shape)
+    if out is not None and t.is_contiguous() and out.is_contiguous():
+        return out, t.data_ptr(), None, out.data_ptr(), None
     p, lay = _rows(t, names[0])
     lay = lay and C.byref(lay)
     if out is None:
         return t, p, lay, p, lay
-    if out.dtype is not t.dtype or out.shape != shape:
-        _typed(t.dtype, **{names[1]: out})
-        _shaped(names[1], out, shape)
     o, out_lay = _rows(out, names[1])
     return out, p, lay, o, out_lay and C.byref(out_lay)
 
@@ -668,13 +684,12 @@ def mustdrop_rotate(q, positions, table, turn, k=None, q_out=None, k_out=None, i
     [:, b, index[b, i]], or [:, b, i] without index [B, N] int32), with table [n_pos, pairs, 2] f32 (rotary_table) and turn = rotary(..).  q_out and
     k_out: None for in place.  rows [B] int32: rows from there on stay.  inverse: the way back.  Returns (q_out, k_out)."""
     import torch
+    i32 = torch.int32
     B, N, Hq, d = q.shape
     if k is None and k_out is not None:
         raise ValueError("k_out without k")
-    L, n_pos = _angles(positions, table, turn, index, B, N)
-    if rows is not None:
-        _typed(torch.int32, rows=rows)
-        _shaped("rows", rows, (B,))
+    L, n_pos = _angles(positions, table, turn, B, torch.float32, i32)
+    at, count = _given("index", index, i32, (B, N)), _given("rows", rows, i32, (B,))
     q_out, qp, ql, qo, qol = _side(q, q_out, (B, N, Hq, d), ("q", "q_out"))
     H, kp, kl, ko, kol = 0, None, None, None, None
     if k is not None:
@@ -686,8 +701,8 @@ def mustdrop_rotate(q, positions, table, turn, k=None, q_out=None, k_out=None, i
         k_out, kp, kl, ko, kol = _side(k, k_out, shape, ("k", "k_out"))
     raw = _here(stream, q, k, positions, table, q_out, k_out, index, rows)
     _call("mustdrop_rotate",
-        qp, kp, _dtype_code(q), _ptr(positions), _ptr(index), _ptr(table), _ptr(rows),
-        B, N, L, Hq, H, d, n_pos, C.byref(turn), int(bool(inverse)), qo, ko, ql, kl, qol, kol, raw)
+        qp, kp, BF16 if q.dtype is torch.bfloat16 else _dtype_code(q), positions.data_ptr(), at, table.data_ptr(), count,
+        B, N, L, Hq, H, d, n_pos, C.byref(turn), 1 if inverse else 0, qo, ko, ql, kl, qol, kol, raw)
     return q_out, k_out
 
 
@@ -696,26 +711,30 @@ def mustdrop_cache4_append(q, k_new, v_new, positions, table, turn, slots, cache
     [B, N, Hq, d] (or None) turned into q_out (None: in place), which is returned.  Rows without a slot stay out, and their queries.  For
     positions, table, turn and index see mustdrop_rotate."""
     import torch
+    i32 = torch.int32
     B, N, H, d = k_new.shape
     n_pages, heads, page = _pool(cache, d)
     if q is None and q_out is not None:
         raise ValueError("q_out without q")
-    L, n_pos = _angles(positions, table, turn, index, B, N)
-    _typed(torch.int32, slots=slots)
-    _shaped("slots", slots, (B, N))
+    L, n_pos = _angles(positions, table, turn, B, torch.float32, i32)
+    if slots.dtype is not i32 or slots.shape != (B, N) or not slots.is_contiguous():
+        _needed("slots", slots, i32, (B, N))
+    at = _given("index", index, i32, (B, N))
     kp, vp, lay = _row_pair(k_new, v_new, ("k_new", "v_new"))
     if heads != H:
         raise ValueError(f"rows of {H} heads for a cache of {heads} heads")
     Hq, qp, ql, qo, qol = 0, None, None, None, None
     if q is not None:
-        Hq = q.shape[2]
-        _typed(k_new.dtype, q=q)
-        _shaped("q", q, (B, N, Hq, d))
-        q_out, qp, ql, qo, qol = _side(q, q_out, (B, N, Hq, d), ("q", "q_out"))
+        shape = q.shape
+        if q.dtype is not k_new.dtype or len(shape) != 4 or shape != (B, N, shape[2], d):
+            _typed(k_new.dtype, q=q)
+            _shaped("q", q, (B, N, shape[2], d))
+        Hq = shape[2]
+        q_out, qp, ql, qo, qol = _side(q, q_out, shape, ("q", "q_out"))
     raw = _here(stream, k_new, v_new, q, q_out, positions, table, slots, cache, index)
     _call("mustdrop_cache4_append",
-        qp, kp, vp, _dtype_code(k_new), _ptr(positions), _ptr(index), _ptr(table), _ptr(slots), _ptr(cache),
-        B, N, L, Hq, H, d, n_pos, n_pages, page, C.byref(turn), qo, ql, lay, qol, raw)
+        qp, kp, vp, BF16 if k_new.dtype is torch.bfloat16 else _dtype_code(k_new), positions.data_ptr(), at, table.data_ptr(), slots.data_ptr(),
+        _ptr(cache), B, N, L, Hq, H, d, n_pos, n_pages, page, C.byref(turn), qo, ql, lay, qol, raw)
     return q_out
 
 
@@ -725,32 +744,42 @@ def cache4_bounds_buffer(n_pages, H, d, device="cuda"):
     return torch.zeros((n_pages, H, 2, d), dtype=torch.int8, device=device), torch.zeros((n_pages, H), dtype=torch.uint8, device=device)
 
 
-def _bounds(bounds, scales):
+def _bounds(bounds, scales, i8, u8):
     """(pages, heads, channels) of a cache's bounds."""
-    import torch
-    _typed(torch.int8, bounds=bounds)
-    _typed(torch.uint8, scales=scales)
-    n_pages, H, two, d = bounds.shape
-    _shaped("bounds", bounds, (n_pages, H, 2, d))
-    _shaped("scales", scales, (n_pages, H))
+    shape = bounds.shape
+    n_pages, H, two, d = shape
+    if bounds.dtype is not i8 or two != 2 or not bounds.is_contiguous():
+        _needed("bounds", bounds, i8, (n_pages, H, 2, d))
+    if scales.dtype is not u8 or scales.shape != (n_pages, H) or not scales.is_contiguous():
+        _needed("scales", scales, u8, (n_pages, H))
     return n_pages, H, d
+
+
+def _requests(table, length, q_len, B, i32):
+    """Checks a block table [B, max_pages], lengths [B] and row counts [B] or None; returns (max_pages, pointer of q_len)."""
+    shape = table.shape
+    if table.dtype is not i32 or len(shape) != 2 or shape[0] != B or not table.is_contiguous():
+        _needed("table", table, i32, (B, shape[-1]))
+    if length.dtype is not i32 or length.shape != (B,) or not length.is_contiguous():
+        _needed("length", length, i32, (B,))
+    return shape[1], None if q_len is None else _given("q_len", q_len, i32, (B,))
 
 
 def mustdrop_cache4_bounds(cache, table, length, n, bounds, scales, first=None, stream=None):
     """Bounds of the keys of the pages that hold entries first .. first + n - 1 (below length) of every sample, into bounds int8
     [n_pages, H, 2, d] and scales uint8 [n_pages, H] (cache4_bounds_buffer)."""
     import torch
-    pages, H, d = _bounds(bounds, scales)
+    i32 = torch.int32
+    pages, H, d = _bounds(bounds, scales, torch.int8, torch.uint8)
     n_pages, heads, page = _pool(cache, d)
-    if (pages, H) != (n_pages, heads):
+    if pages != n_pages or H != heads:
         raise ValueError(f"bounds of {pages} pages and {H} heads for a cache of {n_pages} and {heads}")
-    B, max_pages = table.shape
-    _typed(torch.int32, table=table, length=length, first=first)
-    _shaped("length", length, (B,))
-    _shaped("first", first, (B,))
+    B = table.shape[0]
+    max_pages, _ = _requests(table, length, None, B, i32)
+    start = _given("first", first, i32, (B,))
     raw = _here(stream, cache, table, length, bounds, scales, first)
     _call("mustdrop_cache4_bounds",
-        _ptr(cache), _ptr(table), _ptr(length), _ptr(first), _ptr(bounds), _ptr(scales), B, int(n), H, d, n_pages, page, max_pages, raw)
+        _ptr(cache), table.data_ptr(), length.data_ptr(), start, bounds.data_ptr(), scales.data_ptr(), B, int(n), H, d, n_pages, page, max_pages, raw)
 
 
 def cache4_choose_workspace(q, bounds, table, page=16):
@@ -765,25 +794,24 @@ def mustdrop_cache4_choose(q, bounds, scales, table, length, page, chosen, q_len
     receives entries of the block table in ascending order, then -1.  q [B, N, Hq, d] (bf16 / f32, any layout); bounds and scales from
     mustdrop_cache4_bounds; the first first_pages and the last last_pages are always among them.  Returns chosen."""
     import torch
+    i32 = torch.int32
     B, N, Hq, d = q.shape
-    n_pages, H, channels = _bounds(bounds, scales)
+    n_pages, H, channels = _bounds(bounds, scales, torch.int8, torch.uint8)
     if channels != d:
         raise ValueError(f"bounds of {channels} channels for queries of {d}")
-    max_pages, budget = table.shape[-1], chosen.shape[-1]
-    _typed(torch.int32, table=table, length=length, chosen=chosen, q_len=q_len)
-    _shaped("table", table, (B, max_pages))
-    _shaped("length", length, (B,))
-    _shaped("q_len", q_len, (B,))
-    _shaped("chosen", chosen, (B, N, H, budget))
+    max_pages, rows = _requests(table, length, q_len, B, i32)
+    lists = chosen.shape
+    if chosen.dtype is not i32 or len(lists) != 4 or lists != (B, N, H, lists[3]) or not chosen.is_contiguous():
+        _needed("chosen", chosen, i32, (B, N, H, lists[-1]))
     raw = _here(stream, q, bounds, scales, table, length, chosen, q_len, workspace)
     if workspace is None:
         with _made_on(stream):
             workspace = cache4_choose_workspace(q, bounds, table, int(page))
     qp, lq = _rows(q, "q")
     _call("mustdrop_cache4_choose",
-        qp, _dtype_code(q), _ptr(bounds), _ptr(scales), _ptr(table), _ptr(length), _ptr(q_len),
-        B, N, Hq, H, d, n_pages, int(page), max_pages, int(first_pages), int(last_pages), budget,
-        _ptr(chosen), lq and C.byref(lq), _ptr(workspace), workspace.numel(), raw)
+        qp, BF16 if q.dtype is torch.bfloat16 else _dtype_code(q), bounds.data_ptr(), scales.data_ptr(), table.data_ptr(), length.data_ptr(), rows,
+        B, N, Hq, H, d, n_pages, int(page), max_pages, int(first_pages), int(last_pages), lists[3],
+        chosen.data_ptr(), lq and C.byref(lq), _ptr(workspace), workspace.numel(), raw)
     return chosen
 
 
@@ -799,25 +827,21 @@ def mustdrop_cache4_attend_chosen(q, cache, table, length, chosen, softmax_scale
     """mustdrop_cache4_attend over the pages that chosen [B, N, H, budget] int32 names for each token and K/V head (ascending; what does
     not ascend or is no entry of the table does not count).  Returns out (made as zeros if None)."""
     import torch
-    B, N, Hq, d = q.shape
+    i32 = torch.int32
+    shape = q.shape
+    B, N, Hq, d = shape
     n_pages, H, page = _pool(cache, d)
-    max_pages, budget = table.shape[-1], chosen.shape[-1]
     if out is None:
         with _made_on(stream):
             out = torch.zeros((B, N, Hq, d), dtype=q.dtype, device=q.device)
-    _typed(torch.int32, table=table, length=length, q_len=q_len, chosen=chosen)
-    if lse is not None:
-        _typed(torch.float32, lse=lse)
-        _shaped("lse", lse, (B, Hq, N))
-    if keep is not None:
-        _typed(torch.uint8, keep=keep)
-        _shaped("keep", keep, (B, max_pages * page))
-    _typed(q.dtype, out=out)
-    _shaped("out", out, q.shape)
-    _shaped("table", table, (B, max_pages))
-    _shaped("length", length, (B,))
-    _shaped("q_len", q_len, (B,))
-    _shaped("chosen", chosen, (B, N, H, budget))
+    elif out.dtype is not q.dtype or out.shape != shape:
+        _typed(q.dtype, out=out)
+        _shaped("out", out, shape)
+    max_pages, rows = _requests(table, length, q_len, B, i32)
+    lists = chosen.shape
+    if chosen.dtype is not i32 or len(lists) != 4 or lists != (B, N, H, lists[3]) or not chosen.is_contiguous():
+        _needed("chosen", chosen, i32, (B, N, H, lists[-1]))
+    sums, mask = _given("lse", lse, torch.float32, (B, Hq, N)), _given("keep", keep, torch.uint8, (B, max_pages * page))
     raw = _here(stream, q, cache, table, length, chosen, out, lse, q_len, keep, workspace)
     if workspace is None:
         with _made_on(stream):
@@ -825,9 +849,9 @@ def mustdrop_cache4_attend_chosen(q, cache, table, length, chosen, softmax_scale
     qp, lq = _rows(q, "q")
     op, lo = _rows(out, "out")
     _call("mustdrop_cache4_attend_chosen",
-        qp, _dtype_code(q), _ptr(cache), _ptr(table), _ptr(length), _ptr(q_len), _ptr(keep), _ptr(chosen),
-        B, N, Hq, H, d, n_pages, page, max_pages, budget, softmax_scale,
-        op, _ptr(lse), lq and C.byref(lq), lo and C.byref(lo),
+        qp, BF16 if q.dtype is torch.bfloat16 else _dtype_code(q), _ptr(cache), table.data_ptr(), length.data_ptr(), rows, mask, chosen.data_ptr(),
+        B, N, Hq, H, d, n_pages, page, max_pages, lists[3], softmax_scale,
+        op, sums, lq and C.byref(lq), lo and C.byref(lo),
         _ptr(workspace), workspace.numel(), raw)
     return out
 
