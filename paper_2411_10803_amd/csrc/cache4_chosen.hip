@@ -53,7 +53,10 @@ __global__ __launch_bounds__(256) void cache4_bounds_kernel(
     const int unit = (int)blockIdx.x * 4 + wave_id(), lane = lane_id();
     if (unit >= units) return;
     const int bx = heads.div(unit), h = unit - bx * heads.d, b = span.div(bx), x = bx - b * span.d;
-    const int length = c4_clamp(len[b], 0, p.max_pages << p.page_shift), from = first ? max(first[b], 0) : 0;
+    int length = uniform(len)[b], from = uniform(first ? first : len)[b];
+    asm volatile("" : "+s"(length), "+s"(from));     // (on their way together)
+    length = c4_clamp(length, 0, p.max_pages << p.page_shift);
+    from = first ? max(from, 0) : 0;
     const long e = (long)(from >> p.page_shift) + x;
     if ((e << p.page_shift) >= min((long)from + N, (long)length)) return;
     const int id = c4_page_id(table[(long)b * p.max_pages + e], p.n_pages);
