@@ -344,6 +344,14 @@ struct Rows {
         }
     }
 
+    // Whether a scale of V is beyond 252 in any lane: its numbers may not be finite.
+    __device__ __forceinline__ static bool far(const uint32_t (&vs)[2]) {
+        uint32_t r = 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) r |= ((vs[u] & 0x7F7F7F7Fu) + 0x03030303u) & vs[u] & 0x80808080u;
+        return __any(r != 0);
+    }
+
     // Keys of the step that the call leaves out for all rows get a V scale of 1 (0 * NaN would count); `hides` gets a bit for each
     // of the lane's eight keys that its row does not see: of key x of tile u bit 8 x + 7 - 4 u.  Four keys at a time, a byte each.
     template <class W>
@@ -355,7 +363,7 @@ struct Rows {
         const bool ok[2] = {there(w, step, known, 0), there(w, step, known, 1)};
         const Sight sight = sight_at(w, step);
         const bool inside = step * 32 + 32 <= w.level && ok[0] && ok[1];         // (a prompt's piece has few steps that are not)
-        uint32_t nan = 0;
+        uint32_t on[2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) hides[t] = 0;
 #pragma unroll
@@ -363,22 +371,27 @@ struct Rows {
             const int t = step * 32 + 16 * u + 4 * lb;
             const uint32_t w0 = kp.w[u][0], w1 = kp.w[u][1], w2 = kp.w[u][2], w3 = kp.w[u][3];
             const uint32_t even = lb & 2 ? w2 : w0, odd = lb & 2 ? w3 : w1, kept = lb & 1 ? odd : even;
-            uint32_t on = nonzero(kept);
-            const uint32_t nans = kTops & ~nonzero(~vs[u]);
+            on[u] = nonzero(kept);
             if (inside) {
 #pragma unroll
-                for (int z = 0; z < NT; ++z) hides[z] |= (on & (limit[z] > 0 ? sight.u[u] : 0u)) >> (4 * u);
+                for (int z = 0; z < NT; ++z) hides[z] |= (on[u] & (limit[z] > 0 ? sight.u[u] : 0u)) >> (4 * u);
             } else {
-                on &= first((ok[u] ? w.end : 0) - t);
+                on[u] &= first((ok[u] ? w.end : 0) - t);
 #pragma unroll
-                for (int z = 0; z < NT; ++z) hides[z] |= (on & first(limit[z] - t) & sight.u[u]) >> (4 * u);
+                for (int z = 0; z < NT; ++z) hides[z] |= (on[u] & first(limit[z] - t) & sight.u[u]) >> (4 * u);
             }
-            nan |= on & nans;
-            const uint32_t out = (kTops & ~on) | nans, bytes = (out << 1) - (out >> 7);
-            vs[u] = (vs[u] & ~bytes) | (bytes & 0x7F7F7F7Fu);
         }
 #pragma unroll
         for (int z = 0; z < NT; ++z) hides[z] = ~hides[z];
+        if (!far(vs)) return;                        // (what is finite counts as 0 where its probability is)
+        uint32_t nan = 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t nans = kTops & ~nonzero(~vs[u]);
+            nan |= on[u] & nans;
+            const uint32_t out = (kTops & ~on[u]) | nans, bytes = (out << 1) - (out >> 7);
+            vs[u] = (vs[u] & ~bytes) | (bytes & 0x7F7F7F7Fu);
+        }
         // A NaN in V of a key that some rows see and others do not: the rows that see it get it in that group's channels here.
         if (__any(nan != 0)) {
             const Pages pg = pages_by_number(w, step, known);
@@ -397,6 +410,14 @@ struct Rows {
         }
     }
 
+    // Scores of pages that the lane's row does not see.
+    __device__ __forceinline__ static void hide_pages(f32x4 (&st)[NT][2], const Sight& sight) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+                if (!sight.u[x >> 2]) st[t][x >> 2][x & 3] = -INFINITY;
+    }
     // Scores of keys that the lane's row does not see.
     __device__ __forceinline__ static void hide(f32x4 (&st)[NT][2], uint32_t (&hides)[NT]) {
 #pragma unroll
@@ -532,7 +553,7 @@ struct Sweep : Rows<D, F32, NT> {
         return r;
     }
 
-    __device__ __forceinline__ void step(const Walk& w, const Keys& K, bool masked, uint32_t (&hides)[NT]) {
+    __device__ __forceinline__ void step(const Walk& w, const Keys& K, bool masked, uint32_t (&hides)[NT], bool pages, const Sight& sight) {
         f32x4 st[NT][2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -550,6 +571,7 @@ struct Sweep : Rows<D, F32, NT> {
             }
         }
         if (masked) R::hide(st, hides);
+        if (pages) R::hide_pages(st, sight);
         bf16x8 p[NT][PT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) R::softmax(t, st[t], w.c, p[t]);
@@ -614,16 +636,23 @@ struct Sweep : Rows<D, F32, NT> {
             __builtin_amdgcn_sched_barrier(0);                   // (what is asked for before the wait for LDS is waited for with it)
             next = pages_at(w, ahead + stride);
             later = kept_at(w, i + stride);
-            const bool masked = ((holes >> x) & 1) != 0 || i * 32 + 32 > w.clear || uneven(w, i);
+            bool masked = ((holes >> x) & 1) != 0 || i * 32 + 32 > w.clear, pages = false;
             holes &= ~(1u << x);
             if (ahead < stop) {
                 if (hole(w, ahead, pg)) holes |= 1u << x;
                 ask(w, ahead, pg, ring + x * SLOT);
             }
             x = x + 1 == RING ? 0 : x + 1;
+            // (where nothing but whole pages is hidden, from some rows: without a mask, as long as V is finite)
+            Sight sight{{0, 0}};
+            if (!masked && uneven(w, i)) {
+                pages = !R::far(k.vs);
+                masked = !pages;
+                if (pages) sight = sight_at(w, i);
+            }
             uint32_t hides[NT];
             if (masked) R::mask(w, i, kp, k.vs, hides);
-            step(w, k, masked, hides);
+            step(w, k, masked, hides, pages, sight);
         }
     }
 };

@@ -506,11 +506,12 @@ def test_attend_chosen_nan_reaches_only_the_rows_that_see_it(dtype, d):
     c.check(out, lse)
 
 
+@pytest.mark.parametrize("masked", (True, False))
 @pytest.mark.parametrize("dtype, d", ((BF16, 64), (F32, 128)))
-def test_nan_reaches_only_the_tokens_that_have_chosen_its_page(dtype, d):
+def test_nan_reaches_only_the_tokens_that_have_chosen_its_page(dtype, d, masked):
     """Tokens that go together: a V or K that is no number counts for the tokens whose lists name its page and which see it."""
     import paper_2411_10803_amd as md
-    c = Chosen(45, [400, 400], 97, 8, 8, d, 16, 6, dtype, keep=0.9)              # two tokens in sixteen rows at least: 8 heads of one query each
+    c = Chosen(45, [400, 400], 97, 8, 8, d, 16, 6, dtype, keep=0.9 if masked else None)      # sixteen tokens together
     bad = np.full(d, 1.0)
     bad[40] = np.nan
     one = np.full(d, 1.0)
@@ -518,10 +519,46 @@ def test_nan_reaches_only_the_tokens_that_have_chosen_its_page(dtype, d):
         slot = c.table[b, t // 16] * 16 + t % 16
         ref.put(c.pool, slot, h, k, v, 16)
         c.k[slot, h], c.v[slot, h] = ref.values(*ref.quantise(k)), ref.values(*ref.quantise(v))
-        c.keep[b, t] = 1
-    c.keep[1, 64] = 0
+        if masked:
+            c.keep[b, t] = 1
+    if masked:
+        c.keep[1, 64] = 0
     out, lse = c.call(md)
     assert np.isnan(out).any() and not np.isnan(out).all()
+    c.check(out, lse)
+
+
+@pytest.mark.parametrize("N, H, dtype, d", ((1, 3, BF16, 128), (1, 3, F32, 64), (110, 8, BF16, 128), (110, 8, F32, 64)))
+def test_places_that_nobody_sees_may_hold_anything(N, H, dtype, d):
+    """Entries that are masked and those behind the length hold any bytes, scales beyond every finite number among them; so do pages that are
+    not chosen."""
+    import paper_2411_10803_amd as md
+    page, lengths = 16, [150, 131]
+    c = Chosen(49, lengths, N, 2 * H, H, d, page, 5, dtype, keep=0.6)
+    rng = np.random.default_rng(50)
+    for b, n in enumerate(lengths):
+        used = np.zeros(c.entries, bool)
+        for i, h in np.ndindex(N, H):
+            used[cr.listed(c.lists[b, i, h], c.entries)] = True
+        for t in range(-(-n // page) * page):
+            if t < n and c.keep[b, t] and used[t // page]:
+                continue
+            at, p = c.table[b, t // page], t % page
+            for h in range(H):
+                x = c.pool[at, h]
+                any_bytes = lambda m: rng.choice(np.array([0, 1, 127, 128, 252, 253, 254, 255], np.uint8), m)  # noqa: E731
+                x[p * d // 2:(p + 1) * d // 2] = rng.integers(0, 256, d // 2)
+                o = page * d // 2
+                x[o + p * d // 32:o + (p + 1) * d // 32] = any_bytes(d // 32)
+                o += page * d // 32
+                for part in range(16):
+                    a = o + ((p // 4) * 16 + part) * (d // 8) + (p % 4) * (d // 32)
+                    x[a:a + d // 32] = rng.integers(0, 256, d // 32)
+                o += page * d // 2
+                for g in range(d // 32):
+                    x[o + (p // 4) * (d // 8) + g * 4 + p % 4] = any_bytes(1)[0]
+    out, lse = c.call(md)
+    assert not np.isnan(out).any()
     c.check(out, lse)
 
 
