@@ -129,10 +129,11 @@ inline bool c4_choose_together(int64_t blocks, int pitch, size_t lds) {
 // How the attention over chosen pages is cut.
 //   tokens   that a block takes together, as many as fill 16 query rows with their heads: over all of the pages that any of them has chosen.
 //            What a key costs is then shared, but where tokens choose different pages there are more of them to go through and fewer blocks.
-//            It pays from three tokens on where there are blocks for the chip without it.  us apart / together where tokens choose at
-//            random, and where they choose the same, 1024 keys of about 6000: 1 x 64 tokens of 40 heads 57 / 31, 56 / 14; 4 x 128 of 32 heads
-//            on 8 86 / 86, 82 / 27; 64 x 4 of 32 heads 187 / 153, 160 / 54; 4 x 16 of 32 heads, 512 keys 31 / 31, 31 / 12; but 1 x 16 of 32
-//            on 8 12 / 31, 12 / 13; 16 x 5 of 32 on 8 23 / 33, 21 / 14; two tokens, 64 x 2 of 32 on 8 31 / 36, 26 / 20
+//            It pays where there are blocks for the chip without it.  us apart / together where tokens choose at random, and where they
+//            choose the same, 1024 keys of about 6000: 1 x 64 tokens of 40 heads 55 / 27, 53 / 13; 4 x 128 of 32 heads on 8 83 / 70, 80 / 27; of
+//            64 on 8, two together, 82 / 79, 81 / 49; 64 x 4 of 32 heads 180 / 130, 153 / 54; 4 x 16 of 32 heads, 512 keys 30 / 26, 29 / 12;
+//            2 x 200 of 28 on 4 40 / 43, 38 / 26; but 1 x 16 of 32 on 8 12 / 25, 12 / 13; 16 x 5 of 32 on 8 22 / 28, 21 / 14; 64 x 2 of 32 on 8
+//            31 / 32, 26 / 19
 //   splits   parts of a token's list, a block each, joined by a second launch: where there are few lists and they are long.  us in one
 //            part / in 4 / 8 / 16, of 32-key steps: 8 lists of 32 13.0 / 12.2 / 12.4 / 13.7, of 64 16.5 / 14.8 / 13.8 / 14.1, of 128 25 / 17 / 15 /
 //            16.5, of 256 45 / 23 / 19 / 18; 32 of 128 25 / 19 / 17 / 18; 128 of 128 27 / 23 / 24 / 31
@@ -146,7 +147,7 @@ inline C4Chosen c4_chosen(bool f32, int d, int B, int N, int G, int H, int budge
     C4Chosen c;
     const int64_t apart = (int64_t)B * N * H * ((G + 15) / 16), steps = ((int64_t)budget * page + 31) / 32;
     const int most_waves = f32 && d == 128 ? 4 : 8;
-    c.tokens = G <= 5 && N > 2 && apart >= 1536 && max_pages > 0 && max_pages <= kC4TableMost ? (N < 16 / G ? N : 16 / G) : 1;
+    c.tokens = G <= 8 && N > 1 && apart >= 1536 && max_pages > 0 && max_pages <= kC4TableMost ? (N < 16 / G ? N : 16 / G) : 1;
     const int64_t together = (int64_t)c.tokens * budget, most = together < max_pages ? together : max_pages;
     if (c.tokens > 1 && most <= kC4ListMost) {
         c.splits = 1;

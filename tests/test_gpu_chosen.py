@@ -461,7 +461,9 @@ ATTENDS = [
     dict(lengths=[3000, 700], N=2, Hq=2, H=1, d=64, page=16, budget=190, dtype=F32, keep=0.8, q_len=[2, 1]),
     dict(lengths=[700], N=1, Hq=18, H=1, d=128, page=16, budget=1500, dtype=F32, kind="any"),
     dict(lengths=[600, 90], N=1, Hq=2, H=2, d=64, page=16, budget=2100, dtype=BF16, kind="all"),
-    # several tokens together (1536 tokens and K/V heads and more, five heads to one at most): 4, 16, 3, 5 and 8 tokens
+    # several tokens together (1536 tokens and K/V heads and more, eight heads to one at most): 2, 2, 4, 16, 3, 5 and 8 tokens
+    dict(lengths=[390, 300], N=391, Hq=16, H=2, d=64, page=16, budget=6, dtype=BF16, keep=0.8),
+    dict(lengths=[400, 250], N=400, Hq=14, H=2, d=128, page=32, budget=3, dtype=F32, q_len=[399, 250]),
     dict(lengths=[230, 150], N=200, Hq=16, H=4, d=128, page=16, budget=4, dtype=BF16, q_len=[200, 133]),
     dict(lengths=[120, 70], N=65, Hq=13, H=13, d=64, page=32, budget=2, dtype=BF16, keep=0.5),
     dict(lengths=[300, 200], N=261, Hq=15, H=3, d=64, page=64, budget=3, dtype=F32, kind="any", layout="heads"),
