@@ -977,7 +977,7 @@ int choose_plan(const char* who, int B, int N, int Hq, int H, int d, int n_pages
     if ((long)N * A->G > (1l << 20)) return fail(MD_ESHAPE, "%s: %d tokens of %d query heads are too many for one call", who, N, Hq);
     if ((long)B * H > kMaxUnits || (long)B * H * N > kMaxUnits) return fail(MD_ESHAPE, "%s: %d samples of %d tokens and %d heads are too many for one call", who, B, N, H);
     A->tiles = (N + A->per - 1) / A->per;
-    A->lds = 64 + 32 * (d + 16) + (size_t)A->per * A->pitch * 4;
+    A->lds = 64 + 32 * (d + 16) + (size_t)(N < A->per ? N : A->per) * A->pitch * 4;
     A->together = A->subs == 1 && c4_choose_together((int64_t)B * H * A->tiles, A->pitch, A->lds);
     *bytes = A->together ? 256 : round_up((size_t)B * H * N * A->pitch * 4, 256);        // (scores of one launch for the next)
     return MD_OK;

@@ -121,9 +121,13 @@ inline int c4_span(int N, int page, int max_pages) {
     return most < max_pages ? (int)most : max_pages;
 }
 
-// Whether a call of the choice scores and chooses in one launch: up to 2048 pages, whose scores a block has in LDS.
+// Whether a call of the choice scores and chooses in one launch: up to 2048 pages, whose scores a block has in LDS.  A block then reads all of
+// its pages' bounds by itself, which takes long where there are few blocks.  us in two launches / in one, by blocks and pages: 8 of 119
+// 8.3 / 5.5, of 244 8.2 / 7.7, of 494 8.3 / 11.4, of 994 8.3 / 18; 32 of 244 8.8 / 7.6; 128 of 244 8.6 / 7.6, of 494 10 / 11.7, of 1994 18 / 31;
+// 256 of 994 18 / 20; 512 of 375 36 / 23, of 994 29 / 30, of 1994 66 / 65; 640 of 1875 56 / 63; 1024 of 1994 128 / 115; 1280 of 94 23 / 10, of
+// 375 36 / 22, of 688 99 / 78, of 994 62 / 56; 2048 of 128 22 / 15
 inline bool c4_choose_together(int64_t blocks, int pitch, size_t lds) {
-    return pitch <= 2048 && lds <= 32768 && (blocks >= 256 || pitch <= 256);
+    return pitch <= 2048 && lds <= 61440 && (pitch <= 256 || blocks * 2 >= pitch);
 }
 
 // How the attention over chosen pages is cut.

@@ -37,6 +37,8 @@ int main() {
             eight += c.waves == 8;
         }
     CHECK(together > 0 && split > 0 && eight > 0, "a form that no call takes");
+    CHECK(c4_choose_together(1, 256, 1000) && !c4_choose_together(1, 272, 1000) && c4_choose_together(136, 272, 1000), "few blocks");
+    CHECK(!c4_choose_together(1 << 20, 2064, 1000) && !c4_choose_together(1 << 20, 256, 61441), "more than a block holds");
     for (int page : {16, 32, 256})
         for (int N = 1; N < 700; ++N) {
             int most = 0;

@@ -295,6 +295,7 @@ CHOICES = [
     ([600 * (b % 10) + 17 * b for b in range(18)], 1, 30, 15, 64, 16, 0, 1, 40, F32, ""),
     ([1500 * (b % 12) for b in range(26)], 1, 30, 10, 128, 16, 1, 0, 130, BF16, "few heads"),
     ([3000 + 90 * b for b in range(11)], 23, 12, 2, 64, 64, 1, 1, 8, BF16, "q_len"),
+    ([1500 * (b % 12) for b in range(53)], 1, 20, 10, 128, 16, 1, 2, 77, F32, "few"),
 ]
 
 
