@@ -490,19 +490,20 @@ __global__ __launch_bounds__(256, 4) void cache4_score_choose_kernel(Choose A, F
         choose_by_wave<K>(A, s_score + (i - i0) * A.pitch, sc.seen_by(i), A.chosen + (((long)b * A.N + i) * A.H + h) * A.budget, s_hist[wave_id()]);
 }
 
-// The same by the four waves of a block, of up to 2048 scores in the workspace: wave w's lane l has those of pages (4 j + w) * 64 + l.
-__global__ __launch_bounds__(256) void cache4_choose_block_kernel(Choose A, FastDiv tokens, FastDiv heads)
+// The same by the waves of a block, of up to WAVES * 512 scores in the workspace: wave w's lane l has those of pages (WAVES j + w) * 64 + l.
+template <int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void cache4_choose_block_kernel(Choose A, FastDiv tokens, FastDiv heads)
 {
-    constexpr int K = 8;
+    constexpr int K = 8, PER = WAVES * K / kWave < 1 ? 1 : WAVES * K / kWave;       // counts of 64 pages to a lane
     __shared__ __align__(16) int s_hist[4 * 256];
-    __shared__ uint32_t s_least[4], s_most[4];
-    __shared__ int s_count[4 * K];
+    __shared__ uint32_t s_least[WAVES], s_most[WAVES];
+    __shared__ int s_count[WAVES * K];
     const int bh = tokens.div(blockIdx.x), i = blockIdx.x - bh * tokens.d, b = heads.div(bh), h = bh - b * heads.d;
     const int lane = lane_id(), wv = wave_id();
     const float* score = A.scores + (long)blockIdx.x * A.pitch;
     float f[K];
 #pragma unroll
-    for (int j = 0; j < K; ++j) f[j] = score[min((4 * j + wv) * kWave + lane, A.pitch - 1)];     // (on their way with the length)
+    for (int j = 0; j < K; ++j) f[j] = score[min((WAVES * j + wv) * kWave + lane, A.pitch - 1)];     // (on their way with the length)
     int length = uniform(A.len)[b], nq = uniform(A.q_len ? A.q_len : A.len)[b];
     asm volatile("" : "+s"(length), "+s"(nq));
 #pragma unroll
@@ -513,13 +514,13 @@ __global__ __launch_bounds__(256) void cache4_choose_block_kernel(Choose A, Fast
     const int P = c4_pages_of(min(max(length - nq + i + 1, 0), length), A.page_shift), hi = P - A.last, taken = A.budget;
     int32_t* to = A.chosen + (((long)b * A.N + i) * A.H + h) * A.budget;
     if (P <= taken) {
-        for (int x = threadIdx.x; x < taken; x += 256) to[x] = x < P ? x : -1;
+        for (int x = threadIdx.x; x < taken; x += WAVES * 64) to[x] = x < P ? x : -1;
         return;
     }
     uint32_t key[K], least = 0xFFFFFFFFu, most = 0, ranked = 0;
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-        const int e = (4 * j + wv) * kWave + lane;
+        const int e = (WAVES * j + wv) * kWave + lane;
         const bool in = e >= A.first && e < hi;
         key[j] = in ? ordered(f[j]) : e < P ? 0xFFFFFFFFu : 0u;
         least = min(least, in ? key[j] : 0xFFFFFFFFu);
@@ -529,36 +530,41 @@ __global__ __launch_bounds__(256) void cache4_choose_block_kernel(Choose A, Fast
     least = wave_min_u32(least);
     most = ~wave_min_u32(~most);
     if (lane == 0) { s_least[wv] = least; s_most[wv] = most; }
-    reinterpret_cast<i32x4*>(s_hist)[threadIdx.x] = i32x4{0, 0, 0, 0};
+    if (threadIdx.x < 256) reinterpret_cast<i32x4*>(s_hist)[threadIdx.x] = i32x4{0, 0, 0, 0};
     block_sync_lds();
-    least = min(min(s_least[0], s_least[1]), min(s_least[2], s_least[3]));
-    most = max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]));
+    least = wave_min_u32(s_least[lane & (WAVES - 1)]);
+    most = ~wave_min_u32(~s_most[lane & (WAVES - 1)]);
     const Border r = border_of<K, true>(key, ranked, taken - A.first - A.last, least, most, s_hist);
     // larger ones and equal ones of 64 at a time, and before them
     int mine[K];
 #pragma unroll
     for (int j = 0; j < K; ++j) {
         mine[j] = (int)__popcll(__ballot(key[j] > r.bound)) | (r.ties ? (int)__popcll(__ballot(key[j] == r.bound)) << 16 : 0);
-        if (lane == 0) s_count[4 * j + wv] = mine[j];
+        if (lane == 0) s_count[WAVES * j + wv] = mine[j];
     }
     block_sync_lds();
-    const int count = lane < 4 * K ? s_count[lane] : 0, upto = wave_incl_scan_i(count);
+    int count[PER], sum = 0;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+        count[x] = lane * PER + x < WAVES * K ? s_count[lane * PER + x] : 0;
+        sum += count[x];
+    }
+    const int upto = wave_incl_scan_i(sum), behind = PER == 2 ? count[PER - 1] : 0;
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-        const int before = __builtin_amdgcn_readlane(upto, 4 * j + wv) - mine[j];
+        const int at = WAVES * j + wv;               // (of the two of a lane, the first one has the second behind it)
+        const int before = __builtin_amdgcn_readlane(upto, at / PER) - (PER == 2 && !(at & 1) ? __builtin_amdgcn_readlane(behind, at / PER) : 0) - mine[j];
         const bool larger = key[j] > r.bound, same = r.ties && key[j] == r.bound;
         const int equal = (before >> 16) + lanes_below(__ballot(same));
-        if (larger || (same && equal < r.ties)) to[(before & 0xFFFF) + lanes_below(__ballot(larger)) + min(equal, r.ties)] = (4 * j + wv) * kWave + lane;
+        if (larger || (same && equal < r.ties)) to[(before & 0xFFFF) + lanes_below(__ballot(larger)) + min(equal, r.ties)] = (WAVES * j + wv) * kWave + lane;
     }
 }
 
 // Larger scores first, of equal ones the first page; never 0.
 __device__ __forceinline__ uint64_t page_key(float score, int e) { return ((uint64_t)ordered(score) << 32) | (uint32_t)(0x7FFFFFFF - e); }
 
-// The choice from scores in the workspace, a block per token and K/V head.  IPT: keys that a thread holds, 0: any number, looked up again
-// and again.
-template <int IPT, int THREADS>
-__global__ __launch_bounds__(THREADS) void cache4_choose_kernel(Choose A, FastDiv tokens, FastDiv heads)
+// The choice from any number of scores in the workspace, a block per token and K/V head, which looks them up again and again.
+__global__ __launch_bounds__(1024) void cache4_choose_kernel(Choose A, FastDiv tokens, FastDiv heads)
 {
     __shared__ int s_hist[kSelectHistInts], s_red[16];
     const int bh = tokens.div(blockIdx.x), i = blockIdx.x - bh * tokens.d, b = heads.div(bh), h = bh - b * heads.d, tid = threadIdx.x;
@@ -567,43 +573,23 @@ __global__ __launch_bounds__(THREADS) void cache4_choose_kernel(Choose A, FastDi
     const float* score = A.scores + (long)blockIdx.x * A.pitch;
     int32_t* to = A.chosen + (((long)b * A.N + i) * A.H + h) * A.budget;
     if (P <= A.budget) {
-        for (int x = tid; x < A.budget; x += THREADS) to[x] = x < P ? x : -1;
+        for (int x = tid; x < A.budget; x += 1024) to[x] = x < P ? x : -1;
         return;
     }
     const int lo = A.first, hi = P - A.last, always = lo + P - hi;       // pages lo .. hi - 1 are ranked
-    uint64_t key[IPT ? IPT : 1];
-    if constexpr (IPT > 0) {
-#pragma unroll
-        for (int t = 0; t < IPT; ++t) {
-            const int e = t * THREADS + tid;
-            key[t] = e >= lo && e < hi ? page_key(score[e], e) : 0;
-        }
-    }
-    for (int x = tid; x < kSelectHistInts; x += THREADS) s_hist[x] = 0;
+    for (int x = tid; x < kSelectHistInts; x += 1024) s_hist[x] = 0;
     __syncthreads();
-    SelectBound bound;
-    if constexpr (IPT > 0) bound = block_select_topk<IPT>(key, A.budget - always, s_hist);
-    else
-        bound = block_select_keys([&](auto f) {
-            for (int e = lo + tid; e < hi; e += THREADS) f(page_key(score[e], e));
-        }, A.budget - always, s_hist);
+    const SelectBound bound = block_select_keys([&](auto f) {
+        for (int e = lo + tid; e < hi; e += 1024) f(page_key(score[e], e));
+    }, A.budget - always, s_hist);
     int done = 0;
-    const auto place = [&](int e, uint64_t k) {
-        const bool in = e < P && (e < lo || e >= hi || (A.budget > always && (k >> bound.shift) >= bound.bound));
+    for (int e0 = 0; e0 < P; e0 += 1024) {
+        const int e = e0 + tid;
+        const bool in = e < P && (e < lo || e >= hi || (A.budget > always && (page_key(score[e], e) >> bound.shift) >= bound.bound));
         int total;
         const int at = block_rank(in, s_red, total);
         if (in && done + at < A.budget) to[done + at] = e;
         done += total;
-    };
-    if constexpr (IPT > 0) {
-#pragma unroll
-        for (int t = 0; t < IPT; ++t)
-            if (t * THREADS < P) place(t * THREADS + tid, key[t]);
-    } else {
-        for (int e0 = 0; e0 < P; e0 += THREADS) {
-            const int e = e0 + tid;
-            place(e, e >= lo && e < hi ? page_key(score[e], e) : 0);
-        }
     }
 }
 
@@ -1034,11 +1020,10 @@ int choose_impl(const void* q, int dtype, const int8_t* bounds, const uint8_t* s
     else { if (dtype == MD_F32) MD_C4_SCORE(64, true); else MD_C4_SCORE(64, false); }
 #undef MD_C4_SCORE
 #undef MD_C4_SCORE2
-#define MD_C4_PICK(I_, T_) MD_LAUNCH("cache4_choose", st, (cache4_choose_kernel<I_, T_>), B * H * N, T_, 0, A, FastDiv::make(N), FastDiv::make(H))
-    if (max_pages <= 2048) MD_LAUNCH("cache4_choose", st, (cache4_choose_block_kernel), B * H * N, 256, 0, A, FastDiv::make(N), FastDiv::make(H));
-    else if (max_pages <= 8192) MD_C4_PICK(8, 1024);
-    else MD_C4_PICK(0, 1024);
-#undef MD_C4_PICK
+    // us for 8 lists of 2500 / 7500 scores: sixteen waves with eight each to a lane 6.3 / 7.4, by keys that are looked up again 6.6 / 11.6
+    if (max_pages <= 2048) MD_LAUNCH("cache4_choose", st, (cache4_choose_block_kernel<4>), B * H * N, 256, 0, A, FastDiv::make(N), FastDiv::make(H));
+    else if (max_pages <= 8192) MD_LAUNCH("cache4_choose", st, (cache4_choose_block_kernel<16>), B * H * N, 1024, 0, A, FastDiv::make(N), FastDiv::make(H));
+    else MD_LAUNCH("cache4_choose", st, (cache4_choose_kernel), B * H * N, 1024, 0, A, FastDiv::make(N), FastDiv::make(H));
     return check_launch(who);
 }
 

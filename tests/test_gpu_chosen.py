@@ -290,6 +290,7 @@ CHOICES = [
     ([33000], 2, 2, 1, 128, 16, 0, 1, 3, F32, "few"),
     ([1 << 30, -5], 1, 1, 1, 64, 16, 0, 1, 2, BF16, ""),                         # lengths out of range
     ([140000, 131], 1, 2, 1, 64, 16, 0, 1, 37, BF16, "few"),                     # 8750 pages
+    ([112000, 40000], 2, 2, 1, 64, 16, 1, 1, 300, F32, "few"),                   # 7000
     # scores and choice in one launch: many tiles of query rows, up to 256, 768 and 2048 pages
     ([300 * (b % 14) + b for b in range(17)], 1, 16, 16, 128, 16, 1, 1, 20, BF16, "few"),
     ([600 * (b % 10) + 17 * b for b in range(18)], 1, 30, 15, 64, 16, 0, 1, 40, F32, ""),
