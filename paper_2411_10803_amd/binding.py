@@ -448,9 +448,11 @@ def _here(stream, *tensors) -> int:
     import torch
     at = tensors[0].get_device()
     for t in tensors:
-        if t is not None and (t.get_device() != at or at < 0):
+        if t is not None and t.get_device() != at:
             raise ValueError(f"tensors must be on one GPU: {t.device}, {tensors[0].device}")
-    if at != torch.cuda.current_device():
+    if at < 0:
+        raise ValueError(f"tensors must be on one GPU: {tensors[0].device}")
+    if at != torch._C._cuda_getDevice():                   # (torch.cuda.current_device() asks first whether there is a GPU at all)
         raise ValueError(f"tensors on device {at} in a call on device {torch.cuda.current_device()}: make theirs the current one")
     return torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
 
