@@ -435,8 +435,8 @@ int mustdrop_cache4_attend(
  *
  * Of a row's d channels the first 2 * pairs turn in pairs: pair i is channels (i, i + pairs), or (2i, 2i + 1) where `adjacent`; the
  * others stay.  Pair i has an axis; with p the row's position on it and (c, s) = table[p][i], (x, y) becomes (x c - y s, y c + x s), or
- * with -s in the place of s where `inverse` (the gradient; where c^2 + s^2 = 1 the way back, too).  In fp32: the products are rounded, then their sum, then
- * the result to the rows' type.  What the angles are (base, scaling, any factor) is the table's business.
+ * with -s in the place of s where `inverse` (the gradient; where c^2 + s^2 = 1 the way back, too).  In fp32: the products are rounded, then
+ * their sum, then the result to the rows' type.  What the angles are (base, scaling, any factor) is the table's business.
  *   pairs      a multiple of 4 (8 for mustdrop_cache4_append), 2 * pairs <= d
  *   axes       1 to 4;  axis[i] < axes for i < pairs
  *   table      [n_pos, pairs, 2] f32: cosine and sine of each position's angles
@@ -451,7 +451,8 @@ typedef struct md_rotary {
 /* Rows turned: q [B, N, Hq, d] into q_out, and k [B, N, H, d] into k_out in the same launch (k = k_out = NULL: only q).  An output may be
  * its input, with the same layout; no other overlap.  rows [B] i32 or NULL (= N): rows (b, i) with i >= rows[b] are not read and
  * not written.  d a multiple of 8, at most 256; layouts as md_kv_layout, NULL = dense token-major; B * N <= 2^28 - 16, and at most
- * 2^31 - 512 pieces of 16 channels (of 8, where d or 2 * pairs is no multiple of 16) in all heads of all rows.  Errors: MD_EINVAL, MD_ESHAPE, MD_EDTYPE, MD_EALIGN, MD_EALIAS, MD_EHIP. */
+ * 2^31 - 512 pieces of 16 channels (of 8, where d or 2 * pairs is no multiple of 16) in all heads of all rows.  Errors: MD_EINVAL,
+ * MD_ESHAPE, MD_EDTYPE, MD_EALIGN, MD_EALIAS, MD_EHIP. */
 int mustdrop_rotate(
     const void* q, const void* k, md_dtype dtype, const int32_t* positions, const int32_t* index, const float* table, const int32_t* rows,
     int B, int N, int L, int Hq, int H, int d, int n_pos, const md_rotary* rotary, int inverse,
@@ -476,7 +477,8 @@ int mustdrop_cache4_append(
  * Bounds of a page's keys, per head.  With a the largest magnitude among the page's keys and e = floor(log2 a) - 6 (a = 0: -126), at
  * least -126: bounds [n_pages, H, 2, d] i8, every channel's largest value over 2^e rounded up, then every channel's smallest one rounded
  * down (within -96 and 96); scales [n_pages, H] u8 the byte e + 127, or 255 where a group of the page's keys has a scale beyond 252 (the
- * write makes no other than 255: a key that is no number), whose bounds are then 0.  Values of 4 bits whose group has a scale of at least an eighth of the largest one's are held exactly.
+ * write makes no other than 255: a key that is no number), whose bounds are then 0.  Values of groups whose scale is at least an eighth of
+ * the largest one's are held exactly.
  */
 
 /* Bounds of the pages that hold the entries first[b] .. min(first[b] + N, len[b]) - 1 of every sample, each over all of the page's
@@ -498,7 +500,7 @@ int mustdrop_cache4_bounds(
  * equal ones the first, until there are min(budget, P).
  *   q [B, N, Hq, d] (dtype; q_layout);  q_len [B] i32 or NULL (= N)
  *   chosen [B, N, H, budget] i32: entries of the block table in ascending order, then -1; rows i >= q_len[b] untouched
- * first_pages, last_pages >= 0 with a sum of at most budget; N * G <= 2^20.  The same inputs give the same pages, whatever else differs.
+ * first_pages, last_pages >= 0 with a sum of at most budget; G <= 1024 (sums have 31 bits), N * G <= 2^20.  The same inputs give the same pages, whatever else differs.
  * Errors: MD_EINVAL, MD_ESHAPE (limits, more than 2^23 - 1 tokens and heads), MD_EDTYPE, MD_EALIGN, MD_EALIAS, MD_EWORKSPACE, MD_EHIP. */
 size_t mustdrop_cache4_choose_workspace_bytes(int B, int N, int Hq, int H, int d, int max_pages, int page);
 
@@ -510,8 +512,8 @@ int mustdrop_cache4_choose(
 /* mustdrop_cache4_attend over chosen pages: query row (b, i) sees, for K/V head h, those of the entries that it sees there which lie in
  * the pages that chosen[b][i][h][0 .. budget-1] names.  An entry of chosen that is not in 0 .. max_pages-1, or not above every such entry
  * before it in its list, takes no part: a page counts once.  With all pages chosen the two calls mean the same.  Everything else
- * (values that are no numbers, rows that see nothing, limits of scores) as for mustdrop_cache4_attend; two calls on the same inputs with
- * the same budget give the same bits.  Errors likewise, and MD_ESHAPE for 2^23 or more tiles of 16 query heads or parts of them. */
+ * (values that are no numbers, rows that see nothing, limits of scores) as for mustdrop_cache4_attend; a probability always carries 16 bits
+ * for MD_BF16.  Two calls on the same inputs, with lists and tables of the same width, give the same bits.  Errors likewise, and MD_ESHAPE for 2^23 or more tiles of 16 query heads or parts of them. */
 size_t mustdrop_cache4_attend_chosen_workspace_bytes(int B, int N, int Hq, int H, int d, int budget, int page);
 
 int mustdrop_cache4_attend_chosen(

@@ -960,6 +960,8 @@ int choose_plan(const char* who, int B, int N, int Hq, int H, int d, int n_pages
     while (A->lanes < A->G && A->lanes < 16) A->lanes *= 2;
     A->subs = (A->G + 15) / 16;
     A->per = 16 / A->lanes;
+    // (127 * 128 in each of 128 channels of 1024 heads are less than 2^31)
+    if (A->G > 1024) return fail(MD_ESHAPE, "%s: %d query heads of one K/V head are too many", who, A->G);
     if ((long)N * A->G > (1l << 20)) return fail(MD_ESHAPE, "%s: %d tokens of %d query heads are too many for one call", who, N, Hq);
     if ((long)B * H > kMaxUnits || (long)B * H * N > kMaxUnits) return fail(MD_ESHAPE, "%s: %d samples of %d tokens and %d heads are too many for one call", who, B, N, H);
     A->tiles = (N + A->per - 1) / A->per;

@@ -195,6 +195,7 @@ def test_choose_refusals(lib):
         assert choose(lib, **{n: P(7)}) == EALIAS
     assert choose(lib, ws=P(2)) == EALIAS and choose(lib, ws=None) == EWORKSPACE and choose(lib, ws=moved(P(8), 16)) == EALIGN
     assert choose(lib, ql=layout(3 * 1024, 1024, 4)) == EINVAL
+    assert choose(lib, Hq=1025, H=1, N=1) == ESHAPE and b"query heads" in lib.mustdrop_last_error()
     assert choose(lib, N=1 << 20) == ESHAPE and choose(lib, B=1 << 22, N=1, H=2, Hq=2) == ESHAPE
     size = lib.mustdrop_cache4_choose_workspace_bytes
     need = size(2, 3, 8, 4, 128, 6, 32)

@@ -291,6 +291,7 @@ CHOICES = [
     ([1 << 30, -5], 1, 1, 1, 64, 16, 0, 1, 2, BF16, ""),                         # lengths out of range
     ([140000, 131], 1, 2, 1, 64, 16, 0, 1, 37, BF16, "few"),                     # 8750 pages
     ([112000, 40000], 2, 2, 1, 64, 16, 1, 1, 300, F32, "few"),                   # 7000
+    ([900, 901], 1, 1024, 1, 128, 64, 0, 1, 4, BF16, ""),                        # 1024 heads to one
     # scores and choice in one launch: many tiles of query rows, up to 256, 768 and 2048 pages
     ([300 * (b % 14) + b for b in range(17)], 1, 16, 16, 128, 16, 1, 1, 20, BF16, "few"),
     ([600 * (b % 10) + 17 * b for b in range(18)], 1, 30, 15, 64, 16, 0, 1, 40, F32, ""),
@@ -353,6 +354,28 @@ def test_choice_by_queries_that_are_no_numbers_or_nothing():
     zero = [0, 1, 2, 3, 29]
     assert a[0, 0].tolist() == zero and a[1, 0].tolist() == zero and a[2, 1].tolist() == zero
     assert np.array_equal(a[0, 1], b[0, 1]) and np.array_equal(a[1, 1], b[1, 1]) and np.array_equal(a[2, 0], b[2, 0]) and np.array_equal(a[3], b[3])
+
+
+@pytest.mark.parametrize("sign", (1.0, -1.0))
+def test_the_largest_sums_fit(sign):
+    """1024 heads of 128 channels with the largest whole numbers and bounds of all ones or their ends: sums of nearly 2^31."""
+    import torch
+    import paper_2411_10803_amd as md
+    G, d, pages = 1024, 128, 6
+    bounds = np.zeros((pages, 1, 2, d), np.int8)
+    bounds[:, 0, 0], bounds[:, 0, 1] = 127, -128
+    for p in range(pages):                               # one after the other a little less
+        bounds[p, 0, 0, :8 * p], bounds[p, 0, 1, :8 * p] = 120, -120
+    order = np.array([3, 0, 5, 1, 4, 2])
+    scales = np.full((pages, 1), 127, np.uint8)
+    q = torch.full((1, 1, G, d), sign * 1.99, device="cuda")
+    chosen = torch.zeros((1, 1, 1, 3), dtype=torch.int32, device="cuda")
+    md.mustdrop_cache4_choose(q, dev(bounds), dev(scales), dev(order[None].astype(np.int32)), dev(np.array([16 * pages], np.int32)), 16, chosen, last_pages=0)
+    torch.cuda.synchronize()
+    w = cr.whole(host(q)[0, 0].astype(np.float64))
+    assert abs(int(w[0, 0])) == 127 and cr.score(w, bounds[0, 0].astype(np.int64), 127) > 2.0 ** 30.9
+    want = cr.choose(host(q)[0, 0].astype(np.float64), bounds[:, 0].astype(np.int64), scales[:, 0], order, 16 * pages, 1, 0, 16, 0, 0, 3, pages)
+    assert host(chosen)[0, 0, 0].tolist() == want == [1, 3, 5]
 
 
 # ------------------------------------------------------------------------------------------------ attention
@@ -859,3 +882,48 @@ def test_the_kept_rows_of_a_prompt_at_their_own_positions():
         n = int(length[b])
         want = rounded(cr.turned(host(k)[b, :n], pos[:, b][:, ids[b, :n]], table, np.repeat([0, 1], 16)), BF16)
         assert np.array_equal(host(y)[b, :n], want) and (host(y)[b, n:] == 0).all()
+
+
+def test_nothing_is_written_beside_outputs_and_workspaces():
+    """Every output, the cache and workspaces of the size that is asked for, between bands of memory that stay as they were."""
+    import torch
+    import paper_2411_10803_amd as md
+    bands = []
+
+    def between(shape, dtype):
+        n = int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size()
+        whole = torch.full((n + 16384,), 0xA5, dtype=torch.uint8, device="cuda")
+        bands.append((whole, n))
+        return whole[8192:8192 + n].view(dtype).view(shape)
+
+    def untouched():
+        torch.cuda.synchronize()
+        return all(bool((w[:8192] == 0xA5).all()) and bool((w[8192 + n:] == 0xA5).all()) for w, n in bands)
+    torch.manual_seed(21)
+    rng = np.random.default_rng(22)
+    for B, N, Hq, H, d, page, entries, budget in ((3, 5, 6, 2, 64, 16, 21, 4), (2, 1, 8, 8, 128, 32, 9, 9), (1, 1, 18, 1, 128, 16, 3000, 1500),
+                                                  (2, 130, 8, 8, 64, 16, 40, 3), (1, 2, 4, 4, 128, 16, 330, 200), (1, 7, 40, 1, 64, 16, 700, 5)):
+        n_pages = entries + 2
+        length = dev(np.array([entries * page - 3 * b for b in range(B)], np.int32))
+        table = dev(np.stack([rng.permutation(n_pages)[:entries] for _ in range(B)]).astype(np.int32))
+        cache = between((n_pages, H, ref.page_bytes(page, d)), torch.uint8)
+        cache.zero_()
+        q, k = (torch.randn((B, N, h, d), device="cuda").bfloat16() for h in (Hq, H))
+        at = torch.randint(0, 99, (1, B, N), dtype=torch.int32, device="cuda")
+        angles, turn = md.rotary_table(99, d // 2), md.rotary([d // 2])
+        slots = dev(np.concatenate([rng.permutation(n_pages * page)[:B * N - 1], [n_pages * page - 1]]).reshape(B, N).astype(np.int32))
+        qo, ko = between(q.shape, torch.bfloat16), between(k.shape, torch.bfloat16)
+        md.mustdrop_rotate(q, at, angles, turn, k=k, q_out=qo, k_out=ko)
+        md.mustdrop_cache4_append(q, k, k, at, angles, turn, slots, cache, q_out=qo)
+        bounds, scales = between((n_pages, H, 2, d), torch.int8), between((n_pages, H), torch.uint8)
+        md.mustdrop_cache4_bounds(cache, table, length, entries * page, bounds, scales)
+        chosen = between((B, N, H, budget), torch.int32)
+        lib = md.library()
+        ws = between((lib.mustdrop_cache4_choose_workspace_bytes(B, N, Hq, H, d, entries, page),), torch.uint8)
+        md.mustdrop_cache4_choose(qo, bounds, scales, table, length, page, chosen, workspace=ws)
+        ws = between((lib.mustdrop_cache4_attend_chosen_workspace_bytes(B, N, Hq, H, d, budget, page),), torch.uint8)
+        out, lse = between(q.shape, torch.bfloat16), between((B, Hq, N), torch.float32)
+        md.mustdrop_cache4_attend_chosen(qo, cache, table, length, chosen, 0.1, out=out, lse=lse, workspace=ws)
+        assert untouched(), (B, N, Hq, H, d)
+        assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+        bands.clear()
