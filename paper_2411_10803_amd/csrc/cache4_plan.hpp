@@ -138,9 +138,11 @@ inline bool c4_choose_together(int64_t blocks, int pitch, size_t lds) {
 //            64 on 8, two together, 82 / 79, 81 / 49; 64 x 4 of 32 heads 180 / 130, 153 / 54; 4 x 16 of 32 heads, 512 keys 30 / 26, 29 / 12;
 //            2 x 200 of 28 on 4 40 / 43, 38 / 26; but 1 x 16 of 32 on 8 12 / 25, 12 / 13; 16 x 5 of 32 on 8 22 / 28, 21 / 14; 64 x 2 of 32 on 8
 //            31 / 32, 26 / 19
-//   splits   parts of a token's list, a block each, joined by a second launch: where there are few lists and they are long.  us in one
-//            part / in 4 / 8 / 16, of 32-key steps: 8 lists of 32 13.0 / 12.2 / 12.4 / 13.7, of 64 16.5 / 14.8 / 13.8 / 14.1, of 128 25 / 17 / 15 /
-//            16.5, of 256 45 / 23 / 19 / 18; 32 of 128 25 / 19 / 17 / 18; 128 of 128 27 / 23 / 24 / 31
+//   splits   parts of a token's list, a block each, joined by a second launch: where there are few lists and they are long, up to 512 blocks
+//            of eight steps of 32 keys or more.  us in one part / in 4 / 8 / 16 / 32: 8 lists of 32 steps 11.6 / 12.0 / 11.7 / 11.4, of 64 15.9 /
+//            13.7 / 12.3 / 11.4 / 11.5, of 128 25 / 17 / 14.0 / 12.8 / 11.8, of 256 44 / 23 / 17 / 14.2 / 12.7, of 1024 159 / 65 / 38 / 25 / 20; 32 of
+//            32 11.1 / 12.5 / 11.9 / 12.8, of 64 16.1 / 14.6 / 12.8 / 13.9 / 13.5, of 128 25 / 18 / 15.1 / 15.6 / 16.3, of 512 83 / 38 / 25 / 23 / 24; 128 of
+//            64 17.4 / 18.9 / 19.3, of 128 27 / 23 / 24, of 512 86 / 57 / 56; but 256 of 128 29 / 34 / 37
 //   most     entries of a list to a part (tokens > 1: of the list of all)
 //   waves    of a block: eight while there are no more than 512 blocks.  us with four / eight: 8 lists of 32 steps 12.5 / 13.0, of 64 18.9 / 16.5,
 //            of 128 32 / 25; 512 of 32 17.8 / 17.4; 640 of 32 22.6 / 26; 5120 of 32 86 / 113
@@ -160,8 +162,8 @@ inline C4Chosen c4_chosen(bool f32, int d, int B, int N, int G, int H, int budge
         return c;
     }
     c.tokens = 1;
-    const int64_t parts = steps / 16 < 512 / apart ? steps / 16 : 512 / apart, need = (budget + kC4ListMost - 1) / kC4ListMost;
-    c.splits = (int)(parts > 2 ? (parts < budget ? parts : budget) : 1);
+    const int64_t parts = steps / 8 < 512 / apart ? steps / 8 : 512 / apart, need = (budget + kC4ListMost - 1) / kC4ListMost;
+    c.splits = (int)(parts > 4 || (parts > 2 && steps > 64) ? (parts < budget ? parts : budget) : 1);
     if (c.splits < need) c.splits = (int)need;
     c.most = (budget + c.splits - 1) / c.splits;
     c.splits = (budget + c.most - 1) / c.most;

@@ -486,6 +486,8 @@ ATTENDS = [
     dict(lengths=[3000, 700], N=2, Hq=2, H=1, d=64, page=16, budget=190, dtype=F32, keep=0.8, q_len=[2, 1]),
     dict(lengths=[700], N=1, Hq=18, H=1, d=128, page=16, budget=1500, dtype=F32, kind="any"),
     dict(lengths=[600, 90], N=1, Hq=2, H=2, d=64, page=16, budget=2100, dtype=BF16, kind="all"),
+    dict(lengths=[9000, 40], N=1, Hq=20, H=1, d=64, page=16, budget=560, dtype=BF16, keep=0.7),
+    dict(lengths=[4500], N=2, Hq=3, H=1, d=128, page=32, budget=140, dtype=F32),
     # several tokens together (1536 tokens and K/V heads and more, eight heads to one at most): 2, 2, 4, 16, 3, 5 and 8 tokens
     dict(lengths=[390, 300], N=391, Hq=16, H=2, d=64, page=16, budget=6, dtype=BF16, keep=0.8),
     dict(lengths=[400, 250], N=400, Hq=14, H=2, d=128, page=32, budget=3, dtype=F32, q_len=[399, 250]),
