@@ -43,8 +43,9 @@ __device__ __forceinline__ void halve(float (&v)[16], int lane) {
 // largest values and the largest with the sign turned, 16 numbers.  The four (eight) lanes of the same channels then halve these among
 // them until each has 4 (2) of the one kind, which is a word (half of one) of the result.  (Sixteen bytes to a lane are fewer loads, but 64
 // numbers to halve over sixteen lanes: 22 us for the bounds of 16 x up to 5888 entries of 8 heads instead of 10.6.)
-constexpr int kBoundsAhead = 8;                      // tokens of a lane that are on their way together
-template <int D>
+// AHEAD: tokens of a lane that are on their way together, eight, or as many as a small page has: what follows the loads bounds
+// these.  us with eight / so, 16 x up to 5888 entries of 8 heads: d = 64, pages of 16 27.6 / 17.6, of 32 15.1 / 11.9; d = 128, of 16 27.6 / 21.3
+template <int D, int AHEAD>
 __global__ __launch_bounds__(256) void cache4_bounds_kernel(
     const uint8_t* __restrict__ cache, const int32_t* __restrict__ table, const int32_t* __restrict__ len, const int32_t* __restrict__ first,
     int8_t* __restrict__ bounds, uint8_t* __restrict__ scales, Pool p, int units, int N, FastDiv heads, FastDiv span)
@@ -68,16 +69,16 @@ __global__ __launch_bounds__(256) void cache4_bounds_kernel(
 #pragma unroll
     for (int c = 0; c < 16; ++c) v[c] = -INFINITY;
     uint32_t top = 0;                                // the largest scale
-    for (int t = t0; t - t0 < live; t += TOKENS * kBoundsAhead) {
-        uint32_t w[kBoundsAhead], code[kBoundsAhead];
+    for (int t = t0; t - t0 < live; t += TOKENS * AHEAD) {
+        uint32_t w[AHEAD], code[AHEAD];
 #pragma unroll
-        for (int y = 0; y < kBoundsAhead; ++y) {     // (the last token in the place of those behind it)
+        for (int y = 0; y < AHEAD; ++y) {     // (the last token in the place of those behind it)
             const int at = min(t + y * TOKENS, live - 1);
             w[y] = *reinterpret_cast<const uint32_t*>(base + c4_k_codes(at, D) + part * 4);
             code[y] = base[c4_k_scales(p.page, at, D) + part / 4];
         }
 #pragma unroll
-        for (int y = 0; y < kBoundsAhead; y += 2) {
+        for (int y = 0; y < AHEAD; y += 2) {
             const float s = scale_of(code[y]), s2 = scale_of(code[y + 1]);
             top = max(top, max(code[y], code[y + 1]));
             const f32x2 a[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[y], s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[y], s, 1),
@@ -974,10 +975,13 @@ int bounds_impl(const void* cache, const int32_t* table, const int32_t* len, con
     if (rc != MD_OK) return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int units = B * span * H;
-#define MD_C4_BOUNDS(D_)                                                                                                                  \
-    MD_LAUNCH("cache4_bounds", st, (cache4_bounds_kernel<D_>), (units + 3) / 4, 256, 0, static_cast<const uint8_t*>(cache), table, len, first, \
+#define MD_C4_BOUNDS(D_, A_)                                                                                                              \
+    MD_LAUNCH("cache4_bounds", st, (cache4_bounds_kernel<D_, A_>), (units + 3) / 4, 256, 0, static_cast<const uint8_t*>(cache), table, len, first, \
         bounds, scales, p, units, N, FastDiv::make(H), FastDiv::make(span))
-    if (d == 128) MD_C4_BOUNDS(128); else MD_C4_BOUNDS(64);
+    if (d == 128) { if (page >= 32) MD_C4_BOUNDS(128, 8); else MD_C4_BOUNDS(128, 4); }
+    else if (page >= 64) MD_C4_BOUNDS(64, 8);
+    else if (page >= 32) MD_C4_BOUNDS(64, 4);
+    else MD_C4_BOUNDS(64, 2);
 #undef MD_C4_BOUNDS
     return check_launch("cache4_bounds");
 }
