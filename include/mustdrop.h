@@ -451,8 +451,8 @@ typedef struct md_rotary {
 /* Rows turned: q [B, N, Hq, d] into q_out, and k [B, N, H, d] into k_out in the same launch (k = k_out = NULL: only q).  An output may be
  * its input, with the same layout; no other overlap.  rows [B] i32 or NULL (= N): rows (b, i) with i >= rows[b] are not read and
  * not written.  d a multiple of 8, at most 256; layouts as md_kv_layout, NULL = dense token-major; B * N <= 2^28 - 16, and at most
- * 2^31 - 512 pieces of 16 channels (of 8, where d or 2 * pairs is no multiple of 16) in all heads of all rows.  Errors: MD_EINVAL,
- * MD_ESHAPE, MD_EDTYPE, MD_EALIGN, MD_EALIAS, MD_EHIP. */
+ * 2^31 - 512 pieces of 16 channels (of 8 with MD_F32, or where d or 2 * pairs is no multiple of 16) in all heads of all rows.  Errors:
+ * MD_EINVAL, MD_ESHAPE, MD_EDTYPE, MD_EALIGN, MD_EALIAS, MD_EHIP. */
 int mustdrop_rotate(
     const void* q, const void* k, md_dtype dtype, const int32_t* positions, const int32_t* index, const float* table, const int32_t* rows,
     int B, int N, int L, int Hq, int H, int d, int n_pos, const md_rotary* rotary, int inverse,

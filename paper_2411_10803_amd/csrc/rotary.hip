@@ -32,7 +32,7 @@ __device__ __forceinline__ Position position_of(const Angles& a, int row, int b,
     return p;
 }
 
-// Cosines and sines of pairs p0 .. p0 + W - 1 (p0 a multiple of W, W of 4 or 8; all below `pairs`).
+// Cosines and sines of pairs p0 .. p0 + W - 1 (p0 a multiple of W, W of 2, 4 or 8; all below `pairs`).
 template <int W>
 __device__ __forceinline__ void cosines(const Angles& a, const Position& p, int p0, float (&c)[W], float (&s)[W]) {
     uint32_t word = a.turn.axis[0];
@@ -109,63 +109,92 @@ __device__ __forceinline__ void store_channels(void* base, long at, const float 
     }
 }
 
+// Two runs of W channels of a row that a thread turns, each next to that of the next thread: the halves of pairs p0 .. p0 + W - 1; of neighbours as
+// pairs, and of what does not turn, one of the first half of these channels and one of the second.  half: of the row's channels.
+template <int W, bool ADJACENT>
+struct Runs {
+    int c0, c1;
+    bool turn0, turn1;
+    __device__ __forceinline__ Runs(const Angles& a, int p0, int half) {
+        const int pairs = a.turn.pairs;
+        turn0 = p0 < (ADJACENT ? 2 * pairs : pairs);
+        turn1 = ADJACENT ? p0 + half < 2 * pairs : turn0;
+        c0 = ADJACENT || turn0 ? p0 : p0 + pairs;
+        c1 = !ADJACENT && turn0 ? p0 + pairs : p0 + half;
+    }
+    __device__ __forceinline__ void cosines_of(const Angles& a, const Position& pos, float (&c)[W], float (&s)[W]) const {
+        if (!ADJACENT) {
+            cosines<W>(a, pos, c0, c, s);
+            return;
+        }
+        float c2[W / 2], s2[W / 2];
+        cosines<W / 2>(a, pos, c0 / 2, c2, s2);
+#pragma unroll
+        for (int j = 0; j < W / 2; ++j) { c[j] = c2[j]; s[j] = s2[j]; }
+        if (!turn1) return;
+        cosines<W / 2>(a, pos, c1 / 2, c2, s2);
+#pragma unroll
+        for (int j = 0; j < W / 2; ++j) { c[W / 2 + j] = c2[j]; s[W / 2 + j] = s2[j]; }
+    }
+    __device__ __forceinline__ void turn(const float (&c)[W], const float (&s)[W], float (&lo)[W], float (&hi)[W]) const {
+        if (ADJACENT) {
+            if (turn0)
+#pragma unroll
+                for (int j = 0; j < W / 2; ++j) turn_pair(lo[2 * j], lo[2 * j + 1], c[j], s[j]);
+            if (turn1)
+#pragma unroll
+                for (int j = 0; j < W / 2; ++j) turn_pair(hi[2 * j], hi[2 * j + 1], c[W / 2 + j], s[W / 2 + j]);
+        } else if (turn0) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) turn_pair(lo[j], hi[j], c[j], s[j]);
+        }
+    }
+};
+
 // ------------------------------------------------------------------------------------------------ rows
 
 struct Side { const void* x; void* y; KvLayout xl, yl; int heads; };
 
-// A thread turns W pairs (2 W channels, or copies as many that do not turn) of HEADS heads of a row: their cosines are read once, and
-// the heads' loads are on their way together.  Threads next to each other: channels, then heads.
-template <int W, bool F32, int HEADS>
+// A thread turns W pairs (two runs of W channels, or copies as many that do not turn) of HEADS heads of a row: their cosines are read once, and the
+// heads' loads are on their way together.  Threads next to each other: channels, then heads.
+template <int W, bool F32, bool ADJACENT, int HEADS>
 __global__ __launch_bounds__(256) void rotate_kernel(Side q, Side k, Angles ang, const int32_t* __restrict__ rows, int total, FastDiv items,
-                                                     FastDiv groups, FastDiv tokens, int adjacent)
+                                                     FastDiv groups, FastDiv tokens)
 {
     const int per = 256 / items.d, slot = items.div(threadIdx.x), item = threadIdx.x - slot * items.d;
     const int u = (int)blockIdx.x * per + slot;      // (the host checks that this fits 31 bits, behind the last one too)
     if (slot >= per || u >= total) return;
     const int row = groups.div(u), g = u - row * groups.d, b = tokens.div(row), i = row - b * tokens.d;
     if (rows && i >= rows[b]) return;
-    const int pairs = ang.turn.pairs, p0 = item * W;
-    const bool turns = p0 < pairs;
-    const int c0 = turns && !adjacent ? p0 : 2 * p0, c1 = turns && !adjacent ? p0 + pairs : c0 + W;
+    const Runs<W, ADJACENT> at(ang, item * W, items.d * W);
     float lo[HEADS][W], hi[HEADS][W];
 #pragma unroll
     for (int x = 0; x < HEADS; ++x) {
         const int head = g + x * groups.d, of = head - q.heads;
         if (head < q.heads) {
             const long from = (long)b * q.xl.batch + (long)i * q.xl.token + (long)head * q.xl.head;
-            load_channels<W, F32>(q.x, from + c0, lo[x]);
-            load_channels<W, F32>(q.x, from + c1, hi[x]);
+            load_channels<W, F32>(q.x, from + at.c0, lo[x]);
+            load_channels<W, F32>(q.x, from + at.c1, hi[x]);
         } else if (of < k.heads) {
             const long from = (long)b * k.xl.batch + (long)i * k.xl.token + (long)of * k.xl.head;
-            load_channels<W, F32>(k.x, from + c0, lo[x]);
-            load_channels<W, F32>(k.x, from + c1, hi[x]);
+            load_channels<W, F32>(k.x, from + at.c0, lo[x]);
+            load_channels<W, F32>(k.x, from + at.c1, hi[x]);
         }
     }
     float c[W], s[W];
-    if (turns) cosines<W>(ang, position_of(ang, row, b, i), p0, c, s);
+    if (at.turn0) at.cosines_of(ang, position_of(ang, row, b, i), c, s);
 #pragma unroll
     for (int x = 0; x < HEADS; ++x) {
         const int head = g + x * groups.d, of = head - q.heads;
-        if (turns) {
-            if (adjacent) {
-#pragma unroll
-                for (int j = 0; j < W / 2; ++j) {
-                    turn_pair(lo[x][2 * j], lo[x][2 * j + 1], c[j], s[j]);
-                    turn_pair(hi[x][2 * j], hi[x][2 * j + 1], c[W / 2 + j], s[W / 2 + j]);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < W; ++j) turn_pair(lo[x][j], hi[x][j], c[j], s[j]);
-            }
-        }
+        at.turn(c, s, lo[x], hi[x]);
         if (head < q.heads) {
             const long to = (long)b * q.yl.batch + (long)i * q.yl.token + (long)head * q.yl.head;
-            store_channels<W, F32, (HEADS > 1)>(q.y, to + c0, lo[x]);
-            store_channels<W, F32, (HEADS > 1)>(q.y, to + c1, hi[x]);
+            store_channels<W, F32, (HEADS > 1)>(q.y, to + at.c0, lo[x]);
+            store_channels<W, F32, (HEADS > 1)>(q.y, to + at.c1, hi[x]);
         } else if (of < k.heads) {
             const long to = (long)b * k.yl.batch + (long)i * k.yl.token + (long)of * k.yl.head;
-            store_channels<W, F32, (HEADS > 1)>(k.y, to + c0, lo[x]);
-            store_channels<W, F32, (HEADS > 1)>(k.y, to + c1, hi[x]);
+            store_channels<W, F32, (HEADS > 1)>(k.y, to + at.c0, lo[x]);
+            store_channels<W, F32, (HEADS > 1)>(k.y, to + at.c1, hi[x]);
         }
     }
 }
@@ -234,6 +263,28 @@ __global__ __launch_bounds__(256) void cache4_append_kernel(Append A, Angles ang
     if (at.page < 0) return;                         // (sixteen lanes together, which are all that exchange anything)
     const int b = tokens.div(r), i = r - b * tokens.d, pairs = ang.turn.pairs;
     const int h0 = (part_of - (queries ? 0 : A.q_blocks)) * HEADS, heads = queries ? A.Hq : A.p.H;
+    if constexpr (F32 && D == 128) {                 // (32 bytes to a lane would be half of a line to a store: 88.1 us for the second case above, 77.3 so)
+        if (queries) {
+            const Runs<4, MODE == kAdjacent> at(ang, part * 4, D / 2);
+            const long from = (long)b * A.ql.batch + (long)i * A.ql.token, to = (long)b * A.ol.batch + (long)i * A.ol.token;
+            float lo[HEADS][4], hi[HEADS][4], c[4], s[4];
+#pragma unroll
+            for (int y = 0; y < HEADS; ++y)
+                if (h0 + y < heads) {
+                    load_channels<4, F32>(A.q, from + (long)(h0 + y) * A.ql.head + at.c0, lo[y]);
+                    load_channels<4, F32>(A.q, from + (long)(h0 + y) * A.ql.head + at.c1, hi[y]);
+                }
+            if (at.turn0) at.cosines_of(ang, position_of(ang, r, b, i), c, s);
+#pragma unroll
+            for (int y = 0; y < HEADS; ++y)
+                if (h0 + y < heads) {
+                    at.turn(c, s, lo[y], hi[y]);
+                    store_channels<4, F32, (HEADS > 1)>(A.q_out, to + (long)(h0 + y) * A.ol.head + at.c0, lo[y]);
+                    store_channels<4, F32, (HEADS > 1)>(A.q_out, to + (long)(h0 + y) * A.ol.head + at.c1, hi[y]);
+                }
+            return;
+        }
+    }
     const KvLayout in = queries ? A.ql : A.kl;
     const void* base = queries ? A.q : A.k;
     const long row = (long)b * in.batch + (long)i * in.token;
@@ -332,8 +383,9 @@ int rotate_impl(const void* q, const void* k, int dtype, const int32_t* position
     if (rc != MD_OK) return rc;
     if (!aligned16(q) || !aligned16(q_out) || !aligned16(k) || !aligned16(k_out)) return fail(MD_EALIGN, "rotate: tensors must be 16-byte aligned");
     const long all = (long)B * N;
-    // wide loads where no pair's halves are split over them
-    const int W = ang.turn.pairs % 8 == 0 && d % 16 == 0 ? 8 : 4, items = d / (2 * W);
+    // loads of 16 bytes, where no pair's halves are split over them.  us for 4 x 2000 fp32 rows of 64 heads, eight
+    // channels / four: 120 / 90
+    const int W = dtype != MD_F32 && ang.turn.pairs % 8 == 0 && d % 16 == 0 ? 8 : 4, items = d / (2 * W);
     if (all > kMaxRows || all * (Hq + H) * items > 0x7FFFFFFFl - 511) return fail(MD_ESHAPE, "rotate: %ld rows of %d heads are too many for one call", all, Hq + H);
     const size_t qi = rows_bytes(a.xl, B, N, Hq, d, dtype), qo = rows_bytes(a.yl, B, N, Hq, d, dtype);
     const size_t ki = k ? rows_bytes(c.xl, B, N, H, d, dtype) : 0, ko = k ? rows_bytes(c.yl, B, N, H, d, dtype) : 0;
@@ -348,14 +400,17 @@ int rotate_impl(const void* q, const void* k, int dtype, const int32_t* position
     const bool many = all * (Hq + H) * items >= 4l * 256 * 1024;
     const int groups = many ? (Hq + H + 3) / 4 : Hq + H;
     const int total = (int)(all * groups);
-#define MD_ROTATE2(W_, F_, X_)                                                                                                            \
-    MD_LAUNCH("rotate", st, (rotate_kernel<W_, F_, X_>), (total + per - 1) / per, 256, 0, a, c, ang, rows, total, FastDiv::make(items),    \
-        FastDiv::make(groups), FastDiv::make(N), rotary->adjacent != 0)
-#define MD_ROTATE(W_, F_) do { if (many) MD_ROTATE2(W_, F_, 4); else MD_ROTATE2(W_, F_, 1); } while (0)
-    if (W == 8) { if (dtype == MD_F32) MD_ROTATE(8, true); else MD_ROTATE(8, false); }
-    else { if (dtype == MD_F32) MD_ROTATE(4, true); else MD_ROTATE(4, false); }
+#define MD_ROTATE3(W_, F_, A_, X_)                                                                                                        \
+    MD_LAUNCH("rotate", st, (rotate_kernel<W_, F_, A_, X_>), (total + per - 1) / per, 256, 0, a, c, ang, rows, total, FastDiv::make(items), \
+        FastDiv::make(groups), FastDiv::make(N))
+#define MD_ROTATE2(W_, F_, A_) do { if (many) MD_ROTATE3(W_, F_, A_, 4); else MD_ROTATE3(W_, F_, A_, 1); } while (0)
+#define MD_ROTATE(W_, F_) do { if (rotary->adjacent) MD_ROTATE2(W_, F_, true); else MD_ROTATE2(W_, F_, false); } while (0)
+    if (dtype == MD_F32) MD_ROTATE(4, true);
+    else if (W == 8) MD_ROTATE(8, false);
+    else MD_ROTATE(4, false);
 #undef MD_ROTATE
 #undef MD_ROTATE2
+#undef MD_ROTATE3
     return check_launch(who);
 }
 

@@ -38,6 +38,10 @@ ROTATIONS = [
     (2, 1500, 13, 9, 128, [64], BF16, "heads", False, False, "rows"),            # many rows: four heads to a thread, twenty-two of them
     (1, 5003, 11, 3, 64, [16, 8], F32, "tokens", True, False, "index"),
     (1, 9001, 7, 5, 72, [36], BF16, "tokens", False, True, ""),
+    (3, 40, 3, 2, 128, [40, 8], BF16, "tokens", True, False, "rows"),            # neighbours as pairs, that end in a row's second half
+    (1, 5003, 11, 3, 128, [24, 16], BF16, "tokens", True, True, "rows index"),
+    (1, 4001, 11, 3, 128, [8, 12], F32, "heads", False, False, ""),
+    (1, 9001, 7, 5, 96, [24], BF16, "tokens", False, False, "rows"),
 ]
 
 
@@ -174,7 +178,8 @@ def test_append(B, N, Hq, H, d, page, sections, dtype, layout, adjacent, index, 
     assert np.array_equal(ref.undefined_codes(host(cache), page, d), ref.undefined_codes(pool, page, d))
 
 
-@pytest.mark.parametrize("d, dtype, sections, adjacent", [(128, BF16, [64], False), (64, F32, [8, 8], False), (128, F32, [16, 16], True)])
+@pytest.mark.parametrize("d, dtype, sections, adjacent", [(128, BF16, [64], False), (64, F32, [8, 8], False), (128, F32, [16, 16], True),
+                                                        (128, F32, [64], False), (128, F32, [8, 16], False), (128, F32, [40, 8], True)])
 def test_many_appended_rows_are_what_few_are(d, dtype, sections, adjacent):
     """Enough rows for two heads to a wave, against the same rows in calls of a few."""
     import torch
