@@ -130,7 +130,7 @@ def test_rotation_refusals(lib, call, name):
         assert call(lib, **{n: P(7)}) == EALIAS                                  # an input over an output
     assert call(lib, qo=moved(P(1), 16)) == EALIAS                               # shifted over its own input
     assert call(lib, qo=P(1), qol=layout(3 * 2048, 2048, 256)) == EALIAS         # in place in another layout
-    assert call(lib, ql=layout(3 * 1024, 1024, 4)) == EINVAL and call(lib, qol=layout(3 * 1024, 512, 128)) == ESHAPE
+    assert call(lib, ql=layout(4 * 1024, 1024, 4)) == EINVAL and call(lib, qol=layout(3 * 1024, 512, 128)) == ESHAPE
     assert call(lib, B=1 << 14, N=1 << 15, L=1 << 15) == ESHAPE
 
 
@@ -194,7 +194,7 @@ def test_choose_refusals(lib):
     for n in ("q", "bounds", "scales", "table", "len", "q_len", "ws"):
         assert choose(lib, **{n: P(7)}) == EALIAS
     assert choose(lib, ws=P(2)) == EALIAS and choose(lib, ws=None) == EWORKSPACE and choose(lib, ws=moved(P(8), 16)) == EALIGN
-    assert choose(lib, ql=layout(3 * 1024, 1024, 4)) == EINVAL
+    assert choose(lib, ql=layout(4 * 1024, 1024, 4)) == EINVAL
     assert choose(lib, Hq=1025, H=1, N=1) == ESHAPE and b"query heads" in lib.mustdrop_last_error()
     assert choose(lib, N=1 << 20) == ESHAPE and choose(lib, B=1 << 22, N=1, H=2, Hq=2) == ESHAPE
     size = lib.mustdrop_cache4_choose_workspace_bytes
@@ -226,7 +226,7 @@ def test_attend_chosen_refusals(lib):
         assert attend(lib, **{n: P(7)}) == EALIAS
     assert attend(lib, lse=P(10)) == EALIAS and attend(lib, ws=P(10)) == EALIAS
     assert attend(lib, ws=None) == EWORKSPACE and attend(lib, wsb=C.c_size_t(1)) == EWORKSPACE
-    assert attend(lib, ql=layout(3 * 1024, 1024, 4)) == EINVAL and attend(lib, ol=layout(512, 1024, 128)) == ESHAPE
+    assert attend(lib, ql=layout(4 * 1024, 1024, 4)) == EINVAL and attend(lib, ol=layout(512, 1024, 128)) == ESHAPE
     assert attend(lib, B=1 << 21, N=1, Hq=4, H=4, ql=layout(512, 512, 128), ol=layout(512, 512, 128)) == ESHAPE
     assert attend(lib, budget=1 << 30) == ESHAPE
     size = lib.mustdrop_cache4_attend_chosen_workspace_bytes
