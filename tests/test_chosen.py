@@ -130,7 +130,7 @@ def test_rotation_refusals(lib, call, name):
         assert call(lib, **{n: P(7)}) == EALIAS                                  # an input over an output
     assert call(lib, qo=moved(P(1), 16)) == EALIAS                               # shifted over its own input
     assert call(lib, qo=P(1), qol=layout(3 * 2048, 2048, 256)) == EALIAS         # in place in another layout
-    assert call(lib, ql=layout(4 * 1024, 1024, 4)) == EINVAL and call(lib, qol=layout(3 * 1024, 512, 128)) == ESHAPE
+    assert call(lib, ql=layout(4 * 1024, 1024, 4)) == EINVAL and call(lib, qol=layout(4 * 1024, 512, 128)) == ESHAPE
     assert call(lib, B=1 << 14, N=1 << 15, L=1 << 15) == ESHAPE
 
 
