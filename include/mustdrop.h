@@ -368,7 +368,8 @@ int mustdrop_decode_keep_strided(
  * max_pages * page < 2^30; a pool of at most 256 GiB; H <= 65535; rows in MD_BF16 or MD_F32, fewer than 2^28 - 15 of them
  * (B*N) in or out in a call; base pointers 16-byte aligned.  md_kv_layout as above
  * (elements of the rows' type); NULL = dense token-major.  MD_EALIAS goes by a tensor's first and last element: an output whose rows
- * lie between those of another tensor (K and V side by side in one buffer) is refused, inputs may lie so.
+ * lie between those of another tensor (K and V side by side in one buffer) is refused, inputs may lie so, and so may the q_out of
+ * mustdrop_cache4_append between other rows (see mustdrop_rotate).
  */
 size_t mustdrop_cache4_bytes(int n_pages, int page, int H, int d);      /* 0 for sizes that no call takes */
 
@@ -449,7 +450,9 @@ typedef struct md_rotary {
 } md_rotary;
 
 /* Rows turned: q [B, N, Hq, d] into q_out, and k [B, N, H, d] into k_out in the same launch (k = k_out = NULL: only q).  An output may be
- * its input, with the same layout; no other overlap.  rows [B] i32 or NULL (= N): rows (b, i) with i >= rows[b] are not read and
+ * its input, with the same layout; no other overlap.  Rows may lie between other rows: q and k as views of one projection's output, turned in
+ * place, share no byte (MD_EALIAS goes by bytes where the strides of batch, tokens and heads are the same, else by first and last
+ * element).  rows [B] i32 or NULL (= N): rows (b, i) with i >= rows[b] are not read and
  * not written.  d a multiple of 8, at most 256; layouts as md_kv_layout, NULL = dense token-major; B * N <= 2^28 - 16, and at most
  * 2^31 - 512 pieces of 16 channels (of 8 with MD_F32, or where d or 2 * pairs is no multiple of 16) in all heads of all rows.  Errors:
  * MD_EINVAL, MD_ESHAPE, MD_EDTYPE, MD_EALIGN, MD_EALIAS, MD_EHIP. */

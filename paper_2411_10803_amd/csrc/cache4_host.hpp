@@ -29,15 +29,33 @@ int check_dtype(const char* who, int dtype) {
 constexpr long kMaxRows = (1l << 28) - 16, kMaxUnits = (1l << 23) - 1;
 
 struct Range { const void* p; size_t n; };
+// An output that shares no byte with any of some ranges.
+int check_apart(const char* who, const Range& out, const Range* r, int all) {
+    for (int c = 0; c < all; ++c)
+        if (overlaps(out.p, out.n, r[c].p, r[c].n)) return fail(MD_EALIAS, "%s: the outputs, the workspace and the inputs must not overlap", who);
+    return MD_OK;
+}
 // None of the first `outs` ranges may share a byte with any other range.
 int check_apart(const char* who, const Range* r, int outs, int all) {
-    for (int a = 0; a < outs; ++a)
-        for (int c = a + 1; c < all; ++c)
-            if (overlaps(r[a].p, r[a].n, r[c].p, r[c].n)) return fail(MD_EALIAS, "%s: the outputs, the workspace and the inputs must not overlap", who);
-    return MD_OK;
+    int rc = MD_OK;
+    for (int a = 0; a < outs && rc == MD_OK; ++a) rc = check_apart(who, r[a], r + a + 1, all - a - 1);
+    return rc;
 }
 
 size_t rows_bytes(const KvLayout& l, int B, int N, int H, int d, int dtype) { return layout_extent_bytes(l, B, N, H, d) / 2 * elt_size(dtype); }
+// The bytes of rows, without what lies between them: views of one projection's output share none, though their extents do.
+ByteGrid rows_grid(const void* p, const KvLayout& l, int B, int N, int H, int d, int dtype) {
+    const int64_t e = (int64_t)elt_size(dtype), stride[3] = {l.batch * e, l.token * e, l.head * e}, n[3] = {B, N, H};
+    ByteGrid g{p, 0, {}, {}, d * e};
+    for (int x = 0; x < 3; ++x) {
+        if (n[x] < 2) continue;
+        int at = g.axes++;
+        for (; at > 0 && g.stride[at - 1] < stride[x]; --at) { g.stride[at] = g.stride[at - 1]; g.n[at] = g.n[at - 1]; }
+        g.stride[at] = stride[x];
+        g.n[at] = n[x];
+    }
+    return g;
+}
 
 }  // namespace
 }  // namespace md

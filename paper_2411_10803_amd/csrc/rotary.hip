@@ -387,12 +387,15 @@ int rotate_impl(const void* q, const void* k, int dtype, const int32_t* position
     // channels / four: 120 / 90
     const int W = dtype != MD_F32 && ang.turn.pairs % 8 == 0 && d % 16 == 0 ? 8 : 4, items = d / (2 * W);
     if (all > kMaxRows || all * (Hq + H) * items > 0x7FFFFFFFl - 511) return fail(MD_ESHAPE, "rotate: %ld rows of %d heads are too many for one call", all, Hq + H);
-    const size_t qi = rows_bytes(a.xl, B, N, Hq, d, dtype), qo = rows_bytes(a.yl, B, N, Hq, d, dtype);
-    const size_t ki = k ? rows_bytes(c.xl, B, N, H, d, dtype) : 0, ko = k ? rows_bytes(c.yl, B, N, H, d, dtype) : 0;
-    const Range r[] = {{q_out, qo}, {k_out, ko}, {q, same_place(q, a.xl, q_out, a.yl) ? 0 : qi}, {k, same_place(k, c.xl, k_out, c.yl) ? 0 : ki},
-                       {positions, position_bytes(ang)}, {index, index ? (size_t)all * 4 : 0}, {table, table_bytes(ang)}, {rows, rows ? (size_t)B * 4 : 0}};
-    rc = check_apart(who, r, 2, 8);
+    const ByteGrid qi = rows_grid(q, a.xl, B, N, Hq, d, dtype), qo = rows_grid(q_out, a.yl, B, N, Hq, d, dtype);
+    const ByteGrid ki = rows_grid(k, c.xl, B, N, H, d, dtype), ko = rows_grid(k_out, c.yl, B, N, H, d, dtype);
+    const Range r[] = {{q_out, rows_bytes(a.yl, B, N, Hq, d, dtype)}, {k_out, k ? rows_bytes(c.yl, B, N, H, d, dtype) : 0}, {positions, position_bytes(ang)},
+                       {index, index ? (size_t)all * 4 : 0}, {table, table_bytes(ang)}, {rows, rows ? (size_t)B * 4 : 0}};
+    for (int x = 0; x < 2 && rc == MD_OK; ++x) rc = check_apart(who, r[x], r + 2, 4);
     if (rc != MD_OK) return rc;
+    if (overlaps(qo, ko) || overlaps(qo, ki) || overlaps(ko, qi) || (!same_place(q, a.xl, q_out, a.yl) && overlaps(qo, qi)) ||
+        (!same_place(k, c.xl, k_out, c.yl) && overlaps(ko, ki)))
+        return fail(MD_EALIAS, "rotate: the outputs and the inputs must not overlap");
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int per = 256 / items;
     // four heads to a thread where there are threads for all of the chip several times over.  us with one / two / four, 4 x up to 2371 rows
@@ -438,12 +441,16 @@ int append_impl(const void* q, const void* k_new, const void* v_new, int dtype, 
         return fail(MD_EALIGN, "cache4_append: tensors must be 16-byte aligned");
     const long rows = (long)B * N;
     if (rows > kMaxRows) return fail(MD_ESHAPE, "cache4_append: %ld rows are too many for one call", rows);
-    const size_t in = rows_bytes(A.kl, B, N, H, d, dtype), qi = q ? rows_bytes(A.ql, B, N, Hq, d, dtype) : 0, qo = q ? rows_bytes(A.ol, B, N, Hq, d, dtype) : 0;
-    const Range r[] = {{cache, pool_bytes(A.p)}, {q_out, qo}, {q, same_place(q, A.ql, q_out, A.ol) ? 0 : qi}, {k_new, in}, {v_new, in}, {slots, (size_t)rows * 4},
-                       {positions, position_bytes(ang)}, {index, index ? (size_t)rows * 4 : 0}, {table, table_bytes(ang)}};
-    rc = check_apart(who, r, 2, 9);
+    const size_t in = rows_bytes(A.kl, B, N, H, d, dtype);
+    const ByteGrid ki = rows_grid(k_new, A.kl, B, N, H, d, dtype), vi = rows_grid(v_new, A.kl, B, N, H, d, dtype);
+    const ByteGrid qi = rows_grid(q, A.ql, B, N, Hq, d, dtype), qo = rows_grid(q_out, A.ol, B, N, Hq, d, dtype);
+    const Range r[] = {{cache, pool_bytes(A.p)}, {q_out, q ? rows_bytes(A.ol, B, N, Hq, d, dtype) : 0}, {slots, (size_t)rows * 4}, {positions, position_bytes(ang)},
+                       {index, index ? (size_t)rows * 4 : 0}, {table, table_bytes(ang)}, {k_new, in}, {v_new, in}, {q, q ? rows_bytes(A.ql, B, N, Hq, d, dtype) : 0}};
+    rc = check_apart(who, r[0], r + 1, 8);
+    if (rc == MD_OK) rc = check_apart(who, r[1], r + 2, 4);
     if (rc != MD_OK) return rc;
-    if (q && overlaps(cache, pool_bytes(A.p), q, qi)) return fail(MD_EALIAS, "cache4_append: the outputs, the workspace and the inputs must not overlap");
+    if (overlaps(qo, ki) || overlaps(qo, vi) || (!same_place(q, A.ql, q_out, A.ol) && overlaps(qo, qi)))
+        return fail(MD_EALIAS, "cache4_append: the outputs and the inputs must not overlap");
     A.q = q; A.k = k_new; A.v = v_new; A.q_out = q_out; A.slots = slots; A.cache = static_cast<uint8_t*>(cache); A.Hq = Hq; A.rows = (int)rows;
     hipStream_t st = static_cast<hipStream_t>(stream);
     // two heads to a wave where there are waves for all of the chip more than once.  us with one / two / four, 16 x up to 777 fp32 rows of 40 + 16

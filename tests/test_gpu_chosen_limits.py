@@ -1,0 +1,106 @@
+"""Calls at the ends of what the rotation, the bounds, the choice and the attention over chosen pages take: views of one projection, samples
+without new entries, millions of lists and of pages, lists and tables as long as a block holds."""
+import numpy as np
+import pytest
+
+import cache4_ref as ref
+import chosen_ref as cr
+from test_gpu_cache4 import BF16, F32, dev, host
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ views of one projection
+
+def projection(torch, B, N, heads, d, dtype, layout):
+    """What one product gives, and its views [B, N, h, d] for each of `heads`; two heads between the last one and the next row."""
+    kind = torch.bfloat16 if dtype == BF16 else torch.float32
+    total = sum(heads) + 2
+    shape = {"tokens": (B, N, total, d), "heads": (B, total, N, d), "samples last": (N, B, total, d)}[layout]
+    whole = torch.randn(shape, device="cuda").to(kind)
+    view = {"tokens": lambda t: t, "heads": lambda t: t.transpose(1, 2), "samples last": lambda t: t.transpose(0, 1)}[layout](whole)
+    return whole, list(view.split([*heads, 2], dim=2))[:-1]
+
+
+FUSED = [
+    # B, N, Hq, H, d, sections, dtype, layout, adjacent
+    (2, 3, 8, 4, 128, [64], BF16, "tokens", False),
+    (3, 7, 4, 4, 64, [16, 8], F32, "tokens", True),
+    (2, 5, 6, 2, 128, [32, 16], BF16, "heads", False),
+    (2, 9, 3, 1, 64, [32], F32, "heads", False),
+    (3, 4, 5, 1, 128, [24, 24], BF16, "samples last", True),
+    (1, 40, 4, 2, 128, [64], F32, "tokens", False),
+    (40, 1, 4, 2, 64, [16], BF16, "tokens", False),
+    (2, 2600, 13, 3, 128, [64], BF16, "tokens", False),      # several heads to a thread
+    (2, 1300, 12, 4, 128, [40], F32, "tokens", False),
+]
+
+
+@pytest.mark.parametrize("i", range(len(FUSED)))
+def test_rotation_in_place_of_views_of_one_projection(i):
+    import torch
+    import paper_2411_10803_amd as md
+    torch.manual_seed(i)
+    B, N, Hq, H, d, sections, dtype, layout, adjacent = FUSED[i]
+    whole, (q, k, v) = projection(torch, B, N, (Hq, H, H), d, dtype, layout)
+    table, turn = md.rotary_table(500, sum(sections)), md.rotary(sections, adjacent)
+    pos = torch.randint(0, 500, (len(sections), B, N), dtype=torch.int32, device="cuda")
+    before, copies = whole.clone(), [t.contiguous().clone() for t in (q, k)]
+    want = md.mustdrop_rotate(copies[0], pos, table, turn, k=copies[1], q_out=torch.zeros_like(copies[0]), k_out=torch.zeros_like(copies[1]))
+    got = md.mustdrop_rotate(q, pos, table, turn, k=k)
+    torch.cuda.synchronize()
+    assert got[0] is q and got[1] is k and torch.equal(q, want[0]) and torch.equal(k, want[1])
+    q.copy_(copies[0])
+    k.copy_(copies[1])
+    assert torch.equal(whole, before), "something beside the queries and keys was written"
+    # out into another view of the same memory that shares no byte with any
+    if Hq == H and not layout == "samples last":
+        md.mustdrop_rotate(q, pos, table, turn, q_out=v)
+        torch.cuda.synchronize()
+        assert torch.equal(v, want[0]) and torch.equal(q, copies[0]) and torch.equal(k, copies[1])
+
+
+@pytest.mark.parametrize("i", range(len(FUSED)))
+def test_append_of_views_of_one_projection(i):
+    import torch
+    import paper_2411_10803_amd as md
+    torch.manual_seed(50 + i)
+    B, N, Hq, H, d, sections, dtype, layout, adjacent = FUSED[i]
+    page = 16
+    whole, (q, k, v) = projection(torch, B, N, (Hq, H, H), d, dtype, layout)
+    table, turn = md.rotary_table(500, sum(sections)), md.rotary(sections, adjacent)
+    pos = torch.randint(0, 500, (len(sections), B, N), dtype=torch.int32, device="cuda")
+    n_pages = -(-B * N // page) + 1
+    slots = torch.randperm(n_pages * page, device="cuda")[:B * N].to(torch.int32).reshape(B, N).contiguous()
+    caches = [md.cache4_buffer(n_pages, page, H, d) for _ in range(2)]
+    before, copies = whole.clone(), [t.contiguous().clone() for t in (q, k, v)]
+    want = md.mustdrop_cache4_append(*copies, pos, table, turn, slots, caches[0], q_out=torch.zeros_like(copies[0]))
+    got = md.mustdrop_cache4_append(q, k, v, pos, table, turn, slots, caches[1])
+    torch.cuda.synchronize()
+    assert got is q and torch.equal(q, want) and torch.equal(*caches)
+    q.copy_(copies[0])
+    assert torch.equal(whole, before), "something beside the queries was written"
+
+
+def test_views_that_share_bytes_are_refused():
+    import torch
+    import paper_2411_10803_amd as md
+    whole = torch.randn((2, 6, 10, 64), device="cuda").bfloat16()
+    table, turn = md.rotary_table(9, 32), md.rotary([32])
+    pos = torch.zeros((1, 2, 6), dtype=torch.int32, device="cuda")
+    before = whole.clone()
+    q = whole[:, :, :4]
+    for other in (dict(q_out=whole[:, :, 1:5]), dict(q_out=whole[:, :, 3:7]), dict(k=whole[:, :, 2:5]), dict(k=whole[:, :, 3:4]),
+                  dict(q_out=whole[:, :, 4:8], k=whole[:, :, 7:9]), dict(k=whole[:, :, 4:6], k_out=whole[:, :, 5:7]),
+                  dict(q_out=torch.zeros_like(q), k=whole[:, :, 4:6], k_out=whole[:, :, 2:4])):
+        with pytest.raises(md.MustDropError, match="overlap"):
+            md.mustdrop_rotate(q, pos, table, turn, **other)
+    cache = md.cache4_buffer(2, 16, 3, 64)
+    slots = torch.arange(12, dtype=torch.int32, device="cuda").reshape(2, 6).contiguous()
+    for k in (whole[:, :, 2:5], whole[:, :, 3:6]):
+        with pytest.raises(md.MustDropError, match="overlap"):
+            md.mustdrop_cache4_append(q, k, whole[:, :, 7:], pos, table, turn, slots, cache)
+        with pytest.raises(md.MustDropError, match="overlap"):
+            md.mustdrop_cache4_append(q, whole[:, :, 7:], k, pos, table, turn, slots, cache)
+    torch.cuda.synchronize()
+    assert torch.equal(whole, before) and not bool(cache.any())
