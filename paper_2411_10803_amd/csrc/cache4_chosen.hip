@@ -58,8 +58,8 @@ __global__ __launch_bounds__(256) void cache4_bounds_kernel(
     asm volatile("" : "+s"(length), "+s"(from));     // (on their way together)
     length = c4_clamp(length, 0, p.max_pages << p.page_shift);
     from = first ? max(from, 0) : 0;
-    const long e = (long)(from >> p.page_shift) + x;
-    if ((e << p.page_shift) >= min((long)from + N, (long)length)) return;
+    const long e = (long)(from >> p.page_shift) + x, stop = min((long)from + N, (long)length);
+    if (from >= stop || (e << p.page_shift) >= stop) return;                 // (the page of an entry that is not there yet may hold others)
     const int id = c4_page_id(table[(long)b * p.max_pages + e], p.n_pages);
     if (id < 0) return;
     const int live = min(length - (int)(e << p.page_shift), p.page);

@@ -104,3 +104,34 @@ def test_views_that_share_bytes_are_refused():
             md.mustdrop_cache4_append(q, whole[:, :, 7:], k, pos, table, turn, slots, cache)
     torch.cuda.synchronize()
     assert torch.equal(whole, before) and not bool(cache.any())
+
+
+# ------------------------------------------------------------------------------------------------ bounds
+
+@pytest.mark.parametrize("d, page", [(128, 32), (64, 16), (64, 256)])
+def test_bounds_of_samples_without_new_entries(d, page):
+    """Only pages that hold an entry first .. min(first + n, length) - 1 are written: none where first is the length or behind it."""
+    import torch
+    import paper_2411_10803_amd as md
+    from test_gpu_chosen import filled_pool
+    rng = np.random.default_rng(d)
+    H, entries, n = 2, 3, 7
+    cap = entries * page
+    #         first, length: at the length, behind it, at the pool's end, one entry in the same page, none at all, negative
+    samples = [(page + 1, page + 1), (page + 3, page + 1), (cap, cap), (page + 1, page + 2), (0, 0), (-4, 0), (5, 1), (-3, 1), (2 ** 31 - 1, cap), (page - 1, page + 1)]
+    B = len(samples)
+    pool, _, _ = filled_pool(rng, 4, H, d, page)
+    pool = np.concatenate([pool] * 8)
+    table = rng.permutation(len(pool))[:B * entries].reshape(B, entries).astype(np.int32)
+    b, s = md.cache4_bounds_buffer(len(pool), H, d)
+    b.fill_(99)
+    s.fill_(77)
+    first, length = (dev(np.array(x, np.int32)) for x in zip(*samples))
+    md.mustdrop_cache4_bounds(dev(pool), dev(table), length, n, b, s, first=first)
+    torch.cuda.synchronize()
+    wb, ws, written = np.full((len(pool), H, 2, d), 99), np.full((len(pool), H), 77), 0
+    for x, (lo, to) in enumerate(samples):
+        for e in sorted({t // page for t in range(max(lo, 0), min(max(lo, 0) + n, to))}):
+            wb[table[x, e]], ws[table[x, e]] = cr.bounds(pool, table[x, e], min(page, to - e * page), H, d, page)
+            written += 1
+    assert written == 4 and np.array_equal(host(b), wb) and np.array_equal(host(s), ws)
