@@ -516,7 +516,9 @@ int mustdrop_cache4_choose(
  * the pages that chosen[b][i][h][0 .. budget-1] names.  An entry of chosen that is not in 0 .. max_pages-1, or not above every such entry
  * before it in its list, takes no part: a page counts once.  With all pages chosen the two calls mean the same.  Everything else
  * (values that are no numbers, rows that see nothing, limits of scores) as for mustdrop_cache4_attend; a probability always carries 16 bits
- * for MD_BF16.  Two calls on the same inputs, with lists and tables of the same width, give the same bits.  Errors likewise, and MD_ESHAPE for 2^23 or more tiles of 16 query heads or parts of them. */
+ * for MD_BF16.  Two calls on the same inputs, with lists and tables of the same width, give the same bits.  Errors likewise, and MD_ESHAPE for 2^23 or more tiles of 16 query heads or parts of them.
+ * Lists of more than 1024 entries, and few long ones, are cut into parts, whose sums go through the workspace: its size is what calls with these
+ * sizes and any table need at most, 4 (d + 2) bytes for each query head (of more than 16 to one: 16 at a time) and part; a call whose tokens go together has no parts and needs 256. */
 size_t mustdrop_cache4_attend_chosen_workspace_bytes(int B, int N, int Hq, int H, int d, int budget, int page);
 
 int mustdrop_cache4_attend_chosen(

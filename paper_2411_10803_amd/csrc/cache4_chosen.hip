@@ -670,6 +670,8 @@ __device__ __forceinline__ Sight sight_at(const Shared& w, int step) {
 
 // tokens: that a block takes together; splits, most: parts of a list, and entries of a part
 struct Chosen { const int32_t* list; int budget, splits, most, tokens; };
+// Query rows of a part in the workspace: the heads that one unit has, sixteen at most.
+__host__ __device__ __forceinline__ int part_rows(int G) { return G < 16 ? G : 16; }
 constexpr int kChosenAt = (sizeof(AttendArgs) + 7) / 8 * 8;
 constexpr int kChosenPartsAt = (kChosenAt + (int)sizeof(Chosen) + 7) / 8 * 8;
 
@@ -827,7 +829,7 @@ __global__ __launch_bounds__(F32 && D == 128 ? 256 : 512, F32 && D == 128 ? 3 : 
     } else {
         const Parts parts = argument<Parts>(kChosenPartsAt);
         join_waves<D, 1>(sw, rows, reinterpret_cast<float*>(lds), [&](int row, int part, const float (&x)[D / 16], float m, float l) {
-            store_part<D>(parts, blockIdx.x, 16, row, part, x, m, l);
+            store_part<D>(parts, blockIdx.x, part_rows(A.dim.G), row, part, x, m, l);
         });
     }
 }
@@ -917,7 +919,7 @@ __global__ __launch_bounds__(256) void cache4_attend_chosen_join_kernel(AttendAr
     if (u.i >= s.nq || u.g0 + row >= A.dim.G) return;          // (the whole block)
     float m = kNoKey, l = 0.f, acc[E] = {};
     for (int y = threadIdx.x >> 4; y < C.splits; y += 16) {
-        const long at = ((long)unit * C.splits + y) * 16 + row;
+        const long at = ((long)unit * C.splits + y) * part_rows(A.dim.G) + row;
         const float2 ml = parts.ml[at];
         float v[E];
 #pragma unroll
@@ -1085,9 +1087,9 @@ ChosenPlan chosen_plan(void* workspace, bool f32, int B, int N, int Hq, int d, i
     const size_t join = sizeof(float) * ((size_t)a.cut.waves * rows * (d + 4) + 2 * a.cut.waves * 16), ring = (size_t)a.cut.waves * kRing * (32 * d + 256);
     const size_t list = (size_t)(a.cut.most + 1) / 2 * 16 + (a.cut.tokens > 1 ? (size_t)(a.cut.most + 7) / 8 * 16 : 0);
     a.lds = list + (join > ring ? join : ring);      // (the ring is more than two bytes for each entry of a table that lists are shared in)
-    // parts of lists are joined through the workspace, whose size goes by the calls that have most of them
-    const C4Chosen apart = c4_chosen(f32, d, B, N, G, p.H, budget, p.page, 0);
-    const size_t places = apart.splits > 1 ? (size_t)B * N * p.H * a.tiles * apart.splits * 16 : 0;
+    // (parts of lists are joined through the workspace.  Tokens that go together have none; without max_pages nobody goes together: the most that
+    // a call may need)
+    const size_t places = a.cut.splits > 1 ? (size_t)a.units * a.cut.splits * part_rows(G) : 0;
     Carver c(workspace);
     a.parts.o = c.take<float>(places * d);
     a.parts.ml = c.take<float2>(places);
@@ -1132,7 +1134,7 @@ int attend_chosen_impl(const void* q, int dtype, const void* cache, const int32_
     if (!aligned16(q) || !aligned16(out) || !aligned16(cache) || (reinterpret_cast<uintptr_t>(keep) & 3u))
         return fail(MD_EALIGN, "cache4_attend_chosen: tensors must be 16-byte aligned, keep 4-byte aligned");
     const ChosenPlan plan = chosen_plan(workspace, dtype == MD_F32, B, N, Hq, d, budget, max_pages, p);
-    const size_t need = attend_chosen_bytes(B, N, Hq, H, d, budget, page);
+    const size_t need = plan.bytes;
     const Range r[] = {{out, rows_bytes(ol, B, N, Hq, d, dtype)}, {lse, lse ? (size_t)B * Hq * N * 4 : 0}, {workspace, workspace ? need : 0},
                        {q, rows_bytes(ql, B, N, Hq, d, dtype)}, {cache, pool_bytes(p)}, {table, (size_t)B * max_pages * 4}, {len, (size_t)B * 4},
                        {q_len, q_len ? (size_t)B * 4 : 0}, {keep, keep ? (size_t)B * max_pages * page : 0}, {chosen, (size_t)B * N * H * budget * 4}};
@@ -1150,7 +1152,7 @@ int attend_chosen_impl(const void* q, int dtype, const void* cache, const int32_
     do {                                                                                                                                  \
         if (C.tokens > 1) { MD_LAUNCH("cache4_attend_shared", st, (cache4_attend_shared_kernel<D_, F_, S_>), blocks, plan.cut.waves * 64, plan.lds, A, C); break; } \
         MD_LAUNCH("cache4_attend_chosen", st, (cache4_attend_chosen_kernel<D_, F_, S_>), blocks, plan.cut.waves * 64, plan.lds, A, C, plan.parts); \
-        if (C.splits > 1) MD_LAUNCH("cache4_chosen_join", st, (cache4_attend_chosen_join_kernel<D_, F_>), dim3((unsigned)plan.units, (unsigned)(A.dim.G < 16 ? A.dim.G : 16)), 256, 0, A, C, plan.parts); \
+        if (C.splits > 1) MD_LAUNCH("cache4_chosen_join", st, (cache4_attend_chosen_join_kernel<D_, F_>), dim3((unsigned)plan.units, (unsigned)part_rows(A.dim.G)), 256, 0, A, C, plan.parts); \
     } while (0)
 #define MD_C4_CHOSEN_S(D_, F_) do { if (stream_once) MD_C4_CHOSEN(D_, F_, true); else MD_C4_CHOSEN(D_, F_, false); } while (0)
     if (d == 128) { if (dtype == MD_F32) MD_C4_CHOSEN_S(128, true); else MD_C4_CHOSEN_S(128, false); }

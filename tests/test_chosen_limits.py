@@ -1,11 +1,12 @@
 """The ends of what the rotation and the calls on chosen pages take, without a GPU: what shares a byte, refusals."""
+import ctypes as C
 import os
 import shutil
 import subprocess
 
 import pytest
 
-from test_chosen import EALIAS, append, layout, lib, moved, P, rotate  # noqa: F401
+from test_chosen import EALIAS, EWORKSPACE, append, attend, layout, lib, moved, P, rotate  # noqa: F401
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -35,3 +36,23 @@ def test_views_of_one_projection_that_share_bytes_are_refused(lib):  # noqa: F81
     assert append(lib, **dict(rows, k=moved(q, 7 * head), v=v)) == EALIAS and append(lib, **dict(rows, k=k, v=moved(q, 16 * head))) == EALIAS
     assert append(lib, **dict(rows, k=k, v=v, qo=moved(q, 2 * head))) == EALIAS and append(lib, **dict(rows, k=k, v=v, slots=v)) == EALIAS
     assert append(lib, **dict(rows, k=k, v=v, cache=v)) == EALIAS and append(lib, **dict(rows, k=k, v=v, cache=q)) == EALIAS
+
+
+# ---- the workspace of the attention over chosen pages
+@pytest.mark.parametrize("B, N, Hq, H, d", [(4, 512, 32, 32, 128), (1, 4000, 32, 32, 128), (4, 512, 64, 8, 64), (2, 900, 16, 1, 128), (2, 900, 40, 1, 64)])
+def test_workspace_of_lists_of_more_than_a_part(lib, B, N, Hq, H, d):  # noqa: F811
+    """A sum of d channels and two numbers for each query head and part of 1024 entries; nothing where there is one part."""
+    size = lib.mustdrop_cache4_attend_chosen_workspace_bytes
+    G = Hq // H
+    tile = min(G, 16) * -(-G // 16)                          # (the last sixteen heads of more take whole places)
+    for budget, parts in ((1024, 1), (1025, 2), (2048, 2), (2049, 3), (9000, 9)):
+        want = B * N * H * tile * parts * (d + 2) * 4 if parts > 1 else 0
+        assert max(want, 256) <= size(B, N, Hq, H, d, budget, 16) <= want + 512, budget
+
+
+def test_workspace_of_tokens_that_go_together(lib):  # noqa: F811
+    """Lists that are padded beyond 1024 entries, in a table of fewer: no parts, and none asked for."""
+    for dtype in (0, 1):
+        few = dict(B=4, N=512, Hq=32, H=32, budget=1025, page=16, max_pages=100, dtype=dtype)
+        assert attend(lib, **few, wsb=C.c_size_t(255)) == EWORKSPACE and b"256 bytes needed" in lib.mustdrop_last_error()
+        assert attend(lib, **dict(few, max_pages=5000), wsb=C.c_size_t(256)) == EWORKSPACE       # (such tables are not shared in)

@@ -6,6 +6,7 @@ import pytest
 import cache4_ref as ref
 import chosen_ref as cr
 from test_gpu_cache4 import BF16, F32, dev, host
+from test_gpu_chosen import Chosen
 
 pytestmark = pytest.mark.gpu
 
@@ -135,3 +136,29 @@ def test_bounds_of_samples_without_new_entries(d, page):
             wb[table[x, e]], ws[table[x, e]] = cr.bounds(pool, table[x, e], min(page, to - e * page), H, d, page)
             written += 1
     assert written == 4 and np.array_equal(host(b), wb) and np.array_equal(host(s), ws)
+
+
+# ------------------------------------------------------------------------------------------------ the attention's workspace
+
+def test_tokens_together_with_long_lists_have_no_use_for_a_workspace():
+    """Lists padded to 1100 entries in a table of 26: a workspace of 256 bytes, between bands that stay as they were."""
+    import torch
+    import paper_2411_10803_amd as md
+    c = Chosen(81, [390], 391, 8, 4, 64, 16, 1100, BF16, kind="any")
+    whole = torch.full((256 + 16384,), 0xA5, dtype=torch.uint8, device="cuda")
+    out, lse = c.call(md, workspace=whole[8192:8448])
+    assert bool((whole[:8192] == 0xA5).all()) and bool((whole[8448:] == 0xA5).all())
+    c.check(out, lse)
+
+
+@pytest.mark.parametrize("Hq, H, dtype", [(3, 3, BF16), (10, 2, F32), (20, 1, BF16), (33, 1, F32)])
+def test_parts_leave_their_sums_in_the_workspace_that_is_asked_for(Hq, H, dtype):
+    """Lists in parts, with 1, 5, 20 and 33 query heads to one: exactly the workspace's size, between bands."""
+    import torch
+    import paper_2411_10803_amd as md
+    c = Chosen(82, [1500, 900], 2, Hq, H, 64, 16, 1300, dtype, kind="any", keep=0.8)
+    n = md.library().mustdrop_cache4_attend_chosen_workspace_bytes(2, 2, Hq, H, 64, 1300, 16)
+    whole = torch.full((n + 16384,), 0xA5, dtype=torch.uint8, device="cuda")
+    out, lse = c.call(md, workspace=whole[8192:8192 + n])
+    assert bool((whole[:8192] == 0xA5).all()) and bool((whole[8192 + n:] == 0xA5).all())
+    c.check(out, lse)
