@@ -1024,6 +1024,7 @@ int choose_impl(const void* q, int dtype, const int8_t* bounds, const uint8_t* s
     if (rc == MD_OK) rc = check_dtype(who, dtype);
     if (rc != MD_OK) return rc;
     if (budget <= 0 || first_pages < 0 || last_pages < 0) return fail(MD_EINVAL, "cache4_choose: budget must be positive, first_pages and last_pages not negative");
+    if (budget > 1 << 26) return fail(MD_ESHAPE, "cache4_choose: a list of %d pages is too long", budget);        // (its places are counted in 31 bits, 1024 at a time)
     if ((long)first_pages + last_pages > budget) return fail(MD_EINVAL, "cache4_choose: %d first and %d last pages are more than the budget of %d", first_pages, last_pages, budget);
     if (!q || !bounds || !scales || !table || !len || !chosen) return fail(MD_EINVAL, "cache4_choose: null pointer among the required arguments");
     rc = read_layout(who, "q", q_layout, B, N, Hq, d, &A.ql);

@@ -6,7 +6,7 @@ import subprocess
 
 import pytest
 
-from test_chosen import EALIAS, EWORKSPACE, append, attend, layout, lib, moved, P, rotate  # noqa: F401
+from test_chosen import EALIAS, ESHAPE, EWORKSPACE, append, attend, choose, layout, lib, moved, P, rotate  # noqa: F401
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -56,3 +56,13 @@ def test_workspace_of_tokens_that_go_together(lib):  # noqa: F811
         few = dict(B=4, N=512, Hq=32, H=32, budget=1025, page=16, max_pages=100, dtype=dtype)
         assert attend(lib, **few, wsb=C.c_size_t(255)) == EWORKSPACE and b"256 bytes needed" in lib.mustdrop_last_error()
         assert attend(lib, **dict(few, max_pages=5000), wsb=C.c_size_t(256)) == EWORKSPACE       # (such tables are not shared in)
+
+
+# ---- the choice
+def test_lists_that_are_too_long_are_refused(lib):  # noqa: F811
+    """A list's places are counted in 31 bits, in steps of up to 1024: a budget near 2^31 would not end."""
+    for max_pages in (6, 900, 3000, 9000):
+        for budget in (2 ** 26 + 1, 2 ** 31 - 1024, 2 ** 31 - 1):
+            few = dict(B=1, N=1, H=1, Hq=1, max_pages=max_pages, page=16, budget=budget)
+            assert choose(lib, **few, ws=None) == ESHAPE and b"too long" in lib.mustdrop_last_error()
+    assert choose(lib, B=1, N=1, H=1, Hq=1, budget=2 ** 26, ws=None) == EWORKSPACE
