@@ -491,6 +491,12 @@ __global__ __launch_bounds__(256, 4) void cache4_score_choose_kernel(Choose A, F
         choose_by_wave<K>(A, s_score + (i - i0) * A.pitch, sc.seen_by(i), A.chosen + (((long)b * A.N + i) * A.H + h) * A.budget, s_hist[wave_id()]);
 }
 
+// The list that a block deals with, of one launch's rows of blocks (c4_lists); -1 behind the last one.
+__device__ __forceinline__ int list_at(const Choose& A) {
+    const uint32_t at = blockIdx.y * gridDim.x + blockIdx.x;             // (fewer than 2^23 + 2^21)
+    return at < (uint32_t)(A.B * A.H * A.N) ? (int)at : -1;
+}
+
 // The same by the waves of a block, of up to WAVES * 512 scores in the workspace: wave w's lane l has those of pages (WAVES j + w) * 64 + l.
 template <int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void cache4_choose_block_kernel(Choose A, FastDiv tokens, FastDiv heads)
@@ -499,9 +505,11 @@ __global__ __launch_bounds__(WAVES * 64) void cache4_choose_block_kernel(Choose 
     __shared__ __align__(16) int s_hist[4 * 256];
     __shared__ uint32_t s_least[WAVES], s_most[WAVES];
     __shared__ int s_count[WAVES * K];
-    const int bh = tokens.div(blockIdx.x), i = blockIdx.x - bh * tokens.d, b = heads.div(bh), h = bh - b * heads.d;
+    const int list = list_at(A);
+    if (list < 0) return;
+    const int bh = tokens.div(list), i = list - bh * tokens.d, b = heads.div(bh), h = bh - b * heads.d;
     const int lane = lane_id(), wv = wave_id();
-    const float* score = A.scores + (long)blockIdx.x * A.pitch;
+    const float* score = A.scores + (long)list * A.pitch;
     float f[K];
 #pragma unroll
     for (int j = 0; j < K; ++j) f[j] = score[min((WAVES * j + wv) * kWave + lane, A.pitch - 1)];     // (on their way with the length)
@@ -568,10 +576,12 @@ __device__ __forceinline__ uint64_t page_key(float score, int e) { return ((uint
 __global__ __launch_bounds__(1024) void cache4_choose_kernel(Choose A, FastDiv tokens, FastDiv heads)
 {
     __shared__ int s_hist[kSelectHistInts], s_red[16];
-    const int bh = tokens.div(blockIdx.x), i = blockIdx.x - bh * tokens.d, b = heads.div(bh), h = bh - b * heads.d, tid = threadIdx.x;
+    const int list = list_at(A);
+    if (list < 0) return;
+    const int bh = tokens.div(list), i = list - bh * tokens.d, b = heads.div(bh), h = bh - b * heads.d, tid = threadIdx.x;
     const int P = pages_seen(A, b, i);
     if (P < 0) return;
-    const float* score = A.scores + (long)blockIdx.x * A.pitch;
+    const float* score = A.scores + (long)list * A.pitch;
     int32_t* to = A.chosen + (((long)b * A.N + i) * A.H + h) * A.budget;
     if (P <= A.budget) {
         for (int x = tid; x < A.budget; x += 1024) to[x] = x < P ? x : -1;
@@ -1064,9 +1074,12 @@ int choose_impl(const void* q, int dtype, const int8_t* bounds, const uint8_t* s
 #undef MD_C4_SCORE
 #undef MD_C4_SCORE2
     // us for 8 lists of 2500 / 7500 scores: sixteen waves with eight each to a lane 6.3 / 7.4, by keys that are looked up again 6.6 / 11.6
-    if (max_pages <= 2048) MD_LAUNCH("cache4_choose", st, (cache4_choose_block_kernel<4>), B * H * N, 256, 0, A, FastDiv::make(N), FastDiv::make(H));
-    else if (max_pages <= 8192) MD_LAUNCH("cache4_choose", st, (cache4_choose_block_kernel<16>), B * H * N, 1024, 0, A, FastDiv::make(N), FastDiv::make(H));
-    else MD_LAUNCH("cache4_choose", st, (cache4_choose_kernel), B * H * N, 1024, 0, A, FastDiv::make(N), FastDiv::make(H));
+    const int threads = max_pages <= 2048 ? 256 : 1024;
+    const C4Lists l = c4_lists(B * H * N, threads);
+    const dim3 lists(l.x, l.y);
+    if (max_pages <= 2048) MD_LAUNCH("cache4_choose", st, (cache4_choose_block_kernel<4>), lists, threads, 0, A, FastDiv::make(N), FastDiv::make(H));
+    else if (max_pages <= 8192) MD_LAUNCH("cache4_choose", st, (cache4_choose_block_kernel<16>), lists, threads, 0, A, FastDiv::make(N), FastDiv::make(H));
+    else MD_LAUNCH("cache4_choose", st, (cache4_choose_kernel), lists, threads, 0, A, FastDiv::make(N), FastDiv::make(H));
     return check_launch(who);
 }
 

@@ -130,6 +130,13 @@ inline bool c4_choose_together(int64_t blocks, int pitch, size_t lds) {
     return pitch <= 2048 && lds <= 61440 && (pitch <= 256 || blocks * 2 >= pitch);
 }
 
+// A launch has fewer than 2^32 threads along x: lists of the choice with a block of `threads` threads each, in how many blocks along x, and along y.
+struct C4Lists { int x, y; };
+inline C4Lists c4_lists(int lists, int threads) {
+    const int most = (int)(0x80000000u / (unsigned)threads);
+    return lists <= most ? C4Lists{lists, 1} : C4Lists{most, (int)(((int64_t)lists + most - 1) / most)};
+}
+
 // How the attention over chosen pages is cut.
 //   tokens   that a block takes together, as many as fill 16 query rows with their heads: over all of the pages that any of them has chosen.
 //            What a key costs is then shared, but where tokens choose different pages there are more of them to go through and fewer blocks.

@@ -12,10 +12,12 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 
 
 @pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not found")
-def test_rows_that_share_a_byte(tmp_path):
-    exe = str(tmp_path / "row_overlap")
+@pytest.mark.parametrize("name", ["row_overlap", "cache4_lists"])
+def test_plain_arithmetic(tmp_path, name):
+    """Rows that share a byte, against every byte of small grids; blocks of a launch for any number of lists."""
+    exe = str(tmp_path / name)
     subprocess.check_call(["g++", "-O2", "-std=c++17", "-Wall", "-fsanitize=undefined", "-fno-sanitize-recover=all",
-                           os.path.join(HERE, "plan", "row_overlap_main.cpp"), "-o", exe])
+                           os.path.join(HERE, "plan", name + "_main.cpp"), "-o", exe])
     r = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
     assert r.returncode == 0, r.stdout[-3000:]
 

@@ -162,3 +162,35 @@ def test_parts_leave_their_sums_in_the_workspace_that_is_asked_for(Hq, H, dtype)
     out, lse = c.call(md, workspace=whole[8192:8192 + n])
     assert bool((whole[:8192] == 0xA5).all()) and bool((whole[8192 + n:] == 0xA5).all())
     c.check(out, lse)
+
+
+# ------------------------------------------------------------------------------------------------ the choice
+
+def test_choice_for_millions_of_lists():
+    """4.2 million lists in tables of more than 2048 pages: more threads than one row of blocks has."""
+    import torch
+    import paper_2411_10803_amd as md
+    B, N, d, page, entries, budget, n_pages = 5, 840000, 64, 16, 2049, 4, 40
+    free, _ = torch.cuda.mem_get_info()
+    need = md.library().mustdrop_cache4_choose_workspace_bytes(B, N, 1, 1, d, entries, page)
+    if free < need + (8 << 30):
+        pytest.skip(f"{need >> 30} GiB of workspace")
+    rng = np.random.default_rng(91)
+    lo = rng.integers(-96, 97, (n_pages, 1, d))
+    bounds = np.stack([np.maximum(lo, rng.integers(-96, 97, lo.shape)), lo], 2).astype(np.int8)
+    scales = np.full((n_pages, 1), 127, np.uint8)
+    table = rng.integers(0, n_pages, (B, entries)).astype(np.int32)
+    lengths = [entries * page - 37, 300, 0, entries * page, 5000]
+    torch.manual_seed(92)
+    q = torch.randn((B, N, 1, d), device="cuda").bfloat16()
+    chosen = torch.full((B, N, 1, budget), 99, dtype=torch.int32, device="cuda")
+    ws = torch.empty((need,), dtype=torch.uint8, device="cuda")
+    md.mustdrop_cache4_choose(q, dev(bounds), dev(scales), dev(table), dev(np.array(lengths, np.int32)), page, chosen, first_pages=1, last_pages=1, workspace=ws)
+    torch.cuda.synchronize()
+    for b, n in enumerate(lengths):
+        assert bool((chosen[b, :N - n] == -1).all()), b
+        for i in sorted({N - n, N - n + 65, N - n + 70, N - 1, N - 2, *(N - 1 - rng.integers(0, max(n, 1), 20))} if n else ()):
+            want = cr.choose(host(q[b, i]).astype(np.float64), bounds[:, 0].astype(np.int64), scales[:, 0], table[b], n, N, i, page, 1, 1, budget, n_pages)
+            assert chosen[b, i, 0].tolist() == want, (b, i)
+    del ws
+    torch.cuda.empty_cache()
