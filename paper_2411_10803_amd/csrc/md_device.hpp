@@ -315,6 +315,7 @@ __device__ __forceinline__ SelectBound block_radix_select(KeyFn key, int n, int 
 //   - three histograms take turns (pass p counts into hist[p % 3] and clears hist[(p + 1) % 3], which
 //     nobody reads between the two barriers around it), and every wave scans the finished histogram
 //     itself: one barrier per pass and no hand-over of the result through LDS.
+// Fewer than 2^23 keys.
 // `hist`: 768 ints of shared memory whose first 256 the caller has zeroed, with a block barrier
 // between the zeroing and this call.  All threads of the block (at most 16 waves) must call it.
 constexpr int kSelectHistInts = 768;
@@ -362,7 +363,7 @@ __device__ __forceinline__ SelectBound block_select_keys(ForEach each, int k, in
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 if (run < kk && run + c[t] >= kk)
-                    packed = (255 - (lane * 4 + t)) | ((run + c[t] == kk ? 1 : 0) << 8) | ((kk - run) << 9);
+                    packed = (int)((uint32_t)(255 - (lane * 4 + t)) | ((run + c[t] == kk ? 1u : 0u) << 8) | ((uint32_t)(kk - run) << 9));
                 run += c[t];
             }
         }
@@ -370,7 +371,7 @@ __device__ __forceinline__ SelectBound block_select_keys(ForEach each, int k, in
         const int width = shift - sh;                       // 8, less when the last digit overlaps its predecessor
         prefix = (prefix << width) | ((uint64_t)(packed & 0xFF) & ((1ull << width) - 1ull));
         shift = sh;
-        kk = packed >> 9;
+        kk = (int)((uint32_t)packed >> 9);                  // (23 bits)
         first = false;
         if (((packed >> 8) & 1) || sh == 0) break;          // the chosen bin is taken whole, or no bits are left
         sh = max(sh - 8, 0);

@@ -194,3 +194,32 @@ def test_choice_for_millions_of_lists():
             assert chosen[b, i, 0].tolist() == want, (b, i)
     del ws
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("kind", ["equal", "few", "nothing"])
+def test_choice_of_millions_of_pages(kind):
+    """More than 2^22 pages to take of five million: equal scores, a few values, and queries that are nothing."""
+    import torch
+    import paper_2411_10803_amd as md
+    d, page, entries, budget, n_pages = 64, 16, 5000000, 4600000, 12
+    rng = np.random.default_rng(93)
+    bounds, scales = np.zeros((n_pages, 1, 2, d), np.int8), np.full((n_pages, 1), 127, np.uint8)
+    if kind != "equal":
+        bounds[:, 0, 0, 0] = np.arange(n_pages)
+    q = torch.zeros((1, 1, 1, d), device="cuda")
+    if kind != "nothing":
+        q[..., 0] = 1.0
+    table = rng.integers(0, n_pages, (1, entries)).astype(np.int32)
+    if kind == "few":                                    # nine of ten pages are the same
+        table[rng.random(table.shape) < 0.9] = 2
+    table[0, rng.integers(0, entries, 50)] = -1          # (their scores are below all others)
+    length, last = entries * page - 5, 3
+    chosen = torch.full((1, 1, 1, budget), 99, dtype=torch.int32, device="cuda")
+    md.mustdrop_cache4_choose(q, dev(bounds), dev(scales), dev(table), dev(np.array([length], np.int32)), page, chosen, first_pages=2, last_pages=last)
+    torch.cuda.synchronize()
+    w = cr.whole(host(q)[0, 0].astype(np.float64))
+    by_page = np.array([cr.score(w, bounds[p, 0].astype(np.int64), 127) for p in range(n_pages)] + [-np.inf])
+    score = by_page[table[0]].astype(np.float64)
+    score[:2], score[entries - last:] = np.inf, np.inf
+    want = np.sort(np.argsort(-score, kind="stable")[:budget])
+    assert np.array_equal(host(chosen)[0, 0, 0], want)
