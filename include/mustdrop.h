@@ -503,7 +503,8 @@ int mustdrop_cache4_bounds(
  * equal ones the first, until there are min(budget, P).
  *   q [B, N, Hq, d] (dtype; q_layout);  q_len [B] i32 or NULL (= N)
  *   chosen [B, N, H, budget] i32: entries of the block table in ascending order, then -1; rows i >= q_len[b] untouched
- * first_pages, last_pages >= 0 with a sum of at most budget; budget <= 2^26; G <= 1024 (sums have 31 bits), N * G <= 2^20.  The same inputs give the same pages, whatever else differs.
+ * first_pages, last_pages >= 0 with a sum of at most budget; budget <= 2^26; max_pages <= 2^23 - 128; G <= 1024 (sums have 31 bits),
+ * N * G <= 2^20.  The same inputs give the same pages, whatever else differs.
  * Errors: MD_EINVAL, MD_ESHAPE (limits, more than 2^23 - 1 tokens and heads), MD_EDTYPE, MD_EALIGN, MD_EALIAS, MD_EWORKSPACE, MD_EHIP. */
 size_t mustdrop_cache4_choose_workspace_bytes(int B, int N, int Hq, int H, int d, int max_pages, int page);
 

@@ -1014,6 +1014,8 @@ int choose_plan(const char* who, int B, int N, int Hq, int H, int d, int n_pages
     if (A->G > 1024) return fail(MD_ESHAPE, "%s: %d query heads of one K/V head are too many", who, A->G);
     if ((long)N * A->G > (1l << 20)) return fail(MD_ESHAPE, "%s: %d tokens of %d query heads are too many for one call", who, N, Hq);
     if ((long)B * H > kMaxUnits || (long)B * H * N > kMaxUnits) return fail(MD_ESHAPE, "%s: %d samples of %d tokens and %d heads are too many for one call", who, B, N, H);
+    // (blocks along y; and fewer than 2^23 scores are ranked at a time)
+    if (max_pages > 65535 * 64 * kScoreTiles) return fail(MD_ESHAPE, "%s: %d pages are too many for one request", who, max_pages);
     A->tiles = (N + A->per - 1) / A->per;
     A->lds = 64 + 32 * (d + 16) + (size_t)(N < A->per ? N : A->per) * A->pitch * 4;
     A->together = A->subs == 1 && c4_choose_together((int64_t)B * H * A->tiles, A->pitch, A->lds);
@@ -1053,7 +1055,6 @@ int choose_impl(const void* q, int dtype, const int8_t* bounds, const uint8_t* s
     A.first = first_pages; A.last = last_pages; A.budget = budget;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int tiles = A.tiles, chunks = (max_pages + 64 * kScoreTiles - 1) / (64 * kScoreTiles);
-    if (chunks > 65535) return fail(MD_ESHAPE, "cache4_choose: %d pages are too many for one request", max_pages);
     const long blocks = (long)B * H * tiles;
     if (A.together) {
 #define MD_C4_CHOOSE2(D_, F_, K_)                                                                                                         \

@@ -68,3 +68,12 @@ def test_lists_that_are_too_long_are_refused(lib):  # noqa: F811
             few = dict(B=1, N=1, H=1, Hq=1, max_pages=max_pages, page=16, budget=budget)
             assert choose(lib, **few, ws=None) == ESHAPE and b"too long" in lib.mustdrop_last_error()
     assert choose(lib, B=1, N=1, H=1, Hq=1, budget=2 ** 26, ws=None) == EWORKSPACE
+
+
+def test_choice_in_tables_that_are_too_wide(lib):  # noqa: F811
+    """What no call takes has no workspace, either."""
+    size = lib.mustdrop_cache4_choose_workspace_bytes
+    most = 2 ** 23 - 128
+    assert size(1, 1, 1, 1, 64, most, 16) == most * 4 and size(1, 1, 1, 1, 64, most + 1, 16) == 0
+    few = dict(B=1, N=1, H=1, Hq=1, d=64, page=16, ws=None)
+    assert choose(lib, max_pages=most, **few) == EWORKSPACE and choose(lib, max_pages=most + 1, **few) == ESHAPE
