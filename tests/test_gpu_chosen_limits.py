@@ -223,3 +223,110 @@ def test_choice_of_millions_of_pages(kind):
     score[:2], score[entries - last:] = np.inf, np.inf
     want = np.sort(np.argsort(-score, kind="stable")[:budget])
     assert np.array_equal(host(chosen)[0, 0, 0], want)
+
+
+# ------------------------------------------------------------------------------------------------ lists and tables as long as a block holds
+
+def decoded(pool, d, page):
+    """K and V [pages * page, H, d] of all slots, as float64."""
+    n, H = pool.shape[:2]
+    at = np.cumsum([0, page * d // 2, page * d // 32, page * d // 2, page * d // 32])
+    kc, ks, vc, vs = (pool[:, :, a:b] for a, b in zip(at, at[1:]))
+    nibbles = lambda x: np.stack([x & 15, x >> 4], -1)  # noqa: E731
+    k = ref.values(nibbles(kc.reshape(n, H, page, d // 2)).reshape(n, H, page, d), ks.reshape(n, H, page, d // 32))
+    vc = vc.reshape(n, H, page // 4, 16, 4, d // 32).transpose(0, 1, 2, 4, 3, 5).reshape(n, H, page, d // 2)      # tokens, then their sixteenths
+    vs = vs.reshape(n, H, page // 4, d // 32, 4).transpose(0, 1, 2, 4, 3).reshape(n, H, page, d // 32)
+    v = ref.values(nibbles(vc).reshape(n, H, page, d), vs)
+    return [x.transpose(0, 2, 1, 3).reshape(n * page, H, d) for x in (k, v)]
+
+
+class Wide(Chosen):
+    """Tables of many entries over a pool of any bytes (entries may name a page again), lists of many entries; some rows are checked."""
+
+    def __init__(self, seed, lengths, N, Hq, H, d, page, budget, dtype, entries, n_pages=40, q_len=None, keep=None, kind="sorted"):
+        import torch
+        rng = np.random.default_rng(seed)
+        B = len(lengths)
+        self.B, self.N, self.Hq, self.H, self.d, self.page, self.budget, self.dtype, self.layout, self.lengths = B, N, Hq, H, d, page, budget, dtype, "tokens", lengths
+        self.entries, self.scale = entries, 1 / np.sqrt(d)
+        self.pool = rng.integers(0, 256, (n_pages, H, ref.page_bytes(page, d))).astype(np.uint8)
+        codes = page * d // 2
+        for o in (codes, 2 * codes + page * d // 32):
+            self.pool[:, :, o:o + page * d // 32] = rng.integers(124, 128, (n_pages, H, page * d // 32))
+        self.k, self.v = decoded(self.pool, d, page)
+        self.table = rng.integers(0, n_pages, (B, entries)).astype(np.int32)
+        self.table[rng.random(self.table.shape) < 0.02] = n_pages
+        q = torch.from_numpy(rng.standard_normal((B, N, Hq, d)) * 0.3).to(torch.bfloat16 if dtype == BF16 else torch.float32)
+        self.q, self.qh = q.cuda(), q.double().numpy()
+        self.q_len = None if q_len is None else np.asarray(q_len, np.int32)
+        self.keep = None if keep is None else (rng.random((B, entries * page)) < keep).astype(np.uint8)
+        self.lists = np.full((B, N, H, budget), -1, np.int32)
+        for b, i, h in np.ndindex(B, N, H):
+            if kind == "any":
+                pick = rng.integers(-2, entries + 2, budget)
+                if i % 3 == 0:                           # long runs that ascend, and some that do not
+                    pick[:budget * 3 // 4] = np.sort(pick[:budget * 3 // 4])
+            else:
+                pick = np.sort(rng.choice(entries, min(budget, entries), replace=False))
+            self.lists[b, i, h, :len(pick)] = pick
+
+    def check_some(self, out, lse, seed=0, n=60):
+        rng = np.random.default_rng(seed)
+        step, part = (2.0 ** -8, 2.0 ** -16) if self.dtype == BF16 else (2.0 ** -24, 2.0 ** -23)
+        G, cap, page = self.Hq // self.H, self.entries * self.page, self.page
+        rows = [self.N if self.q_len is None else int(np.clip(self.q_len[b], 0, self.N)) for b in range(self.B)]
+        for b, nq in enumerate(rows):
+            assert (out[b, nq:] == 7).all() and (lse[b, :, nq:] == 7).all(), f"sample {b}: rows behind the last were written"
+        picks = [(b, i, h) for b, nq in enumerate(rows) for i in {0, 1, nq - 1, nq - 2} if 0 <= i < nq for h in (0, self.H - 1)]
+        picks = [picks[x] for x in rng.permutation(len(picks))[:n // 2]]
+        while len(picks) < n:
+            b = int(rng.integers(self.B))
+            if rows[b]:
+                picks.append((b, int(rng.integers(rows[b])), int(rng.integers(self.H))))
+        for b, i, h in picks:
+            seen = cr.seen(self.lengths[b], rows[b], i, cap)
+            pages = np.array([e for e in cr.listed(self.lists[b, i, h], self.entries) if 0 <= self.table[b, e] < len(self.pool)], np.int64)
+            at = (pages[:, None] * page + np.arange(page)).reshape(-1)
+            on = at < seen
+            if self.keep is not None:
+                on &= self.keep[b, at] != 0
+            slot = (self.table[b, at // page].astype(np.int64) * page + at % page)[on]
+            g = slice(h * G, (h + 1) * G)
+            there = np.ones(len(slot), bool)
+            want, wlse, size, score = ref.attend_heads(self.qh[b, i:i + 1, g], self.k[slot, h:h + 1], self.v[slot, h:h + 1], there, len(slot), 1, self.scale) \
+                if len(slot) else (np.zeros((1, G, self.d)), np.full((1, G), -np.inf), np.zeros((1, G, self.d)), np.zeros((1, G)))
+            bound, lb = ref.attend_bounds(want, wlse, size, score, self.d, len(slot), step, part)
+            off = np.abs(out[b, i, g] - want[0]) - bound[0]
+            assert (off <= 0).all(), (b, i, h, len(slot), off.max())
+            empty = np.isneginf(wlse[0])
+            assert np.array_equal(np.isneginf(lse[b, g, i]), empty), (b, i, h, "empty rows")
+            assert np.where(empty, True, np.abs(lse[b, g, i] - np.where(empty, 0, wlse[0])) <= lb[0]).all(), (b, i, h, "lse")
+
+
+WIDE = [
+    # several tokens together: sixteen over a table of 601 entries, blocks of eight waves
+    dict(lengths=[9000], N=768, Hq=2, H=2, d=64, page=16, budget=64, dtype=BF16, entries=601),
+    # four over a table of 4096, joint lists of up to 1024: the most LDS, eight waves
+    dict(lengths=[65500], N=192, Hq=32, H=8, d=128, page=16, budget=256, dtype=BF16, entries=4096),
+    # two over a table of 4096, joint lists of 1024, more than 512 blocks of four waves
+    dict(lengths=[65536, 40000], N=130, Hq=64, H=8, d=64, page=16, budget=512, dtype=BF16, entries=4096, q_len=[130, 77]),
+    # fp32: eight over 1100 entries, a mask, a last group of fewer tokens, a sample of none
+    dict(lengths=[17000, 9000, 400], N=131, Hq=16, H=8, d=128, page=16, budget=100, dtype=F32, entries=1100, keep=0.6, q_len=[131, 90, 0]),
+    # lists in any order of more than 64 entries, rows before the first entry
+    dict(lengths=[40, 30000], N=300, Hq=4, H=4, d=64, page=32, budget=130, dtype=F32, entries=950, kind="any"),
+    dict(lengths=[20000, 100], N=400, Hq=6, H=2, d=128, page=16, budget=200, dtype=BF16, entries=1030, kind="any", keep=0.5),
+    # joint lists as long as the table, in pages of 64: 990 entries of 1000 tokens' sixteenths
+    dict(lengths=[63300], N=400, Hq=4, H=4, d=64, page=64, budget=500, dtype=BF16, entries=990),
+    # one token: lists of 1024 entries in one part, eight waves
+    dict(lengths=[17600 - 11 * b for b in range(38)], N=1, Hq=16, H=8, d=128, page=16, budget=1024, dtype=BF16, entries=1100),
+    dict(lengths=[17600 - 11 * b for b in range(70)], N=1, Hq=20, H=5, d=64, page=16, budget=1024, dtype=F32, entries=1100, keep=0.7, kind="any"),
+    # and of 1025: two parts
+    dict(lengths=[17600 - 11 * b for b in range(38)], N=1, Hq=16, H=8, d=128, page=16, budget=1025, dtype=BF16, entries=1100, keep=0.7),
+]
+
+
+@pytest.mark.parametrize("i", range(len(WIDE)))
+def test_attention_over_many_chosen_pages(i):
+    import paper_2411_10803_amd as md
+    c = Wide(400 + i, **WIDE[i])
+    c.check_some(*c.call(md), seed=i)
