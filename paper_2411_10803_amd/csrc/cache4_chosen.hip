@@ -884,7 +884,6 @@ __global__ __launch_bounds__(F32 && D == 128 ? 256 : 512, F32 && D == 128 ? 3 : 
         sw.limit[0] = (lane_id() & 15) < n * A.dim.G ? limit : 0;
         walk_of(w, A, s, u.h, 0, n * A.dim.G - 1);
         w.level = __builtin_amdgcn_readlane(limit, 0);                   // (the first token sees the least)
-        w.clear = w.keep ? 0 : w.level;
         w.list = lds_address(list);
         w.members = lds_address(members);
         w.all = (1u << n) - 1;

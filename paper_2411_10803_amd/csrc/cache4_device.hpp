@@ -194,7 +194,7 @@ struct Walk {
     uniform_ptr_t row, keep;                         // of the block table; of the mask, or null
     uint32_t pitch;                                  // 64-byte units from page to page
     int n_pages, page, page_shift, last_page;        // of the pool; tokens of a page; the table's last entry
-    int end, level, clear;                           // keys that any row sees; that all rows see; that no mask may leave out either
+    int end, level;                                  // keys that any row sees; that all rows see, but for those that a mask leaves out
     float c;                                         // softmax scale, base 2
 };
 struct Pages { int id[2]; };                         // of a step's two 16-key tiles
@@ -217,7 +217,6 @@ __device__ __forceinline__ void walk_of(Walk& w, const AttendArgs& A, const Samp
     w.page = A.p.page;
     w.end = min(max(s.length - s.nq + last_row / A.dim.G + 1, 0), s.length);
     w.level = min(max(s.length - s.nq + first_row / A.dim.G + 1, 0), w.end);
-    w.clear = A.keep ? 0 : w.level;
     w.c = A.scale * kLog2eC;
 }
 // The entries as they stand in the table, which nobody looks at yet: a wave that asks for them a step ahead does not wait for them.
@@ -362,7 +361,9 @@ struct Rows {
         const Pages known = pages_for_mask(w, step);
         const bool ok[2] = {there(w, step, known, 0), there(w, step, known, 1)};
         const Sight sight = sight_at(w, step);
-        const bool inside = step * 32 + 32 <= w.level && ok[0] && ok[1];         // (a prompt's piece has few steps that are not)
+        // (with a mask most steps are; without one a step comes here for its edge.  us, so / without `w.keep`: 4 x 512 tokens of 32 heads on 8, up to
+        // 5888 keys 199.1 / 200.2, 4 x 2048 first ones 272.2 / 273.7; with a mask 238.5 / 240.1)
+        const bool inside = w.keep && step * 32 + 32 <= w.level && ok[0] && ok[1];
         uint32_t on[2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) hides[t] = 0;
@@ -636,7 +637,7 @@ struct Sweep : Rows<D, F32, NT> {
             __builtin_amdgcn_sched_barrier(0);                   // (what is asked for before the wait for LDS is waited for with it)
             next = pages_at(w, ahead + stride);
             later = kept_at(w, i + stride);
-            bool masked = ((holes >> x) & 1) != 0 || i * 32 + 32 > w.clear, pages = false;
+            bool masked = ((holes >> x) & 1) != 0 || w.keep || i * 32 + 32 > w.level, pages = false;
             holes &= ~(1u << x);
             if (ahead < stop) {
                 if (hole(w, ahead, pg)) holes |= 1u << x;
