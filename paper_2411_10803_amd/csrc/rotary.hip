@@ -354,9 +354,9 @@ int read_rotary(const char* who, const md_rotary* r, int d, int step, int B, int
 }
 size_t position_bytes(const Angles& a) { return (size_t)a.axes * a.plane * 4; }
 size_t table_bytes(const Angles& a) { return (size_t)a.n_pos * a.turn.pairs * 8; }
-// An output that is its input, place by place.
-bool same_place(const void* x, const KvLayout& l, const void* y, const KvLayout& m) {
-    return x == y && l.batch == m.batch && l.token == m.token && l.head == m.head;
+// An output that is its input, place by place (an axis with one place may have any stride).
+bool same_place(const void* x, const KvLayout& l, const void* y, const KvLayout& m, int B, int N, int H) {
+    return x == y && (B == 1 || l.batch == m.batch) && (N == 1 || l.token == m.token) && (H == 1 || l.head == m.head);
 }
 
 int rotate_impl(const void* q, const void* k, int dtype, const int32_t* positions, const int32_t* index, const float* table, const int32_t* rows,
@@ -393,8 +393,8 @@ int rotate_impl(const void* q, const void* k, int dtype, const int32_t* position
                        {index, index ? (size_t)all * 4 : 0}, {table, table_bytes(ang)}, {rows, rows ? (size_t)B * 4 : 0}};
     for (int x = 0; x < 2 && rc == MD_OK; ++x) rc = check_apart(who, r[x], r + 2, 4);
     if (rc != MD_OK) return rc;
-    if (overlaps(qo, ko) || overlaps(qo, ki) || overlaps(ko, qi) || (!same_place(q, a.xl, q_out, a.yl) && overlaps(qo, qi)) ||
-        (!same_place(k, c.xl, k_out, c.yl) && overlaps(ko, ki)))
+    if (overlaps(qo, ko) || overlaps(qo, ki) || overlaps(ko, qi) || (!same_place(q, a.xl, q_out, a.yl, B, N, Hq) && overlaps(qo, qi)) ||
+        (!same_place(k, c.xl, k_out, c.yl, B, N, H) && overlaps(ko, ki)))
         return fail(MD_EALIAS, "rotate: the outputs and the inputs must not overlap");
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int per = 256 / items;
@@ -449,7 +449,7 @@ int append_impl(const void* q, const void* k_new, const void* v_new, int dtype, 
     rc = check_apart(who, r[0], r + 1, 8);
     if (rc == MD_OK) rc = check_apart(who, r[1], r + 2, 4);
     if (rc != MD_OK) return rc;
-    if (overlaps(qo, ki) || overlaps(qo, vi) || (!same_place(q, A.ql, q_out, A.ol) && overlaps(qo, qi)))
+    if (overlaps(qo, ki) || overlaps(qo, vi) || (!same_place(q, A.ql, q_out, A.ol, B, N, Hq) && overlaps(qo, qi)))
         return fail(MD_EALIAS, "cache4_append: the outputs and the inputs must not overlap");
     A.q = q; A.k = k_new; A.v = v_new; A.q_out = q_out; A.slots = slots; A.cache = static_cast<uint8_t*>(cache); A.Hq = Hq; A.rows = (int)rows;
     hipStream_t st = static_cast<hipStream_t>(stream);

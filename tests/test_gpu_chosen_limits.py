@@ -83,6 +83,42 @@ def test_append_of_views_of_one_projection(i):
     assert torch.equal(whole, before), "something beside the queries was written"
 
 
+@pytest.mark.parametrize("axis", ["batch", "tokens", "heads"])
+def test_in_place_whatever_the_stride_of_an_axis_with_one_place(axis):
+    """The same rows by two layouts of the C ABI that differ in nothing but such a stride."""
+    import ctypes as C
+    import torch
+    from paper_2411_10803_amd import binding
+    import paper_2411_10803_amd as md
+    torch.manual_seed(5)
+    at = ("batch", "tokens", "heads").index(axis)
+    shape = [3, 4, 5, 64]
+    whole = torch.randn(shape, device="cuda").bfloat16()
+    q = whole.narrow(at, 0, 1)
+    strides = list(q.stride()[:3])
+    lay = C.byref(md.KvLayout(*strides))
+    strides[at] = 4096
+    other = C.byref(md.KvLayout(*strides))
+    B, N, H, d = q.shape
+    table, turn = md.rotary_table(50, 32), md.rotary([32])
+    pos = torch.randint(0, 50, (1, B, N), dtype=torch.int32, device="cuda")
+    before = whole.clone()
+    want = md.mustdrop_rotate(q.contiguous(), pos, table, turn, q_out=torch.zeros(q.shape, dtype=q.dtype, device="cuda"))[0]
+    angles, by, stream = (pos.data_ptr(), None, table.data_ptr()), C.byref(turn), torch.cuda.current_stream().cuda_stream
+    binding._call("mustdrop_rotate", q.data_ptr(), None, 1, *angles, None, B, N, N, H, 0, d, 50, by, 0, q.data_ptr(), None, lay, None, other, None, stream)
+    torch.cuda.synchronize()
+    assert torch.equal(q, want)
+    q.copy_(before.narrow(at, 0, 1))
+    cache, k = md.cache4_buffer(2, 16, 2, 64), torch.randn((B, N, 2, d), device="cuda").bfloat16()
+    slots = torch.arange(B * N, dtype=torch.int32, device="cuda").reshape(B, N).contiguous()
+    binding._call("mustdrop_cache4_append", q.data_ptr(), k.data_ptr(), k.data_ptr(), 1, *angles, slots.data_ptr(), cache.data_ptr(), B, N, N, H, 2, d, 50, 2, 16, by,
+                  q.data_ptr(), lay, None, other, stream)
+    torch.cuda.synchronize()
+    assert torch.equal(q, want)
+    q.copy_(before.narrow(at, 0, 1))
+    assert torch.equal(whole, before)
+
+
 def test_views_that_share_bytes_are_refused():
     import torch
     import paper_2411_10803_amd as md
