@@ -498,7 +498,8 @@ int mustdrop_cache4_bounds(
  * the nearest (of two as near the even one), within -127 and 127; all 0 where a is 0 or no finite number.  A page's score is
  *   2^e * sum over the G queries and the channels of max(q * largest, q * smallest)
  * with the page's bounds, summed in whole numbers and rounded to fp32 once: no key of the page has a larger sum of its scores with the
- * rounded queries.  Where scales is 255 the score is +infinity; where the table names no page, -infinity.
+ * rounded queries.  The choice does not know the `keep` of the attention: a page keeps its score and its place in the budget whatever a mask leaves
+ * out of it, all of its entries too (a copy of the block table that names no page there keeps such pages out of the choice).  Where scales is 255 the score is +infinity; where the table names no page, -infinity.
  * Of the P pages that the token sees, the first first_pages and the last last_pages are taken, then those with the highest scores, of
  * equal ones the first, until there are min(budget, P).
  *   q [B, N, Hq, d] (dtype; q_layout);  q_len [B] i32 or NULL (= N)

@@ -1,8 +1,10 @@
 // Attention over a part of the cache held in 4 bits.
 //
 //   cache4_bounds_kernel          each page's largest and smallest key values, channel by channel, in 8 bits
+//   cache4_score_choose_kernel    bounds and queries -> scores in LDS -> the pages to read, for up to 2048 pages and blocks enough
 //   cache4_score_kernel           bounds and queries -> a score for each token, K/V head and page
-//   cache4_choose_kernel          scores -> the pages to read
+//   cache4_choose_block_kernel    scores -> the pages to read, for up to 8192 of them, in registers
+//   cache4_choose_kernel          the same for any number, which it looks up again and again
 //   cache4_attend_chosen_kernel   softmax(scale Q K^T) V over them
 //   cache4_attend_shared_kernel   the same for several tokens together, over all of their pages
 //   cache4_attend_chosen_join_kernel   what parts of a list have given, put together
